@@ -265,6 +265,84 @@ int lnmod_qknorm_backward_io(const void* dq_out, const void* dk_out, const void*
 /* Bytes of device workspace lnmod_qknorm_backward needs (0 for invalid arguments).  Host-only. */
 size_t lnmod_qknorm_backward_workspace_bytes(int64_t N, int64_t D);
 
+/*
+ * Activations in 8 bits.  A group of `group` consecutive features of a row (32, 64 or 128; the last group of a row may be
+ * shorter) shares one float32 scale:
+ *
+ *     amax = max |v|     s = max(amax, 2^-100) / Q     r = 1 / s     (both rounded to float32)     Q = 127 or 448
+ *     LNMOD_INT8   code = v*r rounded to the nearest whole number, ties to even: one rounding; |code| <= 127
+ *     LNMOD_E4M3   code = v*r rounded to float32, then to the nearest OCP e4m3, ties to even; at most 448
+ *
+ * The code stands for code*s.  A group that holds an infinity or a NaN has s = NaN and the codes 0: it stands for NaN in
+ * every place.  codes: [N, D] bytes, 16-byte aligned; code_scales: float32 [N, ceil(D / group)], at any float's address.
+ * In these calls D is a multiple of 8 in either element type, and an unknown `code` or `group` is LNMOD_EINVAL.
+ */
+typedef enum { LNMOD_INT8 = 0, LNMOD_E4M3 = 1 } lnmod_code;
+
+/*
+ * The 8-bit checkpoint of a tensor and the way back: x [N, D] in the I/O dtype.  D is a multiple of 8, 8 <= D <= 2^20.
+ * The codes are the same bit for bit whatever call forms them (lnmod_quantize or lnmod_forward_ckpt).
+ * lnmod_dequantize forms code*s in float32 and rounds it once to the I/O dtype; its group may be 0, for codes with one
+ * scale for a row (code_scales [N], see lnmod_rmsnorm_quant_forward).
+ */
+int lnmod_quantize(const void* x, int64_t N, int64_t D, int64_t group, void* stream,
+                   void* codes, float* code_scales, int dtype, int code);
+int lnmod_dequantize(const void* codes, const float* code_scales, int64_t N, int64_t D, int64_t group,
+                     void* stream, void* x, int dtype, int code);
+
+/*
+ * LayerNorm-Modulate whose backward reads an 8-bit checkpoint in x's place.  The forward is lnmod_forward (cu_seqlens NULL:
+ * B samples of S tokens, modulation rows by `mod`) or lnmod_forward_varlen (cu_seqlens given: LNMOD_PER_SAMPLE only) and
+ * writes the codes of x in the same pass; y, mean and rstd are those of x itself.  mean and rstd are required.
+ * The backward is lnmod_backward's with x' = code*s for x:
+ *
+ *     xhat = (x' - mean_n) * rstd_n,     and g, c1, c2, dx, dshift, dscale as at the top
+ *
+ * LNMOD_PER_SAMPLE: dshift, dscale are [B, D] / [nseg, D], float32, or in the I/O dtype where io_grads is not 0, and the
+ * workspace holds lnmod_backward_ckpt_workspace_bytes() bytes (query for each problem).  LNMOD_PER_TOKEN: dshift,
+ * dscale are [B, S, D] in the I/O dtype; io_grads and the workspace are not looked at.
+ */
+int lnmod_forward_ckpt(const void* x, const void* shift, const void* scale, const int32_t* cu_seqlens,
+                       int64_t B_or_nseg, int64_t S_or_T, int64_t D, float eps, int64_t group, void* stream,
+                       void* y, void* codes, float* code_scales, float* mean, float* rstd,
+                       int dtype, int mod, int code);
+int lnmod_backward_ckpt(const void* dy, const void* codes, const float* code_scales, const void* scale,
+                        const int32_t* cu_seqlens, int64_t B_or_nseg, int64_t S_or_T, int64_t D, int64_t group,
+                        void* stream, const float* mean, const float* rstd, void* dx, void* dshift, void* dscale,
+                        void* workspace, size_t workspace_bytes, int dtype, int mod, int code, int io_grads);
+
+/* Bytes of device workspace lnmod_backward_ckpt needs with LNMOD_PER_SAMPLE (0 for invalid arguments).  Host-only. */
+size_t lnmod_backward_ckpt_workspace_bytes(int64_t B_or_nseg, int64_t total_tokens, int64_t D);
+
+/*
+ * Root-mean-square norm with the residual's addition and an output in 8 bits:
+ *
+ *     h[n,d] = x[n,d] + r[n,d]      one float32 addition rounded once to the I/O dtype, and stored
+ *     rstd_n = 1/sqrt((1/D) sum_d h[n,d]^2 + eps)     v[n,d] = (h[n,d]*rstd_n) * w[d]
+ *
+ * x, r, h: [N, D]; w: [D]; rstd: float32 [N] (written).  r and h are both NULL where there is no residual; h is x then.
+ * Either codes and code_scales are given, and hold the codes of v, or y [N, D] in the I/O dtype, which holds the values that
+ * those codes stand for (for training with the rounding in the loop); the other is NULL.  group 0: one scale for a whole
+ * row, code_scales [N].  There the largest |v| is formed as rstd_n times the largest |h*w|.
+ *
+ * Backward, straight through the rounding to codes; dh: gradient that reaches h along the residual stream, or NULL:
+ *
+ *     hhat = h*rstd     g = dy*w     c_n = (1/D) sum_d g*hhat
+ *     dx[n,d] = dh[n,d] + rstd_n*(g - hhat*c_n)     dw[d] = sum_n dy[n,d]*hhat[n,d]
+ *
+ * dx is the gradient of x and of r.  dw: [D], float32 (any float's address), or in the I/O dtype and 16-byte aligned where
+ * io_grads is not 0; zeros when N == 0.  workspace: lnmod_rmsnorm_quant_backward_workspace_bytes(N, D) bytes.
+ */
+int lnmod_rmsnorm_quant_forward(const void* x, const void* r, const void* w, int64_t N, int64_t D, float eps,
+                                int64_t group, void* stream, void* h, void* codes, float* code_scales, void* y,
+                                float* rstd, int dtype, int code);
+int lnmod_rmsnorm_quant_backward(const void* dy, const void* dh, const void* h, const void* w, int64_t N, int64_t D,
+                                 void* stream, const float* rstd, void* dx, void* dw,
+                                 void* workspace, size_t workspace_bytes, int dtype, int io_grads);
+
+/* Bytes of device workspace lnmod_rmsnorm_quant_backward needs (0 for invalid arguments).  Host-only. */
+size_t lnmod_rmsnorm_quant_backward_workspace_bytes(int64_t N, int64_t D);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,11 +26,13 @@ TORCH_MODULE = os.path.join(HERE, "_lnmod_torch.so")
 
 KERNEL_SOURCES = ["lnmod_fwd.hip", "lnmod_bwd.hip", "lnmod_gated_fwd.hip", "lnmod_gated_bwd.hip",
                   "lnmod_qknorm.hip"]
-LIBRARY_SOURCES = KERNEL_SOURCES + ["lnmod_static_ws.hip", "lnmod_api.cpp", "lnmod_sched.cpp"]
+LIBRARY_SOURCES = KERNEL_SOURCES + ["lnmod_quant.hip", "lnmod_ckpt.hip", "lnmod_rmsq.hip", "lnmod_static_ws.hip", "lnmod_api.cpp", "lnmod_sched.cpp"]
 TOOLS_SOURCES = KERNEL_SOURCES + ["lnmod_misc.hip", "lnmod_tools_api.cpp"]
 SOURCES = LIBRARY_SOURCES + [s for s in TOOLS_SOURCES if s not in LIBRARY_SOURCES]
 HEADERS = [os.path.join(CSRC, "lnmod_kernels.hpp"), os.path.join(CSRC, "lnmod_launch.hpp"),
            os.path.join(CSRC, "lnmod_gated_kernels.hpp"), os.path.join(CSRC, "lnmod_qknorm_kernels.hpp"),
+           os.path.join(CSRC, "lnmod_code.hpp"), os.path.join(CSRC, "lnmod_quant_kernels.hpp"),
+           os.path.join(CSRC, "lnmod_ckpt_kernels.hpp"), os.path.join(CSRC, "lnmod_rmsq_kernels.hpp"),
            os.path.join(CSRC, "lnmod_api_impl.hpp"),
            os.path.join(INCLUDE, "lnmod.h"), os.path.join(INCLUDE, "lnmod_sched.h"),
            os.path.join(INCLUDE, "lnmod_tools.h")]

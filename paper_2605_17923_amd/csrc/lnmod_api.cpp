@@ -115,6 +115,35 @@ int qknorm_backward_impl(const void* dq_out, const void* dk_out, const void* q, 
     return e == hipSuccess ? LNMOD_OK : LNMOD_ELAUNCH;
 }
 
+// ---- activations in 8 bits -------------------------------------------------------------------------------------
+bool valid_group(int64_t group) { return group == 32 || group == 64 || group == 128; }
+bool valid_code(int code) { return code == LNMOD_INT8 || code == LNMOD_E4M3; }
+
+int check_rows(int64_t N, int64_t D, int64_t group, int dtype, int code) {
+    if (N < 0 || N >= (int64_t(1) << 31) || D < 0 || !valid_group(group) || !valid_code(code)) return LNMOD_EINVAL;
+    if (dtype != LNMOD_BF16 && dtype != LNMOD_F32) return LNMOD_EINVAL;
+    if (D < 8 || D > (int64_t(1) << 20) || D % 8 != 0) return LNMOD_EUNSUPPORTED;
+    return LNMOD_OK;
+}
+
+size_t ckpt_workspace_bytes(int64_t nseg, int64_t T, int64_t D) {
+    int64_t slots = 0;
+    for (int dtype = 0; dtype < 2; ++dtype) {
+        const int64_t s = lnmod::bwd_slots(lnmod::ckpt_bwd_plan(T, nseg, D, dtype), nseg);
+        if (s > slots) slots = s;
+    }
+    return static_cast<size_t>(slots) * 2u * static_cast<size_t>(D) * sizeof(float);
+}
+
+size_t rmsq_workspace_bytes(int64_t N, int64_t D) {
+    int64_t nb = 0;
+    for (int dtype = 0; dtype < 2; ++dtype) {
+        const int64_t b = lnmod::rmsq_bwd_blocks(N, D, dtype);
+        if (b > nb) nb = b;
+    }
+    return static_cast<size_t>(nb) * static_cast<size_t>(D) * sizeof(float);
+}
+
 }  // namespace
 
 extern "C" {
@@ -311,6 +340,136 @@ size_t lnmod_qknorm_backward_workspace_bytes(int64_t N, int64_t D) {
     if (N < 0 || N >= (int64_t(1) << 31)) return 0;
     if (D < 8 || D > lnmod::kMaxD || D % 4 != 0) return 0;
     return qknorm_workspace_bytes(N, D);
+}
+
+int lnmod_quantize(const void* x, int64_t N, int64_t D, int64_t group, void* stream, void* codes,
+                   float* code_scales, int dtype, int code) {
+    const int st = check_rows(N, D, group, dtype, code);
+    if (st != LNMOD_OK) return st;
+    if (N == 0) return LNMOD_OK;
+    if (!x || !codes || !code_scales) return LNMOD_EINVAL;
+    if (!aligned16(x) || !aligned16(codes)) return LNMOD_EALIGN;
+    const hipError_t e = lnmod::launch_quantize(dtype, code, x, N, D, group, codes, code_scales, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LNMOD_OK : LNMOD_ELAUNCH;
+}
+
+int lnmod_dequantize(const void* codes, const float* code_scales, int64_t N, int64_t D, int64_t group, void* stream,
+                     void* x, int dtype, int code) {
+    const int st = check_rows(N, D, group == 0 ? 32 : group, dtype, code);
+    if (st != LNMOD_OK) return st;
+    if (N == 0) return LNMOD_OK;
+    if (!x || !codes || !code_scales) return LNMOD_EINVAL;
+    if (!aligned16(x) || !aligned16(codes)) return LNMOD_EALIGN;
+    const hipError_t e = lnmod::launch_dequantize(dtype, code, codes, code_scales, N, D, group, x, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LNMOD_OK : LNMOD_ELAUNCH;
+}
+
+int lnmod_forward_ckpt(const void* x, const void* shift, const void* scale, const int32_t* cu_seqlens,
+                       int64_t B_or_nseg, int64_t S_or_T, int64_t D, float eps, int64_t group, void* stream, void* y,
+                       void* codes, float* code_scales, float* mean, float* rstd, int dtype, int mod, int code) {
+    int64_t S, T;
+    if (!gated_shape(cu_seqlens, B_or_nseg, S_or_T, &S, &T)) return LNMOD_EINVAL;
+    if (mod != LNMOD_PER_SAMPLE && (mod != LNMOD_PER_TOKEN || cu_seqlens)) return LNMOD_EINVAL;
+    if (!valid_group(group) || !valid_code(code)) return LNMOD_EINVAL;
+    const int st = check_shape(B_or_nseg, S_or_T, D, eps, dtype, T);
+    if (st != LNMOD_OK) return st;
+    if (D % 8 != 0) return LNMOD_EUNSUPPORTED;
+    if (T == 0) return LNMOD_OK;
+    if (B_or_nseg == 0) return LNMOD_EINVAL;
+    if (!x || !shift || !scale || !y || !codes || !code_scales || !mean || !rstd) return LNMOD_EINVAL;
+    if (!aligned16(x) || !aligned16(shift) || !aligned16(scale) || !aligned16(y) || !aligned16(codes)) return LNMOD_EALIGN;
+    const Problem p{dtype, cu_seqlens, B_or_nseg, S, T, D, eps};
+    const hipError_t e = lnmod::launch_ckpt_fwd(p, mod == LNMOD_PER_TOKEN, x, shift, scale, y, {codes, code_scales, group},
+                                                code, mean, rstd, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LNMOD_OK : LNMOD_ELAUNCH;
+}
+
+int lnmod_backward_ckpt(const void* dy, const void* codes, const float* code_scales, const void* scale,
+                        const int32_t* cu_seqlens, int64_t B_or_nseg, int64_t S_or_T, int64_t D, int64_t group,
+                        void* stream, const float* mean, const float* rstd, void* dx, void* dshift, void* dscale,
+                        void* workspace, size_t workspace_size, int dtype, int mod, int code, int io_grads) {
+    int64_t S, T;
+    if (!gated_shape(cu_seqlens, B_or_nseg, S_or_T, &S, &T)) return LNMOD_EINVAL;
+    if (mod != LNMOD_PER_SAMPLE && (mod != LNMOD_PER_TOKEN || cu_seqlens)) return LNMOD_EINVAL;
+    if (!valid_group(group) || !valid_code(code)) return LNMOD_EINVAL;
+    const int st = check_shape(B_or_nseg, S_or_T, D, 1.0f, dtype, T);
+    if (st != LNMOD_OK) return st;
+    if (D % 8 != 0) return LNMOD_EUNSUPPORTED;
+    const bool token = mod == LNMOD_PER_TOKEN;
+    const hipStream_t hs = static_cast<hipStream_t>(stream);
+    if (T == 0) {
+        if (token || B_or_nseg == 0) return LNMOD_OK;
+        if (!dshift || !dscale) return LNMOD_EINVAL;               // empty sums are zeros
+        if (!aligned16(dshift) || !aligned16(dscale)) return LNMOD_EALIGN;
+        const int64_t n = grad_floats(B_or_nseg * D, dtype, io_grads != 0);
+        hipError_t e = lnmod::launch_zero_f32(static_cast<float*>(dshift), n, hs);
+        if (e == hipSuccess) e = lnmod::launch_zero_f32(static_cast<float*>(dscale), n, hs);
+        return e == hipSuccess ? LNMOD_OK : LNMOD_ELAUNCH;
+    }
+    if (B_or_nseg == 0) return LNMOD_EINVAL;
+    if (!dy || !codes || !code_scales || !scale || !mean || !rstd || !dx || !dshift || !dscale) return LNMOD_EINVAL;
+    if (!aligned16(dy) || !aligned16(codes) || !aligned16(scale) || !aligned16(dx) || !aligned16(dshift) || !aligned16(dscale))
+        return LNMOD_EALIGN;
+    if (!token) {
+        if (!workspace || workspace_size < ckpt_workspace_bytes(B_or_nseg, T, D)) return LNMOD_EWORKSPACE;
+        if (!aligned16(workspace)) return LNMOD_EALIGN;
+    }
+    const Problem p{dtype, cu_seqlens, B_or_nseg, S, T, D, 1.0f};
+    const hipError_t e = lnmod::launch_ckpt_bwd(p, token, dy, {const_cast<void*>(codes), const_cast<float*>(code_scales), group},
+                                                code, scale, mean, rstd, dx, dshift, dscale, io_grads != 0,
+                                                static_cast<float*>(workspace), hs);
+    return e == hipSuccess ? LNMOD_OK : LNMOD_ELAUNCH;
+}
+
+size_t lnmod_backward_ckpt_workspace_bytes(int64_t B_or_nseg, int64_t total, int64_t D) {
+    if (B_or_nseg < 0 || total < 0 || total >= (int64_t(1) << 31)) return 0;
+    if (D < 8 || D > lnmod::kMaxD || D % 8 != 0) return 0;
+    return ckpt_workspace_bytes(B_or_nseg, total, D);
+}
+
+int lnmod_rmsnorm_quant_forward(const void* x, const void* r, const void* w, int64_t N, int64_t D, float eps,
+                                int64_t group, void* stream, void* h, void* codes, float* code_scales, void* y,
+                                float* rstd, int dtype, int code) {
+    if ((group != 0 && !valid_group(group)) || !valid_code(code)) return LNMOD_EINVAL;
+    const int st = check_shape(1, N, D, eps, dtype, N);
+    if (st != LNMOD_OK) return st;
+    if (D % 8 != 0) return LNMOD_EUNSUPPORTED;
+    if (N == 0) return LNMOD_OK;
+    if (!x || !w || !rstd || (r == nullptr) != (h == nullptr)) return LNMOD_EINVAL;
+    if ((codes == nullptr) == (y == nullptr) || (codes == nullptr) != (code_scales == nullptr)) return LNMOD_EINVAL;
+    if (!aligned16(x) || !aligned16(r) || !aligned16(w) || !aligned16(h) || !aligned16(codes) || !aligned16(y))
+        return LNMOD_EALIGN;
+    const hipError_t e = lnmod::launch_rmsq_fwd(dtype, code, x, r, w, N, D, eps, group, h, y ? y : codes, code_scales, rstd,
+                                                y != nullptr, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LNMOD_OK : LNMOD_ELAUNCH;
+}
+
+int lnmod_rmsnorm_quant_backward(const void* dy, const void* dh, const void* h, const void* w, int64_t N, int64_t D,
+                                 void* stream, const float* rstd, void* dx, void* dw, void* workspace,
+                                 size_t workspace_size, int dtype, int io_grads) {
+    const int st = check_shape(1, N, D, 1.0f, dtype, N);
+    if (st != LNMOD_OK) return st;
+    if (D % 8 != 0) return LNMOD_EUNSUPPORTED;
+    const hipStream_t hs = static_cast<hipStream_t>(stream);
+    if (!dw) return LNMOD_EINVAL;
+    if (io_grads && !aligned16(dw)) return LNMOD_EALIGN;
+    if (N == 0) {                                                  // empty sums are zeros
+        const hipError_t e = lnmod::launch_zero_f32(static_cast<float*>(dw), grad_floats(D, dtype, io_grads != 0), hs);
+        return e == hipSuccess ? LNMOD_OK : LNMOD_ELAUNCH;
+    }
+    if (!dy || !h || !w || !rstd || !dx) return LNMOD_EINVAL;
+    if (!aligned16(dy) || !aligned16(dh) || !aligned16(h) || !aligned16(w) || !aligned16(dx)) return LNMOD_EALIGN;
+    if (!workspace || workspace_size < rmsq_workspace_bytes(N, D)) return LNMOD_EWORKSPACE;
+    if (!aligned16(workspace)) return LNMOD_EALIGN;
+    const hipError_t e = lnmod::launch_rmsq_bwd(dtype, dy, dh, h, w, N, D, rstd, dx, dw, io_grads != 0,
+                                                static_cast<float*>(workspace), hs);
+    return e == hipSuccess ? LNMOD_OK : LNMOD_ELAUNCH;
+}
+
+size_t lnmod_rmsnorm_quant_backward_workspace_bytes(int64_t N, int64_t D) {
+    if (N < 0 || N >= (int64_t(1) << 31)) return 0;
+    if (D < 8 || D > lnmod::kMaxD || D % 8 != 0) return 0;
+    return rmsq_workspace_bytes(N, D);
 }
 
 }  // extern "C"

@@ -1,0 +1,209 @@
+// lnmod_code.hpp -- gfx950 device code shared by the kernels that hold activations in 8 bits: rows in units of eight
+// features per lane, codes of a group of features with one scale, and the way back.
+//
+//   amax = max |v| of the group    s = fp32(max(amax, 2^-100) / Q)    r = fp32(1 / s)    Q = 127 (int8), 448 (e4m3)
+//   int8: code = v*r to the nearest whole number, ties to even, in one rounding
+//   e4m3: code = v*r rounded to fp32, then to the nearest e4m3, ties to even
+//   the code stands for code*s.  A group that holds an infinity or a NaN has s = NaN and the codes 0.
+//
+// The codes are a function of the group's values alone, bit for bit: both quotients are correctly rounded, so any
+// program that follows these lines gets the same codes.  |v*r| stays below Q (1 + 2^-21), which rounds to Q.  The floor
+// of 2^-100 keeps s and r normal numbers; a group of zeros has the codes 0.
+#pragma once
+#include "lnmod_kernels.hpp"
+
+namespace lnmod {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kUnit = 8;                     // features per lane and chunk, in either element type
+
+// ---- eight features of a row in one lane ------------------------------------------------------------------------
+template <typename Tag> struct Unit;
+
+template <> struct Unit<bf16_io> {
+    static constexpr int NV = 1;             // 16-byte vectors
+    static constexpr uint32_t kBytes = 16;
+    __device__ static inline void unpack(const u32x4 (&q)[1], float (&v)[8]) { IO<bf16_io>::unpack(q[0], v); }
+    __device__ static inline void pack(const float (&v)[8], u32x4 (&q)[1]) { q[0] = IO<bf16_io>::pack(v); }
+    // bits of the largest |v| as fp32, NaN above infinity above every number
+    __device__ static inline uint32_t amax_bits(const u32x4 (&q)[1]) {
+        u16x2 m = __builtin_bit_cast(u16x2, q[0][0] & 0x7fff7fffu);
+#pragma unroll
+        for (int j = 1; j < 4; ++j) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, q[0][j] & 0x7fff7fffu));
+        const uint32_t b = __builtin_bit_cast(uint32_t, m);
+        const uint32_t lo = b << 16, hi = b & 0xffff0000u;
+        return lo > hi ? lo : hi;
+    }
+};
+
+template <> struct Unit<f32_io> {
+    static constexpr int NV = 2;
+    static constexpr uint32_t kBytes = 32;
+    __device__ static inline void unpack(const u32x4 (&q)[2], float (&v)[8]) {
+        const f32x4 a = __builtin_bit_cast(f32x4, q[0]), b = __builtin_bit_cast(f32x4, q[1]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[j] = a[j];
+            v[4 + j] = b[j];
+        }
+    }
+    __device__ static inline void pack(const float (&v)[8], u32x4 (&q)[2]) {
+        const f32x4 a = {v[0], v[1], v[2], v[3]}, b = {v[4], v[5], v[6], v[7]};
+        q[0] = __builtin_bit_cast(u32x4, a);
+        q[1] = __builtin_bit_cast(u32x4, b);
+    }
+    __device__ static inline uint32_t amax_bits(const u32x4 (&q)[2]) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t b = q[h][j] & 0x7fffffffu;
+                m = b > m ? b : m;
+            }
+        }
+        return m;
+    }
+};
+
+template <typename Tag>
+__device__ inline void load_unit(const void* base, int64_t uniform_off, uint32_t chunk, u32x4 (&q)[Unit<Tag>::NV]) {
+#pragma unroll
+    for (int h = 0; h < Unit<Tag>::NV; ++h) q[h] = load16_u(base, uniform_off, chunk * Unit<Tag>::kBytes + 16u * h);
+}
+template <typename Tag>
+__device__ inline void load_unit_cached(const void* base, int64_t uniform_off, uint32_t chunk, u32x4 (&q)[Unit<Tag>::NV]) {
+#pragma unroll
+    for (int h = 0; h < Unit<Tag>::NV; ++h)
+        q[h] = load16_cached(base, uniform64(uniform_off), chunk * Unit<Tag>::kBytes + 16u * h);
+}
+template <typename Tag>
+__device__ inline void store_unit(void* base, int64_t uniform_off, uint32_t chunk, const u32x4 (&q)[Unit<Tag>::NV]) {
+#pragma unroll
+    for (int h = 0; h < Unit<Tag>::NV; ++h) store16_u(base, uniform_off, chunk * Unit<Tag>::kBytes + 16u * h, q[h]);
+}
+template <int NV>
+__device__ inline void clear(u32x4 (&q)[NV]) {
+#pragma unroll
+    for (int h = 0; h < NV; ++h) q[h] = u32x4{0u, 0u, 0u, 0u};
+}
+template <int NV>
+__device__ inline void opaque(u32x4 (&q)[NV]) {        // the fp32 values are rebuilt behind this, not carried across it
+#pragma unroll
+    for (int h = 0; h < NV; ++h) asm volatile("" : "+v"(q[h]));
+}
+
+// Eight codes are eight bytes of a lane.
+__device__ inline u32x2 load_codes(const void* base, int64_t uniform_off, uint32_t chunk) {
+    return __builtin_nontemporal_load(
+        reinterpret_cast<const u32x2*>(static_cast<const char*>(base) + uniform64(uniform_off) + chunk * 8u));
+}
+__device__ inline void store_codes(void* base, int64_t uniform_off, uint32_t chunk, const u32x2& c) {
+    __builtin_nontemporal_store(c, reinterpret_cast<u32x2*>(static_cast<char*>(base) + uniform64(uniform_off) + chunk * 8u));
+}
+
+// ---- largest magnitude of a group: 4, 8 or 16 consecutive lanes, inside one DPP row ----------------------------------
+template <int CTRL> __device__ inline uint32_t dpp_max(uint32_t v) {
+    const uint32_t t = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, 0xf, 0xf, false));
+    return t > v ? t : v;
+}
+// Every lane of the group returns it; all 64 lanes take part.  lanes_log2 is uniform: 2, 3 or 4.
+__device__ inline uint32_t group_max(uint32_t v, int lanes_log2) {
+    v = dpp_max<0xB1>(v);                    // quad_perm [1,0,3,2]
+    v = dpp_max<0x4E>(v);                    // quad_perm [2,3,0,1]
+    if (lanes_log2 > 2) v = dpp_max<0x141>(v);   // row_half_mirror
+    if (lanes_log2 > 3) v = dpp_max<0x140>(v);   // row_mirror
+    return v;
+}
+
+// ---- codes ------------------------------------------------------------------------------------------------------
+struct int8_code {
+    static constexpr float kLargest = 127.0f;
+};
+struct e4m3_code {
+    static constexpr float kLargest = 448.0f;
+};
+
+struct Scale {
+    float s, r;                              // r = 0 where s is NaN
+    bool good;
+};
+
+// s and r of a group.  A division costs a dozen instructions; these two are a product and two or four fused steps:
+// with c = fp32(1/Q), q = a*c and the exact remainder a - Q q, q + c (a - Q q) is the correctly rounded a / Q (Markstein's
+// theorem on division by fused multiply-add; for Q = 127 and 448 checked for every significand of a), and two Newton steps on
+// the hardware's reciprocal give the correctly rounded 1 / s (checked for every significand of s).
+template <typename C>
+__device__ inline Scale scale_of(uint32_t amax_bits) {
+    constexpr float Q = C::kLargest, c = 1.0f / Q;
+    const bool good = amax_bits < 0x7f800000u;
+    float a = __builtin_bit_cast(float, amax_bits);
+    a = good ? (a > 0x1p-100f ? a : 0x1p-100f) : 1.0f;
+    const float q = a * c;
+    const float s = __builtin_fmaf(__builtin_fmaf(-Q, q, a), c, q);
+    float r = __builtin_amdgcn_rcpf(s);
+    r = __builtin_fmaf(__builtin_fmaf(-s, r, 1.0f), r, r);
+    r = __builtin_fmaf(__builtin_fmaf(-s, r, 1.0f), r, r);
+    return Scale{good ? s : __builtin_nanf(""), good ? r : 0.0f, good};
+}
+
+template <typename C> __device__ u32x2 encode(const float (&v)[8], const Scale& sc);
+
+// 1.5 * 2^23 + code: the fused sum rounds v*r once, and the low byte of its bits is the code
+template <>
+__device__ inline u32x2 encode<int8_code>(const float (&v)[8], const Scale& sc) {
+    u32x2 w;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint32_t t[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t[j] = __builtin_bit_cast(uint32_t, __builtin_fmaf(v[4 * h + j], sc.r, 0x1.8p23f));
+        const uint32_t lo = __builtin_amdgcn_perm(t[1], t[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(t[3], t[2], 0x04000c0cu);
+        w[h] = sc.good ? lo | hi : 0u;
+    }
+    return w;
+}
+
+template <>
+__device__ inline u32x2 encode<e4m3_code>(const float (&v)[8], const Scale& sc) {
+    u32x2 w;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        int t = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h] * sc.r, v[4 * h + 1] * sc.r, 0, false);
+        t = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h + 2] * sc.r, v[4 * h + 3] * sc.r, t, true);
+        w[h] = sc.good ? static_cast<uint32_t>(t) : 0u;
+    }
+    return w;
+}
+
+// The numbers that eight codes are, not yet times the scale.
+template <typename C> __device__ void decode(const u32x2& w, float (&v)[8]);
+
+template <>
+__device__ inline void decode<int8_code>(const u32x2& w, float (&v)[8]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int t = static_cast<int>(w[h]);
+        v[4 * h] = static_cast<float>(static_cast<int8_t>(t));
+        v[4 * h + 1] = static_cast<float>(static_cast<int8_t>(t >> 8));
+        v[4 * h + 2] = static_cast<float>(static_cast<int8_t>(t >> 16));
+        v[4 * h + 3] = static_cast<float>(t >> 24);
+    }
+}
+
+template <>
+__device__ inline void decode<e4m3_code>(const u32x2& w, float (&v)[8]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(w[h]), false);
+        const f32x2 b = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(w[h]), true);
+        v[4 * h] = a[0];
+        v[4 * h + 1] = a[1];
+        v[4 * h + 2] = b[0];
+        v[4 * h + 3] = b[1];
+    }
+}
+
+}  // namespace lnmod

@@ -873,4 +873,30 @@ hipError_t launch_qknorm_bwd(int dtype, const void* dq_out, const void* dk_out, 
                              const float* rstd_q, const float* rstd_k, void* dq, void* dk,
                              void* dwq, void* dwk, bool io_grads, float* ws, hipStream_t st);
 
+
+// Activations in 8 bits.
+constexpr int group_lanes_log2(int64_t group) { return group == 32 ? 2 : group == 64 ? 3 : 4; }   // eight features a lane
+struct Checkpoint {
+    void* codes;
+    float* scales;
+    int64_t group;             // 32, 64 or 128
+};
+hipError_t launch_quantize(int dtype, int code, const void* x, int64_t N, int64_t D, int64_t group, void* codes,
+                           float* scales, hipStream_t st);
+hipError_t launch_dequantize(int dtype, int code, const void* codes, const float* scales, int64_t N, int64_t D, int64_t group,
+                             void* x, hipStream_t st);
+RowPlan ckpt_bwd_plan(int64_t T, int64_t nseg, int64_t D, int dtype, Shape* shape = nullptr, const Shape* force = nullptr);
+hipError_t launch_ckpt_fwd(const Problem& p, bool token, const void* x, const void* shift, const void* scale, void* y,
+                           const Checkpoint& c, int code, float* mean, float* rstd, hipStream_t st);
+hipError_t launch_ckpt_bwd(const Problem& p, bool token, const void* dy, const Checkpoint& c, int code, const void* scale,
+                           const float* mean, const float* rstd, void* dx, void* dshift, void* dscale, bool io_grads,
+                           float* ws, hipStream_t st);
+int64_t rmsq_bwd_blocks(int64_t N, int64_t D, int dtype);        // partial-sum slots
+hipError_t launch_rmsq_fwd(int dtype, int code, const void* x, const void* r, const void* w, int64_t N, int64_t D, float eps,
+                           int64_t group, void* h, void* out, float* scales, float* rstd, bool values, hipStream_t st,
+                           const Shape* force = nullptr);
+hipError_t launch_rmsq_bwd(int dtype, const void* dy, const void* dh, const void* h, const void* w, int64_t N, int64_t D,
+                           const float* rstd, void* dx, void* dw, bool io_grads, float* ws, hipStream_t st,
+                           const Shape* force = nullptr);
+
 }  // namespace lnmod

@@ -1,0 +1,370 @@
+// lnmod_rmsq_kernels.hpp -- gfx950 device code of the root-mean-square norm with the residual's addition and an output in
+// 8 bits.
+//
+//   h = x + r, one fp32 addition rounded once to the I/O type and stored (without a residual h is x, and not stored)
+//   rstd_n = 1/sqrt(mean_d h^2 + eps)      v = (h*rstd_n)*w
+//   out: the codes of v and their scales (lnmod_code.hpp), or in the I/O type the values that the codes stand for
+//
+// Backward, straight through the rounding to codes:
+//
+//   hhat = h*rstd   g = dy*w   c_n = mean_d g*hhat   dx = dh + rstd*(g - hhat*c)   dw[d] = sum_n dy*hhat
+//
+// With a scale for the whole row, its largest |v| is rstd times the largest |h*w|, so one barrier carries both the sum of
+// squares and the maximum; the maximum then differs from the largest |v| by two roundings at most, and a code whose v*r comes
+// out at Q (1 + 2^-21) still rounds to Q.  A group's maximum is that of v itself, as it is coded.  Layout and pipeline are those
+// of lnmod_ckpt_kernels.hpp.
+#pragma once
+#include "lnmod_code.hpp"
+
+namespace lnmod {
+
+struct RmsqFwdArgs {
+    const void* x;
+    const void* r;
+    const void* w;
+    void* h;                 // written if there is a residual
+    void* out;               // codes or values
+    float* scales;           // with codes
+    float* rstd;
+    int64_t N;
+    int32_t nb;              // blocks
+    int32_t D;
+    int32_t nchunks;         // units of a row
+    int32_t groups;          // of a row
+    int32_t lanes_log2;      // of a group; 0: the row is one
+    float eps;
+    float inv_D;
+};
+
+constexpr int rmsq_waves(int regs) {
+    const int w = 512 / regs;
+    return w > 4 ? 4 : w < 1 ? 1 : w;
+}
+
+// VALUES: out holds the values that the codes stand for.
+template <typename Tag, typename C, int VPL, int K, int R, bool RES, bool VALUES>
+__global__ __launch_bounds__(K* kWave)
+LNMOD_OCCUPANCY(rmsq_waves(VPL * (8 + R * 4 * Unit<Tag>::NV * (RES ? 4 : 2)) + 48))
+void rmsq_fwd_kernel(const RmsqFwdArgs a) {
+    using U = Unit<Tag>;
+    constexpr int NV = U::NV;
+    __shared__ float part[2][R][K][2];
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t row_bytes = static_cast<int64_t>(a.D) * IO<Tag>::kBytes;
+
+    uint32_t chunk[VPL];
+    bool ok[VPL];
+    float W[VPL][8];
+    struct Rows {
+        u32x4 x[R][VPL][NV], r[RES ? R : 1][RES ? VPL : 1][NV];
+    };
+    const auto fetch = [&](int64_t base, Rows& q) {
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int64_t row = base + j;
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) {
+                clear(q.x[j][i]);
+                if constexpr (RES) clear(q.r[j][i]);
+                if (row < a.N && ok[i]) {
+                    load_unit<Tag>(a.x, row * row_bytes, chunk[i], q.x[j][i]);
+                    if constexpr (RES) load_unit<Tag>(a.r, row * row_bytes, chunk[i], q.r[j][i]);
+                }
+            }
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+        chunk[i] = static_cast<uint32_t>((i * K + wave) * kWave + lane);
+        ok[i] = chunk[i] < static_cast<uint32_t>(a.nchunks);
+    }
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * R, step = static_cast<int64_t>(a.nb) * R;
+    Rows now;
+    fetch(first, now);
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+        u32x4 t[NV];
+        clear(t);
+        if (ok[i]) load_unit_cached<Tag>(a.w, 0, chunk[i], t);
+        U::unpack(t, W[i]);
+    }
+    int buf = 0;
+    for (int64_t base = first; base < a.N; base += step) {
+        Rows nxt;
+        fetch(base + step, nxt);
+        __builtin_amdgcn_sched_barrier(0);                   // keep the requests up here
+        float rs[R], big[R];
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int64_t row = base + j;
+            float s = 0.0f;
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) {
+                float v[8];
+                if constexpr (RES) {
+                    float rv[8];
+                    U::unpack(now.x[j][i], v);
+                    U::unpack(now.r[j][i], rv);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] += rv[e];
+                    U::pack(v, now.x[j][i]);
+                    if (row < a.N && ok[i]) store_unit<Tag>(a.h, row * row_bytes, chunk[i], now.x[j][i]);
+                }
+                U::unpack(now.x[j][i], v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    s += v[e] * v[e];
+                    const uint32_t b = __builtin_bit_cast(uint32_t, v[e] * W[i][e]) & 0x7fffffffu;
+                    top = b > top ? b : top;
+                }
+            }
+            rs[j] = wave_sum(s);
+            if (a.lanes_log2 == 0) {
+                top = group_max(top, 4);
+                const uint32_t t0 = __builtin_amdgcn_readlane(top, 0), t1 = __builtin_amdgcn_readlane(top, 16);
+                const uint32_t t2 = __builtin_amdgcn_readlane(top, 32), t3 = __builtin_amdgcn_readlane(top, 48);
+                const uint32_t u = t0 > t1 ? t0 : t1, w = t2 > t3 ? t2 : t3;
+                top = u > w ? u : w;
+            }
+            big[j] = __builtin_bit_cast(float, top);
+        }
+        if constexpr (K > 1) {
+            if (lane == 0) {
+#pragma unroll
+                for (int j = 0; j < R; ++j) {
+                    part[buf][j][wave][0] = rs[j];
+                    part[buf][j][wave][1] = big[j];
+                }
+            }
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                float s = 0.0f;
+                uint32_t top = 0;
+#pragma unroll
+                for (int w = 0; w < K; ++w) {
+                    s += part[buf][j][w][0];
+                    const uint32_t b = __builtin_bit_cast(uint32_t, part[buf][j][w][1]);
+                    top = b > top ? b : top;
+                }
+                rs[j] = s;
+                big[j] = __builtin_bit_cast(float, top);
+            }
+            buf ^= 1;
+        }
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            rs[j] = 1.0f / sqrtf(rs[j] * a.inv_D + a.eps);
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) opaque(now.x[j][i]);
+        }
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int64_t row = base + j;
+            if (row < a.N) {
+                if (wave == 0 && lane == 0) a.rstd[row] = rs[j];
+                Scale sc;
+                if (a.lanes_log2 == 0) {
+                    sc = scale_of<C>(__builtin_bit_cast(uint32_t, big[j] * rs[j]) & 0x7fffffffu);
+                    if (!VALUES && wave == 0 && lane == 0) a.scales[row] = sc.s;
+                }
+#pragma unroll
+                for (int i = 0; i < VPL; ++i) {
+                    float v[8];
+                    U::unpack(now.x[j][i], v);
+                    uint32_t top = 0;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = (v[e] * rs[j]) * W[i][e];
+                    if (a.lanes_log2 != 0) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const uint32_t b = __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu;
+                            top = b > top ? b : top;
+                        }
+                        // lanes beyond the row hold zeros, or NaN where rstd is NaN
+                        sc = scale_of<C>(group_max(ok[i] ? top : 0u, a.lanes_log2));
+                    }
+                    const u32x2 w = encode<C>(v, sc);
+                    if (ok[i]) {
+                        if constexpr (VALUES) {
+                            u32x4 o[NV];
+                            decode<C>(w, v);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v[e] *= sc.s;
+                            U::pack(v, o);
+                            store_unit<Tag>(a.out, row * row_bytes, chunk[i], o);
+                        } else {
+                            store_codes(a.out, row * a.D, chunk[i], w);
+                            if (a.lanes_log2 != 0 && (lane & ((1 << a.lanes_log2) - 1)) == 0)
+                                a.scales[uniform64(row * a.groups) + (chunk[i] >> a.lanes_log2)] = sc.s;
+                        }
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
+        now = nxt;
+    }
+}
+
+struct RmsqBwdArgs {
+    const void* dy;
+    const void* dh;
+    const void* h;
+    const void* w;
+    const float* rstd;
+    void* dx;
+    float* ws;               // [nb][D] fp32 partial dw sums
+    int64_t N;
+    int32_t nb;
+    int32_t D;
+    int32_t nchunks;
+    float inv_D;
+};
+
+template <typename Tag, int VPL, int K, int R, bool DH>
+__global__ __launch_bounds__(K* kWave)
+LNMOD_OCCUPANCY(rmsq_waves(VPL * (16 + 2 * R * 4 * Unit<Tag>::NV * (DH ? 3 : 2)) + 56))
+void rmsq_bwd_kernel(const RmsqBwdArgs a) {
+    using U = Unit<Tag>;
+    constexpr int NV = U::NV;
+    __shared__ float part[2][R][K];
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t row_bytes = static_cast<int64_t>(a.D) * IO<Tag>::kBytes;
+
+    uint32_t chunk[VPL];
+    bool ok[VPL];
+    float W[VPL][8], acc[VPL][8];
+    struct Rows {
+        u32x4 dy[R][VPL][NV], h[R][VPL][NV], dh[DH ? R : 1][DH ? VPL : 1][NV];
+        float rs[R];
+    };
+    const auto fetch = [&](int64_t base, Rows& q) {
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int64_t row = base + j;
+            const bool live = row < a.N;
+            q.rs[j] = live ? a.rstd[row] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) {
+                clear(q.dy[j][i]);
+                clear(q.h[j][i]);
+                if constexpr (DH) clear(q.dh[j][i]);
+                if (live && ok[i]) {
+                    load_unit<Tag>(a.dy, row * row_bytes, chunk[i], q.dy[j][i]);
+                    load_unit<Tag>(a.h, row * row_bytes, chunk[i], q.h[j][i]);
+                    if constexpr (DH) load_unit<Tag>(a.dh, row * row_bytes, chunk[i], q.dh[j][i]);
+                }
+            }
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+        chunk[i] = static_cast<uint32_t>((i * K + wave) * kWave + lane);
+        ok[i] = chunk[i] < static_cast<uint32_t>(a.nchunks);
+    }
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * R, step = static_cast<int64_t>(a.nb) * R;
+    Rows now;
+    fetch(first, now);
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+        u32x4 t[NV];
+        clear(t);
+        if (ok[i]) load_unit_cached<Tag>(a.w, 0, chunk[i], t);
+        U::unpack(t, W[i]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[i][e] = 0.0f;
+    }
+    int buf = 0;
+    for (int64_t base = first; base < a.N; base += step) {
+        Rows nxt;
+        fetch(base + step, nxt);
+        __builtin_amdgcn_sched_barrier(0);                   // keep the requests up here
+        float c[R];
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            float p = 0.0f;
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) {
+                float dyv[8], hv[8];
+                U::unpack(now.dy[j][i], dyv);
+                U::unpack(now.h[j][i], hv);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float t = dyv[e] * (hv[e] * now.rs[j]);
+                    p += t * W[i][e];
+                    acc[i][e] += t;
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(acc[i][e]));     // pinned here (see ckpt_bwd_kernel)
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            c[j] = wave_sum(p);
+        }
+        if constexpr (K > 1) {
+            if (lane == 0) {
+#pragma unroll
+                for (int j = 0; j < R; ++j) part[buf][j][wave] = c[j];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                float t = 0.0f;
+#pragma unroll
+                for (int w = 0; w < K; ++w) t += part[buf][j][w];
+                c[j] = t;
+            }
+            buf ^= 1;
+        }
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) {
+                opaque(now.dy[j][i]);
+                opaque(now.h[j][i]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int64_t row = base + j;
+            if (row < a.N) {
+                const float k2 = now.rs[j] * (c[j] * a.inv_D);
+#pragma unroll
+                for (int i = 0; i < VPL; ++i) {
+                    if (ok[i]) {
+                        float dyv[8], hv[8], o[8];
+                        U::unpack(now.dy[j][i], dyv);
+                        U::unpack(now.h[j][i], hv);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) o[e] = (dyv[e] * W[i][e]) * now.rs[j] - (hv[e] * now.rs[j]) * k2;
+                        if constexpr (DH) {
+                            float t[8];
+                            U::unpack(now.dh[j][i], t);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) o[e] += t[e];
+                        }
+                        u32x4 t[NV];
+                        U::pack(o, t);
+                        store_unit<Tag>(a.dx, row * row_bytes, chunk[i], t);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
+        now = nxt;
+    }
+    float* slot = a.ws + static_cast<int64_t>(blockIdx.x) * a.D;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+        if (ok[i]) {
+            f32x4* ps = reinterpret_cast<f32x4*>(slot + chunk[i] * kUnit);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) ps[q] = f32x4{acc[i][4 * q], acc[i][4 * q + 1], acc[i][4 * q + 2], acc[i][4 * q + 3]};
+        }
+    }
+}
+
+}  // namespace lnmod

@@ -11,6 +11,7 @@
 // status other than LNMOD_OK) goes back to the Python path, which raises its own errors.  The kernels,
 // their arguments and the saved tensors with their order are the same either way.
 #include <torch/extension.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_cpp_function.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -96,6 +97,7 @@ Tensor scratch(size_t bytes, const Tensor& x) {
 // ---- the Python path, for a backward that is not the plain case ------------------------------------
 py::object to_python(const Tensor& t) { return t.defined() ? py::cast(t) : py::none(); }
 py::object to_python(double v) { return py::float_(v); }
+py::object to_python(int64_t v) { return py::int_(v); }
 
 // name(args...) of functional.py, with None for an undefined tensor.  Runs on a thread of the autograd engine,
 // without the interpreter lock: no Python object is made before it is taken here.  The function's exception (a ValueError of a check, an LnmodError) is kept
@@ -293,6 +295,170 @@ struct QkNorm : public torch::autograd::Function<QkNorm> {
     }
 };
 
+// ---- activations in 8 bits -------------------------------------------------------------------------------------
+bool is_group(int64_t group) { return group == 32 || group == 64 || group == 128; }
+
+at::ScalarType type_of_code(int code) { return code == LNMOD_INT8 ? at::kChar : at::kFloat8_e4m3fn; }
+
+bool plain_codes(const Tensor& codes, at::IntArrayRef shape, const at::Device& dev) {
+    return codes.defined() && (codes.scalar_type() == at::kChar || codes.scalar_type() == at::kFloat8_e4m3fn) &&
+           plain(codes, shape, codes.scalar_type(), dev);
+}
+int code_of_codes(const Tensor& codes) { return codes.scalar_type() == at::kChar ? LNMOD_INT8 : LNMOD_E4M3; }
+
+// one scale per group of the last dimension; group 0: one per row
+std::vector<int64_t> scales_shape(at::IntArrayRef shape, int64_t group) {
+    std::vector<int64_t> s = shape.vec();
+    if (group == 0) s.pop_back();
+    else s.back() = (s.back() + group - 1) / group;
+    return s;
+}
+
+int64_t rows_of(const Tensor& t) {
+    const int64_t D = t.size(-1);
+    return t.numel() / (D > 0 ? D : 1);
+}
+
+variable_list quantize_call(const Tensor& x, int code, int64_t group) {
+    if (!plain_first(x) || x.dim() < 1 || !is_group(group)) throw NotPlain();
+    Tensor codes = at::empty(x.sizes(), x.options().dtype(type_of_code(code)));
+    Tensor scales = at::empty(scales_shape(x.sizes(), group), f32_like(x));
+    if (lnmod_quantize(ptr(x), rows_of(x), x.size(-1), group, stream_of(x), out(codes), f32_out(scales), code_of(x), code) != LNMOD_OK)
+        throw NotPlain();
+    return {codes, scales};
+}
+
+variable_list dequantize_call(const Tensor& codes, const Tensor& scales, at::ScalarType type, int64_t group) {
+    if (!codes.defined() || !codes.is_cuda() || codes.device().index() != c10::hip::current_device() || codes.dim() < 1 ||
+        !plain_codes(codes, codes.sizes(), codes.device()) || !(group == 0 || is_group(group)) ||
+        !plain(scales, scales_shape(codes.sizes(), group), at::kFloat, codes.device()) || (type != at::kBFloat16 && type != at::kFloat))
+        throw NotPlain();
+    Tensor x = at::empty(codes.sizes(), codes.options().dtype(type));
+    if (lnmod_dequantize(ptr(codes), f32(scales), rows_of(codes), codes.size(-1), group, stream_of(codes), out(x), code_of(x),
+                         code_of_codes(codes)) != LNMOD_OK)
+        throw NotPlain();
+    return {x};
+}
+
+// y, codes, scales, mean, rstd; throws NotPlain
+variable_list ckpt_forward(const Tensor& x, const Tensor& shift, const Tensor& scale, const Tensor& cu, double eps, int code,
+                           int64_t group) {
+    Batch b;
+    bool token;
+    if (!is_group(group) || !ln_shapes(x, scale, cu, &b, &token) || !plain(shift, scale.sizes(), x.scalar_type(), x.device()))
+        throw NotPlain();
+    Tensor y = at::empty_like(x), codes = at::empty(x.sizes(), x.options().dtype(type_of_code(code)));
+    Tensor scales = at::empty(scales_shape(x.sizes(), group), f32_like(x));
+    Tensor mean = at::empty(x.sizes().slice(0, x.dim() - 1), f32_like(x)), rstd = at::empty_like(mean);
+    const int st = lnmod_forward_ckpt(ptr(x), ptr(shift), ptr(scale), cu_ptr(cu), b.n, b.s_or_t, b.D, static_cast<float>(eps),
+                                      group, stream_of(x), out(y), out(codes), f32_out(scales), f32_out(mean), f32_out(rstd),
+                                      code_of(x), token ? LNMOD_PER_TOKEN : LNMOD_PER_SAMPLE, code);
+    if (st != LNMOD_OK) throw NotPlain();
+    return {y, codes, scales, mean, rstd};
+}
+
+struct LnModulateCkpt : public torch::autograd::Function<LnModulateCkpt> {
+    static Tensor forward(AutogradContext* ctx, const Tensor& x, const Tensor& shift, const Tensor& scale,
+                          const std::optional<Tensor>& cu_seqlens, double eps, int64_t code, int64_t group) {
+        const Tensor cu = cu_seqlens.value_or(Tensor());
+        const variable_list r = ckpt_forward(x, shift, scale, cu, eps, static_cast<int>(code), group);
+        ctx->saved_data["group"] = group;
+        ctx->save_for_backward({r[1], r[2], scale, cu, r[3], r[4]});
+        return r[0];
+    }
+
+    static variable_list backward(AutogradContext* ctx, variable_list grads) {
+        const variable_list s = ctx->get_saved_variables();
+        const Tensor &codes = s[0], &scales = s[1], &scale = s[2], &cu = s[3], &mean = s[4], &rstd = s[5];
+        const int64_t group = ctx->saved_data["group"].toInt();
+        const Tensor dy = grads[0].contiguous();
+        Batch b;
+        bool token = false;
+        if (plain_state() && ln_shapes(dy, scale, cu, &b, &token) && plain_codes(codes, dy.sizes(), dy.device()) &&
+            plain(scales, scales_shape(dy.sizes(), group), at::kFloat, dy.device()) &&
+            plain(mean, dy.sizes().slice(0, dy.dim() - 1), at::kFloat, dy.device()) &&
+            plain(rstd, mean.sizes(), at::kFloat, dy.device())) {
+            Tensor dx = at::empty_like(dy), dshift = at::empty_like(scale), dscale = at::empty_like(scale), ws;
+            if (!token) ws = scratch(lnmod_backward_ckpt_workspace_bytes(b.n, b.T, b.D), dy);
+            const int st = lnmod_backward_ckpt(ptr(dy), ptr(codes), f32(scales), ptr(scale), cu_ptr(cu), b.n, b.s_or_t, b.D,
+                                               group, stream_of(dy), f32(mean), f32(rstd), out(dx), out(dshift), out(dscale),
+                                               token ? nullptr : out(ws), token ? 0 : static_cast<size_t>(ws.numel()),
+                                               code_of(dy), token ? LNMOD_PER_TOKEN : LNMOD_PER_SAMPLE,
+                                               code_of_codes(codes), 1);
+            if (st == LNMOD_OK) return {dx, dshift, dscale, Tensor(), Tensor(), Tensor(), Tensor()};
+        }
+        variable_list r = python_backward("_ckpt_backward", 3, dy, codes, scales, scale, mean, rstd, cu, group);
+        r.resize(7);
+        return r;
+    }
+};
+
+bool rms_shapes(const Tensor& x, const Tensor& w, const Tensor& other, int64_t* N, int64_t* D) {
+    if (!plain_first(x) || x.dim() < 1) return false;
+    *D = x.size(-1);
+    *N = rows_of(x);
+    return plain(w, at::IntArrayRef(D, 1), x.scalar_type(), x.device()) &&
+           (!other.defined() || plain(other, x.sizes(), x.scalar_type(), x.device()));
+}
+
+// codes and scales, or y; then h (x itself without a residual) and rstd; throws NotPlain
+variable_list rms_forward(const Tensor& x, const Tensor& w, const Tensor& residual, double eps, int code, int64_t group,
+                          bool values) {
+    int64_t N, D;
+    if (!(group == 0 || is_group(group)) || !rms_shapes(x, w, residual, &N, &D)) throw NotPlain();
+    Tensor codes, scales, y, h;
+    if (values) {
+        y = at::empty_like(x);
+    } else {
+        codes = at::empty(x.sizes(), x.options().dtype(type_of_code(code)));
+        scales = at::empty(scales_shape(x.sizes(), group), f32_like(x));
+    }
+    if (residual.defined()) h = at::empty_like(x);
+    Tensor rstd = at::empty({N}, f32_like(x));
+    const int st = lnmod_rmsnorm_quant_forward(ptr(x), ptr(residual), ptr(w), N, D, static_cast<float>(eps), group,
+                                               stream_of(x), h.defined() ? out(h) : nullptr, values ? nullptr : out(codes),
+                                               values ? nullptr : f32_out(scales), values ? out(y) : nullptr, f32_out(rstd),
+                                               code_of(x), code);
+    if (st != LNMOD_OK) throw NotPlain();
+    if (!h.defined()) h = x;
+    return values ? variable_list{y, h, rstd} : variable_list{codes, scales, h, rstd};
+}
+
+// dx, dw; empty where the call is not the plain case
+variable_list rms_backward(const Tensor& dy, const Tensor& h, const Tensor& w, const Tensor& rstd, const Tensor& dh, bool io_grads) {
+    int64_t N, D;
+    if (!rms_shapes(h, w, dh, &N, &D) || !plain(dy, h.sizes(), h.scalar_type(), h.device()) ||
+        !plain(rstd, at::IntArrayRef(&N, 1), at::kFloat, h.device()))
+        return {};
+    Tensor dx = at::empty_like(h), dw = at::empty({D}, io_grads ? h.options() : f32_like(h));
+    const Tensor ws = scratch(lnmod_rmsnorm_quant_backward_workspace_bytes(N, D), h);
+    const int st = lnmod_rmsnorm_quant_backward(ptr(dy), ptr(dh), ptr(h), ptr(w), N, D, stream_of(h), f32(rstd), out(dx), out(dw),
+                                                out(ws), static_cast<size_t>(ws.numel()), code_of(h), io_grads);
+    return st == LNMOD_OK ? variable_list{dx, dw} : variable_list{};
+}
+
+struct RmsNormQuant : public torch::autograd::Function<RmsNormQuant> {
+    static variable_list forward(AutogradContext* ctx, const Tensor& x, const Tensor& w, const std::optional<Tensor>& residual,
+                                 double eps, int64_t code, int64_t group) {
+        const Tensor r = residual.value_or(Tensor());
+        const variable_list o = rms_forward(x, w, r, eps, static_cast<int>(code), group, true);
+        ctx->saved_data["residual"] = r.defined();
+        ctx->save_for_backward({o[1], w, o[2]});
+        return r.defined() ? variable_list{o[1], o[0]} : variable_list{o[0]};
+    }
+
+    static variable_list backward(AutogradContext* ctx, variable_list grads) {
+        const variable_list s = ctx->get_saved_variables();
+        const Tensor &h = s[0], &w = s[1], &rstd = s[2];
+        const bool residual = ctx->saved_data["residual"].toBool();
+        const Tensor dy = grads.back().contiguous(), dh = residual ? grads[0].contiguous() : Tensor();
+        variable_list r;
+        if (plain_state()) r = rms_backward(dy, h, w, rstd, dh, true);
+        if (r.empty()) r = python_backward("_rms_quant_backward", 2, dy, h, w, rstd, dh);
+        return {r[0], r[1], residual ? r[0] : Tensor(), Tensor(), Tensor(), Tensor()};
+    }
+};
+
 // ---- Python entry points: None where the call is left to the Python path ------------------------------------
 template <typename F>
 py::object attempt(const std::vector<py::object>& tensors, const py::object& cu, F&& call) {
@@ -346,6 +512,82 @@ py::object qk_norm(const py::object& q, const py::object& k, const py::object& w
     });
 }
 
+// the number of "int8" or "e4m3", or -1; the group, or -1
+int code_number(const py::object& code) {
+    if (!py::isinstance<py::str>(code)) return -1;
+    const std::string name = code.cast<std::string>();
+    return name == "int8" ? LNMOD_INT8 : name == "e4m3" ? LNMOD_E4M3 : -1;
+}
+int64_t group_number(const py::object& group) {
+    if (!PyLong_CheckExact(group.ptr())) return -1;
+    const long v = PyLong_AsLong(group.ptr());
+    if (v == -1 && PyErr_Occurred()) PyErr_Clear();
+    return v == 0 || is_group(v) ? v : -1;
+}
+
+// whether a tensor of a call that is differentiated elsewhere asks for a gradient is no matter here: these calls have none
+py::object quantize(const py::object& x, const py::object& code, const py::object& group) {
+    const int c = code_number(code);
+    const int64_t g = group_number(group);
+    if (c < 0 || g < 0) return py::none();
+    return attempt({x}, py::none(), [&] { return quantize_call(unpack(x), c, g); });
+}
+
+py::object dequantize(const py::object& codes, const py::object& scales, const py::object& dtype, const py::object& group) {
+    const int64_t g = group_number(group);
+    if (g < 0 || !THPDtype_Check(dtype.ptr())) return py::none();
+    const at::ScalarType type = reinterpret_cast<THPDtype*>(dtype.ptr())->scalar_type;
+    return attempt({codes, scales}, py::none(), [&] { return dequantize_call(unpack(codes), unpack(scales), type, g); });
+}
+
+py::object forward_ckpt(const py::object& x, const py::object& shift, const py::object& scale, const py::object& cu, double eps,
+                        const py::object& code, const py::object& group) {
+    const int c = code_number(code);
+    const int64_t g = group_number(group);
+    if (c < 0 || g < 0) return py::none();
+    return attempt({x, shift, scale}, cu, [&] {
+        return ckpt_forward(unpack(x), unpack(shift), unpack(scale), unpack_or(cu).value_or(Tensor()), eps, c, g);
+    });
+}
+
+py::object ln_modulate_ckpt(const py::object& x, const py::object& shift, const py::object& scale, const py::object& cu,
+                            double eps, const py::object& code, const py::object& group) {
+    const int64_t c = code_number(code), g = group_number(group);
+    if (c < 0 || g < 0) return py::none();
+    return attempt({x, shift, scale}, cu, [&] {
+        return variable_list{LnModulateCkpt::apply(unpack(x), unpack(shift), unpack(scale), unpack_or(cu), eps, c, g)};
+    });
+}
+
+// attempt() checks the optional last tensor as it does cu_seqlens
+py::object rmsnorm_quant_forward(const py::object& x, const py::object& w, const py::object& residual, double eps,
+                                 const py::object& code, const py::object& group) {
+    const int c = code_number(code);
+    const int64_t g = group_number(group);
+    if (c < 0 || g < 0) return py::none();
+    return attempt({x, w}, residual, [&] {
+        return rms_forward(unpack(x), unpack(w), unpack_or(residual).value_or(Tensor()), eps, c, g, false);
+    });
+}
+
+py::object rmsnorm_quant_backward(const py::object& dy, const py::object& h, const py::object& w, const py::object& rstd,
+                                  const py::object& dh) {
+    return attempt({dy, h, w, rstd}, dh, [&] {
+        variable_list r = rms_backward(unpack(dy), unpack(h), unpack(w), unpack(rstd), unpack_or(dh).value_or(Tensor()), false);
+        if (r.empty()) throw NotPlain();
+        return r;
+    });
+}
+
+py::object rms_norm_quant(const py::object& x, const py::object& w, const py::object& residual, double eps,
+                          const py::object& code, const py::object& group) {
+    const int64_t c = code_number(code), g = group_number(group);
+    if (c < 0 || g < 0) return py::none();
+    return attempt({x, w}, residual, [&] {
+        return RmsNormQuant::apply(unpack(x), unpack(w), unpack_or(residual), eps, c, g);
+    });
+}
+
 // ---- what y.grad_fn shows --------------------------------------------------------------------------------------
 // The node's Python type, with the saved tensors that the Python classes' nodes show (the same ones in the same order,
 // None where nothing was saved; an error once the backward has freed them).
@@ -379,8 +621,17 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
     register_node<LnModulate>("LnModulateBackward");
     register_node<GatedLnModulate>("GatedLnModulateBackward");
     register_node<QkNorm>("QkNormBackward");
+    register_node<LnModulateCkpt>("LnModulateCkptBackward");
+    register_node<RmsNormQuant>("RmsNormQuantBackward");
     m.def("forward", &forward);
     m.def("ln_modulate", &ln_modulate);
     m.def("gated_ln_modulate", &gated_ln_modulate);
     m.def("qk_norm", &qk_norm);
+    m.def("quantize", &quantize);
+    m.def("dequantize", &dequantize);
+    m.def("forward_ckpt", &forward_ckpt);
+    m.def("ln_modulate_ckpt", &ln_modulate_ckpt);
+    m.def("rmsnorm_quant_forward", &rmsnorm_quant_forward);
+    m.def("rmsnorm_quant_backward", &rmsnorm_quant_backward);
+    m.def("rms_norm_quant", &rms_norm_quant);
 }

@@ -1,4 +1,4 @@
-"""torch.autograd wrappers over the C ABI: the three fused operators as differentiable functions.
+"""torch.autograd wrappers over the C ABI: the fused operators as differentiable functions.
 
 Everything numerical runs in the HIP kernels; the functions allocate outputs with torch and
 keep what the backward needs; the kernels round the float32 sums of the parameter gradients to the
@@ -14,6 +14,9 @@ the errors), tensor subclasses, functorch transforms, dispatch modes, tracers.
     y        = ln_modulate(x, shift, scale, cu_seqlens=cu)       x [T,D] packed; shift, scale [nseg,D]
     h, y     = gated_ln_modulate(x, u, gate, shift, scale)       h = x + gate*u, y = LN(h)(1+scale)+shift
     qn, kn   = qk_norm(q, k, wq, wk)                             RMS norm with weight of q and of k
+    y        = ln_modulate_ckpt(x, shift, scale)                 ln_modulate that keeps x in 8 bits for the backward
+    y        = rms_norm_quant(x, w)                              RMS norm with weight, rounded to 8 bits and back
+    h, y     = rms_norm_quant(x, w, residual)                    h = x + residual first
 """
 import torch
 
@@ -118,3 +121,67 @@ def qk_norm(q, k, wq, wk, eps=1e-6):
     host = lnmod.native()
     r = None if host is None else host.qk_norm(q, k, wq, wk, float(eps))
     return _QkNorm.apply(q, k, wq, wk, float(eps)) if r is None else r
+
+
+def _ckpt_backward(dy, codes, scales, scale, mean, rstd, cu_seqlens, group):
+    return lnmod._backward_ckpt(dy, codes, scales, scale, mean, rstd, cu_seqlens, int(group), io_grads=True)
+
+
+class _LnModulateCkpt(torch.autograd.Function):
+    """ln_modulate whose backward reads the 8-bit checkpoint that the forward wrote beside y."""
+
+    @staticmethod
+    def forward(ctx, x, shift, scale, cu_seqlens, eps, code, group):
+        _contig(x, shift, scale, cu_seqlens)
+        y, codes, scales, mean, rstd = lnmod.forward_ckpt(x, shift, scale, cu_seqlens, eps, code, group)
+        ctx.group = group
+        ctx.save_for_backward(codes, scales, scale, cu_seqlens, mean, rstd)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        codes, scales, scale, cu, mean, rstd = ctx.saved_tensors
+        return _ckpt_backward(dy.contiguous(), codes, scales, scale, mean, rstd, cu, ctx.group) + (None,) * 4
+
+
+def ln_modulate_ckpt(x, shift, scale, eps=1e-6, cu_seqlens=None, code="int8", group=128):
+    """ln_modulate that keeps x in 8 bits between the passes ("int8" or "e4m3", one scale for each `group` = 32, 64 or 128
+    features of a row): D + 4 ceil(D / group) + 8 bytes per token where ln_modulate keeps 2 D + 8 (bf16).  y and dshift
+    are ln_modulate's; dx and dscale are formed with the values that the codes stand for, at most half a code's step from
+    x (int8: 1/254 of the group's largest value)."""
+    host = lnmod.native()
+    y = None if host is None else host.ln_modulate_ckpt(x, shift, scale, cu_seqlens, float(eps), code, group)
+    return _LnModulateCkpt.apply(x, shift, scale, cu_seqlens, float(eps), code, group) if y is None else y
+
+
+def _rms_quant_backward(dy, h, w, rstd, dh):
+    return lnmod._rmsnorm_quant_backward(dy, h, w, rstd, dh, io_grads=True)
+
+
+class _RmsNormQuant(torch.autograd.Function):
+    """RMS norm of x (+ residual), rounded to 8 bits and back; the gradient passes straight through the rounding."""
+
+    @staticmethod
+    def forward(ctx, x, w, residual, eps, code, group):
+        _contig(x, w, residual)
+        _, _, y, h, rstd = lnmod._rmsnorm_quant(x, w, residual, eps, code, group)
+        ctx.save_for_backward(h, w, rstd)
+        ctx.residual = residual is not None
+        return (h, y) if ctx.residual else y
+
+    @staticmethod
+    def backward(ctx, *grads):
+        h, w, rstd = ctx.saved_tensors
+        dh = grads[0].contiguous() if ctx.residual else None
+        dx, dw = _rms_quant_backward(grads[-1].contiguous(), h, w, rstd, dh)
+        return dx, dw, dx if ctx.residual else None, None, None, None
+
+
+def rms_norm_quant(x, w, residual=None, eps=1e-6, code="e4m3", group=0):
+    """y = h * rsqrt(mean(h^2) + eps) * w rounded to 8 bits (one scale for each `group` = 32, 64 or 128 features, or 0: for
+    a row), as the values that the codes stand for: what a model trains on that is served with lnmod.rmsnorm_quant_forward.
+    h = x; with a residual h = x + residual, and (h, y) is returned.  As with torch's own addition, x and the residual get
+    one and the same gradient tensor from torch.autograd.grad."""
+    host = lnmod.native()
+    r = None if host is None else host.rms_norm_quant(x, w, residual, float(eps), code, group)
+    return _RmsNormQuant.apply(x, w, residual, float(eps), code, group) if r is None else r

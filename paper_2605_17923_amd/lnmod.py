@@ -15,6 +15,7 @@ import os
 LNMOD_OK, LNMOD_EINVAL, LNMOD_EUNSUPPORTED, LNMOD_EALIGN, LNMOD_EWORKSPACE, LNMOD_ELAUNCH = range(6)
 LNMOD_BF16, LNMOD_F32 = 0, 1
 LNMOD_PER_SAMPLE, LNMOD_PER_TOKEN = 0, 1
+LNMOD_INT8, LNMOD_E4M3 = 0, 1
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIBRARY = os.path.join(_HERE, "liblnmod.so")
@@ -26,7 +27,10 @@ EXPORTS = ("lnmod_forward", "lnmod_backward", "lnmod_forward_varlen", "lnmod_bac
            "lnmod_backward_static", "lnmod_backward_workspace_bytes", "lnmod_status_string", "lnmod_gated_forward",
            "lnmod_gated_backward", "lnmod_gated_backward_workspace_bytes", "lnmod_qknorm_forward",
            "lnmod_qknorm_backward", "lnmod_qknorm_backward_workspace_bytes", "lnmod_backward_io",
-           "lnmod_gated_backward_io", "lnmod_qknorm_backward_io", "lnmod_backward_token")
+           "lnmod_gated_backward_io", "lnmod_qknorm_backward_io", "lnmod_backward_token", "lnmod_quantize",
+           "lnmod_dequantize", "lnmod_forward_ckpt", "lnmod_backward_ckpt", "lnmod_backward_ckpt_workspace_bytes",
+           "lnmod_rmsnorm_quant_forward", "lnmod_rmsnorm_quant_backward",
+           "lnmod_rmsnorm_quant_backward_workspace_bytes")
 
 _lib = None
 _native = None
@@ -89,6 +93,24 @@ def library() -> ctypes.CDLL:
     lib.lnmod_qknorm_backward_io.argtypes = lib.lnmod_qknorm_backward.argtypes
     lib.lnmod_qknorm_backward_workspace_bytes.restype = sz
     lib.lnmod_qknorm_backward_workspace_bytes.argtypes = [i64, i64]
+    lib.lnmod_quantize.restype = cint
+    lib.lnmod_quantize.argtypes = [vp, i64, i64, i64, vp, vp, vp, cint, cint]
+    lib.lnmod_dequantize.restype = cint
+    lib.lnmod_dequantize.argtypes = [vp, vp, i64, i64, i64, vp, vp, cint, cint]
+    lib.lnmod_forward_ckpt.restype = cint
+    lib.lnmod_forward_ckpt.argtypes = [vp, vp, vp, vp, i64, i64, i64, f32, i64, vp, vp, vp, vp, vp, vp,
+                                       cint, cint, cint]
+    lib.lnmod_backward_ckpt.restype = cint
+    lib.lnmod_backward_ckpt.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, sz,
+                                        cint, cint, cint, cint]
+    lib.lnmod_backward_ckpt_workspace_bytes.restype = sz
+    lib.lnmod_backward_ckpt_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.lnmod_rmsnorm_quant_forward.restype = cint
+    lib.lnmod_rmsnorm_quant_forward.argtypes = [vp, vp, vp, i64, i64, f32, i64, vp, vp, vp, vp, vp, vp, cint, cint]
+    lib.lnmod_rmsnorm_quant_backward.restype = cint
+    lib.lnmod_rmsnorm_quant_backward.argtypes = [vp, vp, vp, vp, i64, i64, vp, vp, vp, vp, vp, sz, cint, cint]
+    lib.lnmod_rmsnorm_quant_backward_workspace_bytes.restype = sz
+    lib.lnmod_rmsnorm_quant_backward_workspace_bytes.argtypes = [i64, i64]
     _lib = lib
     return lib
 
@@ -248,6 +270,45 @@ def lnmod_qknorm_backward_workspace_bytes(N, D):
     return int(library().lnmod_qknorm_backward_workspace_bytes(N, D))
 
 
+def lnmod_quantize(x, N, D, group, stream, codes, code_scales, dtype, code):
+    return library().lnmod_quantize(_p(x), N, D, group, stream, _p(codes), _p(code_scales), dtype, code)
+
+
+def lnmod_dequantize(codes, code_scales, N, D, group, stream, x, dtype, code):
+    return library().lnmod_dequantize(_p(codes), _p(code_scales), N, D, group, stream, _p(x), dtype, code)
+
+
+def lnmod_forward_ckpt(x, shift, scale, cu_seqlens, B_or_nseg, S_or_T, D, eps, group, stream, y, codes, code_scales,
+                       mean, rstd, dtype, mod, code):
+    return library().lnmod_forward_ckpt(_p(x), _p(shift), _p(scale), _p(cu_seqlens), B_or_nseg, S_or_T, D, eps,
+                                        group, stream, _p(y), _p(codes), _p(code_scales), _p(mean), _p(rstd),
+                                        dtype, mod, code)
+
+
+def lnmod_backward_ckpt(dy, codes, code_scales, scale, cu_seqlens, B_or_nseg, S_or_T, D, group, stream, mean, rstd,
+                        dx, dshift, dscale, workspace, workspace_bytes, dtype, mod, code, io_grads):
+    return library().lnmod_backward_ckpt(_p(dy), _p(codes), _p(code_scales), _p(scale), _p(cu_seqlens), B_or_nseg,
+                                         S_or_T, D, group, stream, _p(mean), _p(rstd), _p(dx), _p(dshift),
+                                         _p(dscale), _p(workspace), workspace_bytes, dtype, mod, code, io_grads)
+
+
+def lnmod_backward_ckpt_workspace_bytes(B_or_nseg, total_tokens, D):
+    return int(library().lnmod_backward_ckpt_workspace_bytes(B_or_nseg, total_tokens, D))
+
+
+def lnmod_rmsnorm_quant_forward(x, r, w, N, D, eps, group, stream, h, codes, code_scales, y, rstd, dtype, code):
+    return library().lnmod_rmsnorm_quant_forward(_p(x), _p(r), _p(w), N, D, eps, group, stream, _p(h), _p(codes),
+                                                 _p(code_scales), _p(y), _p(rstd), dtype, code)
+
+
+def lnmod_rmsnorm_quant_backward(dy, dh, h, w, N, D, stream, rstd, dx, dw, workspace, workspace_bytes, dtype,
+                                 io_grads):
+    return library().lnmod_rmsnorm_quant_backward(_p(dy), _p(dh), _p(h), _p(w), N, D, stream, _p(rstd), _p(dx),
+                                                  _p(dw), _p(workspace), workspace_bytes, dtype, io_grads)
+
+
+def lnmod_rmsnorm_quant_backward_workspace_bytes(N, D):
+    return int(library().lnmod_rmsnorm_quant_backward_workspace_bytes(N, D))
 
 
 # ---- conveniences: check the tensors, allocate outputs with torch, raise on a non-zero status ---
@@ -647,3 +708,278 @@ def _qknorm_backward(dq_out, dk_out, q, k, wq, wk, rstd_q, rstd_k, eps, stream=N
         _check(call(dq_out, dk_out, q, k, wq, wk, N, D, eps, handle, rstd_q, rstd_k, dq, dk, dwq, dwk, ws,
                     ws.numel(), code), call.__name__)
     return dq, dk, dwq, dwk
+
+
+# ---- activations in 8 bits ------------------------------------------------------------------------
+GROUPS = (32, 64, 128)
+
+
+class _on_device:
+    """_on_stream with the tensor's own device as the current one: its current stream, its memory pool.  A stream of
+    another device is refused."""
+
+    def __init__(self, t, stream):
+        import torch
+        if isinstance(stream, torch.cuda.Stream) and stream.device != t.device:
+            raise ValueError("stream is on %s, the tensors are on %s" % (stream.device, t.device))
+        self._device = torch.cuda.device(t.device)
+        self._stream = stream
+
+    def __enter__(self):
+        self._device.__enter__()
+        try:
+            self._ctx = _on_stream(self._stream)
+            return self._ctx.__enter__()
+        except BaseException:
+            self._device.__exit__(None, None, None)
+            raise
+
+    def __exit__(self, *exc):
+        try:
+            self._ctx.__exit__(*exc)
+        finally:
+            self._device.__exit__(*exc)
+        return False
+
+
+def _code_of(code):
+    """"int8" or "e4m3" -> (its number, the codes' torch dtype)."""
+    import torch
+    if code == "int8":
+        return LNMOD_INT8, torch.int8
+    if code == "e4m3":
+        return LNMOD_E4M3, torch.float8_e4m3fn
+    raise ValueError("code must be 'int8' or 'e4m3', got %r" % (code,))
+
+
+def _code_number(codes):
+    import torch
+    if isinstance(codes, torch.Tensor):
+        if codes.dtype == torch.int8:
+            return LNMOD_INT8
+        if codes.dtype == torch.float8_e4m3fn:
+            return LNMOD_E4M3
+        raise ValueError("codes must be int8 or float8_e4m3fn, got %s" % (codes.dtype,))
+    raise ValueError("codes must be a tensor")
+
+
+def _group_of(group, row=False):
+    if isinstance(group, bool) or not isinstance(group, int) or not (group in GROUPS or (row and group == 0)):
+        raise ValueError("group must be %s, got %r" % ("0 (the row), 32, 64 or 128" if row else "32, 64 or 128", group))
+    return group
+
+
+def _rows(t, name):
+    if t.dim() < 1:
+        raise ValueError("%s must be [..., D]" % name)
+    D = t.shape[-1]
+    return t.numel() // max(D, 1), D
+
+
+def _scales_shape(shape, group):
+    """One scale per group of the last dimension; group 0: one per row."""
+    return tuple(shape[:-1]) + ((-(-shape[-1] // group),) if group else ())
+
+
+def _host(t, stream, eps=0.0):
+    """The host path in C++ where a call may be the plain case, or None."""
+    if stream is not None or type(eps) is not float or not getattr(t, "is_cuda", False):
+        return None
+    return native()
+
+
+def quantize(x, code="int8", group=128, stream=None):
+    """The 8-bit checkpoint of x [..., D] (D a multiple of 8): one scale for each `group` (32, 64, 128) features of a
+    row -> codes (int8, or float8_e4m3fn for "e4m3", shaped like x) and scales (float32 [..., ceil(D / group)]); what
+    the codes stand for is codes * scale."""
+    import torch
+    host = _host(x, stream)
+    r = None if host is None else host.quantize(x, code, group)
+    if r is not None:
+        return r
+    number, kind = _code_of(code)
+    _group_of(group)
+    a = _Args(x)
+    dt = _dtype_code(x)
+    N, D = _rows(x, "x")
+    a.expect("x", x, x.shape)
+    a.on_gpu()
+    with _on_device(x, stream) as handle:
+        codes = torch.empty(x.shape, dtype=kind, device=x.device)
+        scales = torch.empty(_scales_shape(x.shape, group), dtype=torch.float32, device=x.device)
+        _check(lnmod_quantize(x, N, D, group, handle, codes, scales, dt, number), "lnmod_quantize")
+    return codes, scales
+
+
+def dequantize(codes, scales, dtype, group=128, stream=None):
+    """What the codes of quantize() stand for, in `dtype` (bfloat16 or float32).  Of codes with one scale for a row
+    (rmsnorm_quant_forward with group 0): group=0."""
+    import torch
+    host = _host(codes, stream)
+    r = None if host is None else host.dequantize(codes, scales, dtype, group)
+    if r is not None:
+        return r
+    number = _code_number(codes)
+    _group_of(group, row=True)
+    N, D = _rows(codes, "codes")
+    a = _Args(codes)
+    a.expect("codes", codes, codes.shape)
+    a.expect("scales", scales, _scales_shape(codes.shape, group), torch.float32)
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("dtype must be torch.bfloat16 or torch.float32, got %r" % (dtype,))
+    dt = LNMOD_BF16 if dtype == torch.bfloat16 else LNMOD_F32
+    a.on_gpu()
+    with _on_device(codes, stream) as handle:
+        x = torch.empty(codes.shape, dtype=dtype, device=codes.device)
+        _check(lnmod_dequantize(codes, scales, N, D, group, handle, x, dt, number), "lnmod_dequantize")
+    return x
+
+
+def _ckpt_batch(a, x, scale, cu_seqlens):
+    """-> (samples or segments, S or T, total tokens, D, mod, shape of the modulation rows)."""
+    if cu_seqlens is None:
+        mod, mshape = _mod_rows(x, scale, "scale")
+        B, S, D = x.shape
+        return B, S, B * S, D, mod, mshape
+    T, D = _packed(x)
+    nseg = a.expect_cu(cu_seqlens)
+    return nseg, T, T, D, LNMOD_PER_SAMPLE, (nseg, D)
+
+
+def forward_ckpt(x, shift, scale, cu_seqlens=None, eps=1e-6, code="int8", group=128, stream=None):
+    """forward() / forward_varlen() that writes the 8-bit checkpoint of x in the same pass.  x [B,S,D] with shift, scale
+    [B,D] or [B,S,D], or packed [T,D] with cu_seqlens and [nseg,D] -> y, codes, scales, mean, rstd (codes and scales
+    as quantize(x, code, group) gives them; mean and rstd [B,S] or [T])."""
+    import torch
+    host = _host(x, stream, eps)
+    r = None if host is None else host.forward_ckpt(x, shift, scale, cu_seqlens, eps, code, group)
+    if r is not None:
+        return r
+    number, kind = _code_of(code)
+    _group_of(group)
+    a = _Args(x)
+    dt = _dtype_code(x)
+    n, s_or_t, T, D, mod, mshape = _ckpt_batch(a, x, scale, cu_seqlens)
+    a.expect("x", x, x.shape)
+    a.expect("shift", shift, mshape)
+    a.expect("scale", scale, mshape)
+    a.on_gpu()
+    with _on_device(x, stream) as handle:
+        y = torch.empty_like(x)
+        codes = torch.empty(x.shape, dtype=kind, device=x.device)
+        scales = torch.empty(_scales_shape(x.shape, group), dtype=torch.float32, device=x.device)
+        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+        rstd = torch.empty_like(mean)
+        _check(lnmod_forward_ckpt(x, shift, scale, cu_seqlens, n, s_or_t, D, eps, group, handle, y, codes, scales, mean,
+                                  rstd, dt, mod, number), "lnmod_forward_ckpt")
+    return y, codes, scales, mean, rstd
+
+
+def backward_ckpt(dy, codes, scales, scale, mean, rstd, cu_seqlens=None, group=128, stream=None, ws=None):
+    """backward() / backward_varlen() from the checkpoint: what forward_ckpt() returned, in x's place -> dx, dshift,
+    dscale (float32 [B,D] / [nseg,D]; I/O dtype [B,S,D] per token)."""
+    return _backward_ckpt(dy, codes, scales, scale, mean, rstd, cu_seqlens, group, stream, ws)
+
+
+def _backward_ckpt(dy, codes, scales, scale, mean, rstd, cu_seqlens, group, stream=None, ws=None, io_grads=False):
+    """backward_ckpt(); with io_grads dshift and dscale come in the I/O dtype in either mode."""
+    import torch
+    number = _code_number(codes)
+    _group_of(group)
+    a = _Args(dy)
+    dt = _dtype_code(dy)
+    n, s_or_t, T, D, mod, mshape = _ckpt_batch(a, dy, scale, cu_seqlens)
+    a.expect("dy", dy, dy.shape)
+    a.expect("codes", codes, dy.shape, codes.dtype)
+    a.expect("scales", scales, _scales_shape(dy.shape, group), torch.float32)
+    a.expect("scale", scale, mshape)
+    a.expect("mean", mean, dy.shape[:-1], torch.float32)
+    a.expect("rstd", rstd, dy.shape[:-1], torch.float32)
+    need = lnmod_backward_ckpt_workspace_bytes(n, T, D) if mod == LNMOD_PER_SAMPLE else 0
+    if mod == LNMOD_PER_SAMPLE:
+        a.expect_workspace(ws, need)
+    a.on_gpu()
+    with _on_device(dy, stream) as handle:
+        dx = torch.empty_like(dy)
+        if mod == LNMOD_PER_TOKEN:
+            dshift, dscale, ws = torch.empty_like(dy), torch.empty_like(dy), None
+        else:
+            grad = dy.dtype if io_grads else torch.float32
+            dshift, dscale = (torch.empty(mshape, dtype=grad, device=dy.device) for _ in range(2))
+            if ws is None:
+                ws = torch.empty(max(need, 16), dtype=torch.uint8, device=dy.device)
+        _check(lnmod_backward_ckpt(dy, codes, scales, scale, cu_seqlens, n, s_or_t, D, group, handle, mean, rstd, dx,
+                                   dshift, dscale, ws, 0 if ws is None else ws.numel(), dt, mod, number,
+                                   int(io_grads)), "lnmod_backward_ckpt")
+    return dx, dshift, dscale
+
+
+def _rms_args(x, w, **like_x):
+    a = _Args(x)
+    dt = _dtype_code(x)
+    N, D = _rows(x, "x")
+    a.expect("x", x, x.shape)
+    a.expect("w", w, (D,))
+    for name, t in like_x.items():
+        if t is not None:
+            a.expect(name, t, x.shape)
+    return a, dt, N, D
+
+
+def rmsnorm_quant_forward(x, w, residual=None, eps=1e-6, code="e4m3", group=0, stream=None):
+    """h = x + residual (x itself without one), then the codes of h * rsqrt(mean(h^2) + eps) * w, [..., D], with one scale
+    for each `group` features (32, 64, 128) or for a row (0) -> codes, scales, h, rstd (float32, one per row)."""
+    host = _host(x, stream, eps)
+    r = None if host is None else host.rmsnorm_quant_forward(x, w, residual, eps, code, group)
+    if r is not None:
+        return r
+    codes, scales, _, h, rstd = _rmsnorm_quant(x, w, residual, eps, code, group, stream, values=False)
+    return codes, scales, h, rstd
+
+
+def _rmsnorm_quant(x, w, residual, eps, code, group, stream=None, values=True):
+    """-> codes, scales, y, h, rstd: codes and scales, or with `values` y (what they stand for, in the I/O dtype)."""
+    import torch
+    number, kind = _code_of(code)
+    _group_of(group, row=True)
+    a, dt, N, D = _rms_args(x, w, residual=residual)
+    a.on_gpu()
+    with _on_device(x, stream) as handle:
+        codes = scales = y = None
+        if values:
+            y = torch.empty_like(x)
+        else:
+            codes = torch.empty(x.shape, dtype=kind, device=x.device)
+            scales = torch.empty(_scales_shape(x.shape, group), dtype=torch.float32, device=x.device)
+        h = None if residual is None else torch.empty_like(x)
+        rstd = torch.empty(N, dtype=torch.float32, device=x.device)
+        _check(lnmod_rmsnorm_quant_forward(x, residual, w, N, D, eps, group, handle, h, codes, scales, y, rstd, dt,
+                                           number), "lnmod_rmsnorm_quant_forward")
+    return codes, scales, y, x if h is None else h, rstd
+
+
+def rmsnorm_quant_backward(dy, h, w, rstd, dh=None, stream=None, ws=None):
+    """Straight through the rounding: dy is the gradient of the normed rows, dh (or None) the one that reaches h along the
+    residual stream -> dx (of x and of the residual, I/O dtype) and dw (float32 [D])."""
+    host = None if ws is not None else _host(dy, stream)
+    r = None if host is None else host.rmsnorm_quant_backward(dy, h, w, rstd, dh)
+    return _rmsnorm_quant_backward(dy, h, w, rstd, dh, stream, ws) if r is None else r
+
+
+def _rmsnorm_quant_backward(dy, h, w, rstd, dh, stream=None, ws=None, io_grads=False):
+    """rmsnorm_quant_backward(); with io_grads dw comes in the I/O dtype."""
+    import torch
+    a, dt, N, D = _rms_args(h, w, dh=dh)
+    a.expect("dy", dy, h.shape)
+    a.expect("rstd", rstd, (N,), torch.float32)
+    need = lnmod_rmsnorm_quant_backward_workspace_bytes(N, D)
+    a.expect_workspace(ws, need)
+    a.on_gpu()
+    with _on_device(h, stream) as handle:
+        dx = torch.empty_like(h)
+        dw = torch.empty(D, dtype=h.dtype if io_grads else torch.float32, device=h.device)
+        if ws is None:
+            ws = torch.empty(max(need, 16), dtype=torch.uint8, device=h.device)
+        _check(lnmod_rmsnorm_quant_backward(dy, dh, h, w, N, D, handle, rstd, dx, dw, ws, ws.numel(), dt,
+                                            int(io_grads)), "lnmod_rmsnorm_quant_backward")
+    return dx, dw
