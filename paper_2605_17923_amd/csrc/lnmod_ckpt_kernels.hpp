@@ -40,10 +40,10 @@ constexpr int waves_for(int regs, int most = LNMOD_MAX_WAVES_PER_EU) {
     return w > most ? most : w < 1 ? 1 : w;
 }
 constexpr int ckpt_fwd_waves(int vpl, int nv, int r, bool tok) {
-    return waves_for(vpl * ((tok ? 0 : 16) + 2 * r * 4 * nv * (tok ? 3 : 1)) + 56);
+    return waves_for(vpl * ((tok ? 0 : 16) + kDepth * r * 4 * nv * (tok ? 3 : 1)) + 56);
 }
 constexpr int ckpt_bwd_waves(int vpl, int nv, int r, bool tok) {
-    return waves_for(vpl * ((tok ? 0 : 24) + 2 * r * (4 * nv * (tok ? 2 : 1) + 3)) + 56);
+    return waves_for(vpl * ((tok ? 0 : 24) + kDepth * r * (4 * nv * (tok ? 2 : 1) + 3)) + 56);
 }
 
 template <typename Tag, typename C, int VPL, int K, int R, bool TOK>
@@ -60,13 +60,15 @@ void ckpt_fwd_kernel(const CkptFwdArgs args) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t row_bytes = static_cast<int64_t>(a.D) * IO<Tag>::kBytes;
 
-    uint32_t chunk[VPL];
+    uint32_t chunk[VPL], scale_off[VPL];                     // scale_off: the group's first lane stores its scale
     bool ok[VPL];
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
         chunk[i] = static_cast<uint32_t>((i * K + wave) * kWave + lane);
         ok[i] = chunk[i] < static_cast<uint32_t>(a.nchunks);
+        scale_off[i] = ok[i] && (lane & ((1 << cd.lanes_log2) - 1)) == 0 ? (chunk[i] >> cd.lanes_log2) * 4u : kNowhere;
     }
+    const uint32_t first_lane = threadIdx.x == 0 ? 0u : kNowhere;
     float cnt[K], my_cnt = 0.0f;                             // features each wave holds
 #pragma unroll
     for (int w = 0; w < K; ++w) {
@@ -88,19 +90,18 @@ void ckpt_fwd_kernel(const CkptFwdArgs args) {
     if (stop > a.T) stop = a.T;
     const int64_t first = r0 + at.member * R, step = static_cast<int64_t>(a.nb) * R;
 
+    const uint32_t unit_bytes = static_cast<uint32_t>(row_bytes);
+
     // the modulation row of segment m lives in registers until a row of another segment comes; seg_end is where m's rows end
     float A[TOK ? 1 : VPL][8], B[TOK ? 1 : VPL][8];
     int64_t m = 0, seg_end = a.T;
     const auto load_modulation = [&] {
+        const Row rsc = row_of(a.scale, m * row_bytes, unit_bytes), rsh = row_of(a.shift, m * row_bytes, unit_bytes);
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
             u32x4 sc[NV], sh[NV];
-            clear(sc);
-            clear(sh);
-            if (ok[i]) {
-                load_unit_cached<Tag>(a.scale, m * row_bytes, chunk[i], sc);
-                load_unit_cached<Tag>(a.shift, m * row_bytes, chunk[i], sh);
-            }
+            load_unit<Tag, 0>(rsc, chunk[i], sc);
+            load_unit<Tag, 0>(rsh, chunk[i], sh);
             U::unpack(sc, A[i]);
             U::unpack(sh, B[i]);
 #pragma unroll
@@ -111,23 +112,23 @@ void ckpt_fwd_kernel(const CkptFwdArgs args) {
 #pragma unroll
         for (int j = 0; j < R; ++j) {
             const int64_t row = base + j;
+            const uint32_t bytes = row < stop ? unit_bytes : 0u;
+            const Row rx = row_of(a.x, row * row_bytes, bytes);
 #pragma unroll
-            for (int i = 0; i < VPL; ++i) {
-                if (row < stop && ok[i]) {
-                    load_unit<Tag>(a.x, row * row_bytes, chunk[i], q[0][j][i]);
-                    if constexpr (TOK) {
-                        load_unit<Tag>(a.scale, row * row_bytes, chunk[i], q[1][j][i]);
-                        load_unit<Tag>(a.shift, row * row_bytes, chunk[i], q[2][j][i]);
-                    }
-                } else {
+            for (int i = 0; i < VPL; ++i) load_unit<Tag>(rx, chunk[i], q[0][j][i]);
+            if constexpr (TOK) {
+                const Row rsc = row_of(a.scale, row * row_bytes, bytes), rsh = row_of(a.shift, row * row_bytes, bytes);
 #pragma unroll
-                    for (int t = 0; t < NS; ++t) clear(q[t][j][i]);
+                for (int i = 0; i < VPL; ++i) {
+                    load_unit<Tag>(rsc, chunk[i], q[NS - 2][j][i]);
+                    load_unit<Tag>(rsh, chunk[i], q[NS - 1][j][i]);
                 }
             }
         }
     };
-    u32x4 raw[NS][R][VPL][NV];
-    fetch(first, raw);
+    u32x4 bufs[kDepth][NS][R][VPL][NV];
+#pragma unroll
+    for (int d = 0; d < kDepth - 1; ++d) fetch(first + d * step, bufs[d]);
     if constexpr (!TOK) {
         m = find_segment(a.seg, first < stop ? first : r0);
         if (a.seg.nseg > 1) seg_end = m + 1 < a.seg.nseg ? seg_begin(a.seg, m + 1) : a.T;
@@ -135,11 +136,7 @@ void ckpt_fwd_kernel(const CkptFwdArgs args) {
     }
 
     int buf = 0;
-    for (int64_t base = first; base < stop; base += step) {
-        u32x4 nxt[NS][R][VPL][NV];
-        fetch(base + step, nxt);
-        __builtin_amdgcn_sched_barrier(0);                   // keep the requests up here
-
+    const auto compute = [&](int64_t base, u32x4 (&raw)[NS][R][VPL][NV]) {
         // this wave's part of each row: mean, then centred sum of squares; the parts are merged by
         // M2 = sum_k M2_k + sum_k n_k (mean_k - mean)^2
         float mu[R], rs[R];
@@ -157,12 +154,11 @@ void ckpt_fwd_kernel(const CkptFwdArgs args) {
             float q2 = 0.0f;
 #pragma unroll
             for (int i = 0; i < VPL; ++i) {
-                if (ok[i]) {
-                    float v[8];
-                    U::unpack(raw[0][j][i], v);
+                float v[8], t = 0.0f;
+                U::unpack(raw[0][j][i], v);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) q2 += (v[e] - mu[j]) * (v[e] - mu[j]);
-                }
+                for (int e = 0; e < 8; ++e) t += (v[e] - mu[j]) * (v[e] - mu[j]);
+                q2 += ok[i] ? t : 0.0f;
             }
             rs[j] = wave_sum(q2);
         }
@@ -180,7 +176,7 @@ void ckpt_fwd_kernel(const CkptFwdArgs args) {
                 float sum = 0.0f;
 #pragma unroll
                 for (int w = 0; w < K; ++w) sum += cnt[w] * part[buf][j][w][0];
-                const float mean = sum / static_cast<float>(a.D);
+                const float mean = sum * a.inv_D;
                 float m2 = 0.0f;
 #pragma unroll
                 for (int w = 0; w < K; ++w) {
@@ -194,7 +190,7 @@ void ckpt_fwd_kernel(const CkptFwdArgs args) {
         }
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-            rs[j] = 1.0f / sqrtf(rs[j] * a.inv_D + a.eps);
+            rs[j] = rsqrtf(rs[j] * a.inv_D + a.eps);
 #pragma unroll
             for (int i = 0; i < VPL; ++i) opaque(raw[0][j][i]);
         }
@@ -209,17 +205,18 @@ void ckpt_fwd_kernel(const CkptFwdArgs args) {
                     if (seg_end <= row) seg_end = row + 1;
                     load_modulation();
                 }
-                if (wave == 0 && lane == 0) {
-                    a.mean[row] = mu[j];
-                    a.rstd[row] = rs[j];
-                }
+                store_float(row_of(a.mean, row * 4, 4), first_lane, mu[j]);
+                store_float(row_of(a.rstd, row * 4, 4), first_lane, rs[j]);
+                const Row ry = row_of(a.y, row * row_bytes, unit_bytes), rc = row_of(cd.codes, row * a.D, static_cast<uint32_t>(a.D));
+                const Row rcs = row_of(cd.scales, row * cd.groups * 4, static_cast<uint32_t>(cd.groups) * 4u);
 #pragma unroll
                 for (int i = 0; i < VPL; ++i) {
-                    // all lanes: those beyond the row hold zeros
+                    // lanes beyond the row hold zeros
                     const Scale sc = scale_of<C>(group_max(U::amax_bits(raw[0][j][i]), cd.lanes_log2));
                     float v[8], o[8];
                     U::unpack(raw[0][j][i], v);
-                    const u32x2 w = encode<C>(v, sc);
+                    store_codes(rc, chunk[i], encode<C>(v, sc));
+                    store_float(rcs, scale_off[i], sc.s);
                     if constexpr (TOK) {
                         float p[8], t[8];
                         U::unpack(raw[NS - 2][j][i], p);
@@ -230,26 +227,23 @@ void ckpt_fwd_kernel(const CkptFwdArgs args) {
 #pragma unroll
                         for (int e = 0; e < 8; ++e) o[e] = ((v[e] - mu[j]) * rs[j]) * A[i][e] + B[i][e];
                     }
-                    if (ok[i]) {
-                        u32x4 y[NV];
-                        U::pack(o, y);
-                        store_unit<Tag>(a.y, row * row_bytes, chunk[i], y);
-                        store_codes(cd.codes, row * a.D, chunk[i], w);
-                        if ((lane & ((1 << cd.lanes_log2) - 1)) == 0)
-                            cd.scales[uniform64(row * cd.groups) + (chunk[i] >> cd.lanes_log2)] = sc.s;
-                    }
+                    u32x4 y[NV];
+                    U::pack(o, y);
+                    store_unit<Tag>(ry, chunk[i], y);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
         }
+    };
+    for (int64_t base = first; base < stop;) {
 #pragma unroll
-        for (int t = 0; t < NS; ++t)
-#pragma unroll
-            for (int j = 0; j < R; ++j)
-#pragma unroll
-                for (int i = 0; i < VPL; ++i)
-#pragma unroll
-                    for (int h = 0; h < NV; ++h) raw[t][j][i][h] = nxt[t][j][i][h];
+        for (int d = 0; d < kDepth; ++d) {
+            if (base >= stop) break;
+            fetch(base + (kDepth - 1) * step, bufs[(d + kDepth - 1) % kDepth]);
+            __builtin_amdgcn_sched_barrier(0);               // keep the requests up here
+            compute(base, bufs[d]);
+            base += step;
+        }
     }
 }
 
@@ -270,12 +264,13 @@ void ckpt_bwd_kernel(const CkptBwdArgs args) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t row_bytes = static_cast<int64_t>(a.D) * IO<Tag>::kBytes;
 
-    uint32_t chunk[VPL];
-    bool ok[VPL];
+    const uint32_t unit_bytes = static_cast<uint32_t>(row_bytes);
+
+    uint32_t chunk[VPL], scale_off[VPL];
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
         chunk[i] = static_cast<uint32_t>((i * K + wave) * kWave + lane);
-        ok[i] = chunk[i] < static_cast<uint32_t>(a.nchunks);
+        scale_off[i] = (chunk[i] >> cd.lanes_log2) * 4u;
     }
     const Place at = place_of(a.split, a.interleave);
     const int64_t cluster = at.cluster, member = at.member;
@@ -304,35 +299,39 @@ void ckpt_bwd_kernel(const CkptBwdArgs args) {
             for (int j = 0; j < R; ++j) {
                 const int64_t row = base + j;
                 const bool live = row < stop;
-                q.mu[j] = live ? a.mean[row] : 0.0f;
-                q.rs[j] = live ? a.rstd[row] : 0.0f;
+                const uint32_t on = live ? ~0u : 0u;
+                const int64_t of = live ? row : stop - 1;    // a row beyond the last: statistics 0, everything else reads as 0
+                q.mu[j] = live ? float_at(a.mean, of) : 0.0f;
+                q.rs[j] = live ? float_at(a.rstd, of) : 0.0f;
+                const Row rdy = row_of(a.dy, row * row_bytes, unit_bytes & on);
+                const Row rc = row_of(cd.codes, row * a.D, static_cast<uint32_t>(a.D) & on);
+                const Row rcs = row_of(cd.scales, row * cd.groups * 4, (static_cast<uint32_t>(cd.groups) * 4u) & on);
 #pragma unroll
                 for (int i = 0; i < VPL; ++i) {
-                    clear(q.dy[j][i]);
-                    if constexpr (TOK) clear(q.sc[j][i]);
-                    q.code[j][i] = u32x2{0u, 0u};
-                    q.s[j][i] = 0.0f;
-                    if (live && ok[i]) {
-                        load_unit<Tag>(a.dy, row * row_bytes, chunk[i], q.dy[j][i]);
-                        if constexpr (TOK) load_unit<Tag>(a.scale, row * row_bytes, chunk[i], q.sc[j][i]);
-                        q.code[j][i] = load_codes(cd.codes, row * a.D, chunk[i]);
-                        q.s[j][i] = cd.scales[uniform64(row * cd.groups) + (chunk[i] >> cd.lanes_log2)];
-                    }
+                    load_unit<Tag>(rdy, chunk[i], q.dy[j][i]);
+                    q.code[j][i] = load_codes(rc, chunk[i]);
+                    q.s[j][i] = load_float(rcs, scale_off[i]);
+                }
+                if constexpr (TOK) {
+                    const Row rsc = row_of(a.scale, row * row_bytes, unit_bytes & on);
+#pragma unroll
+                    for (int i = 0; i < VPL; ++i) load_unit<Tag>(rsc, chunk[i], q.sc[j][i]);
                 }
             }
         };
         const int64_t step = static_cast<int64_t>(a.nb) * R;
         const int64_t first = take_turn<R>(turn, r0, stop, member, a.nb);
-        Rows now;
-        fetch(first, now);
+        Rows bufs[kDepth];
+#pragma unroll
+        for (int d = 0; d < kDepth - 1; ++d) fetch(first + d * step, bufs[d]);
 
         float A[TOK ? 1 : VPL][8], acc_s[TOK ? 1 : VPL][8], acc_c[TOK ? 1 : VPL][8];
         if constexpr (!TOK) {
+            const Row rsc = row_of(a.scale, m * row_bytes, unit_bytes);
 #pragma unroll
             for (int i = 0; i < VPL; ++i) {
                 u32x4 r[NV];
-                clear(r);
-                if (ok[i]) load_unit_cached<Tag>(a.scale, m * row_bytes, chunk[i], r);
+                load_unit<Tag, 0>(rsc, chunk[i], r);
                 U::unpack(r, A[i]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -343,10 +342,7 @@ void ckpt_bwd_kernel(const CkptBwdArgs args) {
             }
         }
 
-        for (int64_t base = first; base < stop; base += step) {
-            Rows nxt;
-            fetch(base + step, nxt);
-            __builtin_amdgcn_sched_barrier(0);               // keep the requests up here
+        const auto compute = [&](int64_t base, Rows& now) {
             float c1[R], c2[R];
 #pragma unroll
             for (int j = 0; j < R; ++j) {
@@ -415,51 +411,56 @@ void ckpt_bwd_kernel(const CkptBwdArgs args) {
                 const int64_t row = base + j;
                 if (row < stop) {
                     const float b = -now.mu[j] * now.rs[j];
+                    // rstd*(g - c1 - xhat*c2) with xhat = code*p + b
                     const float k1 = now.rs[j] * (c1[j] * a.inv_D), k2 = now.rs[j] * (c2[j] * a.inv_D);
+                    const float bk = -(k1 + b * k2);
+                    const Row rdx = row_of(a.dx, row * row_bytes, unit_bytes);
 #pragma unroll
                     for (int i = 0; i < VPL; ++i) {
-                        if (ok[i]) {
-                            float dyv[8], cv[8], scv[8], o[8], ds[8];
-                            U::unpack(now.dy[j][i], dyv);
-                            decode<C>(now.code[j][i], cv);
-                            if constexpr (TOK) U::unpack(now.sc[j][i], scv);
-                            const float p = now.s[j][i] * now.rs[j];
+                        float dyv[8], cv[8], scv[8], o[8], ds[8];
+                        U::unpack(now.dy[j][i], dyv);
+                        decode<C>(now.code[j][i], cv);
+                        if constexpr (TOK) U::unpack(now.sc[j][i], scv);
+                        const float p = now.s[j][i] * now.rs[j], pk = -p * k2;
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                const float h = __builtin_fmaf(cv[e], p, b);
-                                o[e] = (dyv[e] * (TOK ? 1.0f + scv[e] : A[TOK ? 0 : i][e])) * now.rs[j] - k1 - h * k2;
-                                ds[e] = dyv[e] * h;
-                            }
-                            u32x4 t[NV];
-                            U::pack(o, t);
-                            store_unit<Tag>(a.dx, row * row_bytes, chunk[i], t);
-                            if constexpr (TOK) {             // dshift = dy as loaded, dscale = dy*xhat
-                                store_unit<Tag>(a.dshift, row * row_bytes, chunk[i], now.dy[j][i]);
-                                U::pack(ds, t);
-                                store_unit<Tag>(a.dscale, row * row_bytes, chunk[i], t);
-                            }
+                        for (int e = 0; e < 8; ++e) {
+                            const float g = dyv[e] * (TOK ? 1.0f + scv[e] : A[TOK ? 0 : i][e]);
+                            o[e] = __builtin_fmaf(g, now.rs[j], __builtin_fmaf(cv[e], pk, bk));
+                            if constexpr (TOK) ds[e] = dyv[e] * __builtin_fmaf(cv[e], p, b);
+                        }
+                        u32x4 t[NV];
+                        U::pack(o, t);
+                        store_unit<Tag>(rdx, chunk[i], t);
+                        if constexpr (TOK) {                 // dshift = dy as loaded, dscale = dy*xhat
+                            store_unit<Tag>(row_of(a.dshift, row * row_bytes, unit_bytes), chunk[i], now.dy[j][i]);
+                            U::pack(ds, t);
+                            store_unit<Tag>(row_of(a.dscale, row * row_bytes, unit_bytes), chunk[i], t);
                         }
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
             }
-            now = nxt;
+        };
+        for (int64_t base = first; base < stop;) {
+#pragma unroll
+            for (int d = 0; d < kDepth; ++d) {
+                if (base >= stop) break;
+                fetch(base + (kDepth - 1) * step, bufs[(d + kDepth - 1) % kDepth]);
+                __builtin_amdgcn_sched_barrier(0);           // keep the requests up here
+                compute(base, bufs[d]);
+                base += step;
+            }
         }
 
         if constexpr (!TOK) {
             // this block's partial sums for segment m (slots: see bwd_seg_kernel)
-            float* slot = a.ws + ((cluster + m) * a.nb + member) * 2 * a.D;
+            const int64_t slot = ((cluster + m) * a.nb + member) * 2 * a.D * 4;
+            const Row ps = row_of(a.ws, slot, static_cast<uint32_t>(a.D) * 4u);
+            const Row pc = row_of(a.ws, slot + static_cast<int64_t>(a.D) * 4, static_cast<uint32_t>(a.D) * 4u);
 #pragma unroll
             for (int i = 0; i < VPL; ++i) {
-                if (ok[i]) {
-                    f32x4* ps = reinterpret_cast<f32x4*>(slot + chunk[i] * kUnit);
-                    f32x4* pc = reinterpret_cast<f32x4*>(slot + a.D + chunk[i] * kUnit);
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        ps[q] = f32x4{acc_s[i][4 * q], acc_s[i][4 * q + 1], acc_s[i][4 * q + 2], acc_s[i][4 * q + 3]};
-                        pc[q] = f32x4{acc_c[i][4 * q], acc_c[i][4 * q + 1], acc_c[i][4 * q + 2], acc_c[i][4 * q + 3]};
-                    }
-                }
+                store_sums8(ps, chunk[i], acc_s[i]);
+                store_sums8(pc, chunk[i], acc_c[i]);
             }
         }
         r0 = stop;

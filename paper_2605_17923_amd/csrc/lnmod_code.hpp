@@ -18,6 +18,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kUnit = 8;                     // features per lane and chunk, in either element type
+constexpr int kDepth = 2;                    // steps of rows in registers: the one that is computed and the one requested
 
 // ---- eight features of a row in one lane ------------------------------------------------------------------------
 template <typename Tag> struct Unit;
@@ -68,55 +69,75 @@ template <> struct Unit<f32_io> {
     }
 };
 
-template <typename Tag>
-__device__ inline void load_unit(const void* base, int64_t uniform_off, uint32_t chunk, u32x4 (&q)[Unit<Tag>::NV]) {
-#pragma unroll
-    for (int h = 0; h < Unit<Tag>::NV; ++h) q[h] = load16_u(base, uniform_off, chunk * Unit<Tag>::kBytes + 16u * h);
+// A row as a buffer of its own: a read beyond its end gives zeros and a write beyond it does nothing, so lanes without
+// features, and rows beyond the last one (0 bytes), need no branch and no address of their own.  With a comparison and an
+// execution mask around every access the forward's loop was cut into thirty blocks, and a 64-bit address was formed for each.
+typedef __amdgpu_buffer_rsrc_t Row;
+constexpr uint32_t kNowhere = 0x7ffffff0u;   // an offset beyond every row
+constexpr int kStream = 2;                   // cache policy: nontemporal
+
+__device__ inline Row row_of(const void* base, int64_t uniform_off, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base)) + uniform64(uniform_off), 0,
+                                             static_cast<int>(bytes), 0x00027000);
 }
-template <typename Tag>
-__device__ inline void load_unit_cached(const void* base, int64_t uniform_off, uint32_t chunk, u32x4 (&q)[Unit<Tag>::NV]) {
+template <typename Tag, int POLICY = kStream>
+__device__ inline void load_unit(Row row, uint32_t chunk, u32x4 (&q)[Unit<Tag>::NV]) {
 #pragma unroll
     for (int h = 0; h < Unit<Tag>::NV; ++h)
-        q[h] = load16_cached(base, uniform64(uniform_off), chunk * Unit<Tag>::kBytes + 16u * h);
+        q[h] = __builtin_amdgcn_raw_buffer_load_b128(row, static_cast<int>(chunk * Unit<Tag>::kBytes + 16u * h), 0, POLICY);
 }
 template <typename Tag>
-__device__ inline void store_unit(void* base, int64_t uniform_off, uint32_t chunk, const u32x4 (&q)[Unit<Tag>::NV]) {
+__device__ inline void store_unit(Row row, uint32_t chunk, const u32x4 (&q)[Unit<Tag>::NV]) {
 #pragma unroll
-    for (int h = 0; h < Unit<Tag>::NV; ++h) store16_u(base, uniform_off, chunk * Unit<Tag>::kBytes + 16u * h, q[h]);
+    for (int h = 0; h < Unit<Tag>::NV; ++h)
+        __builtin_amdgcn_raw_buffer_store_b128(q[h], row, static_cast<int>(chunk * Unit<Tag>::kBytes + 16u * h), 0, kStream);
 }
-template <int NV>
-__device__ inline void clear(u32x4 (&q)[NV]) {
+// Eight codes are eight bytes of a lane.
+__device__ inline u32x2 load_codes(Row row, uint32_t chunk) {
+    return __builtin_amdgcn_raw_buffer_load_b64(row, static_cast<int>(chunk * 8u), 0, kStream);
+}
+__device__ inline void store_codes(Row row, uint32_t chunk, const u32x2& c) {
+    __builtin_amdgcn_raw_buffer_store_b64(c, row, static_cast<int>(chunk * 8u), 0, kStream);
+}
+// One float of a row; the scales of a row are shared by the waves of a block, so they stay in the cache.
+__device__ inline float load_float(Row row, uint32_t offset) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(row, static_cast<int>(offset), 0, 0));
+}
+__device__ inline void store_float(Row row, uint32_t offset, float v) {
+    __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), row, static_cast<int>(offset), 0, 0);
+}
+// Eight partial sums of a lane; they stay in the cache for the second pass.
+__device__ inline void store_sums8(Row row, uint32_t chunk, const float (&v)[8]) {
 #pragma unroll
-    for (int h = 0; h < NV; ++h) q[h] = u32x4{0u, 0u, 0u, 0u};
+    for (int h = 0; h < 2; ++h) {
+        const f32x4 t = {v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, t), row, static_cast<int>(chunk * 32u + 16u * h), 0, 0);
+    }
 }
+// A float that no kernel of the launch writes, at a uniform address: a scalar load (see table_at).
+typedef const float __attribute__((address_space(4))) * const_f32_ptr;
+__device__ inline float float_at(const float* p, int64_t i) { return ((const_f32_ptr)p)[i]; }
+
 template <int NV>
 __device__ inline void opaque(u32x4 (&q)[NV]) {        // the fp32 values are rebuilt behind this, not carried across it
 #pragma unroll
     for (int h = 0; h < NV; ++h) asm volatile("" : "+v"(q[h]));
 }
 
-// Eight codes are eight bytes of a lane.
-__device__ inline u32x2 load_codes(const void* base, int64_t uniform_off, uint32_t chunk) {
-    return __builtin_nontemporal_load(
-        reinterpret_cast<const u32x2*>(static_cast<const char*>(base) + uniform64(uniform_off) + chunk * 8u));
-}
-__device__ inline void store_codes(void* base, int64_t uniform_off, uint32_t chunk, const u32x2& c) {
-    __builtin_nontemporal_store(c, reinterpret_cast<u32x2*>(static_cast<char*>(base) + uniform64(uniform_off) + chunk * 8u));
-}
-
 // ---- largest magnitude of a group: 4, 8 or 16 consecutive lanes, inside one DPP row ----------------------------------
-template <int CTRL> __device__ inline uint32_t dpp_max(uint32_t v) {
-    const uint32_t t = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, 0xf, 0xf, false));
+template <int CTRL> __device__ inline uint32_t dpp_max(uint32_t v, uint32_t mask = ~0u) {
+    const uint32_t t = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, 0xf, 0xf, false)) & mask;
     return t > v ? t : v;
 }
-// Every lane of the group returns it; all 64 lanes take part.  lanes_log2 is uniform: 2, 3 or 4.
+// Every lane of the group returns it; all 64 lanes take part.  lanes_log2 is uniform: 2, 3 or 4; the steps that a smaller
+// group has none of are masked, not branched around.
 __device__ inline uint32_t group_max(uint32_t v, int lanes_log2) {
-    v = dpp_max<0xB1>(v);                    // quad_perm [1,0,3,2]
-    v = dpp_max<0x4E>(v);                    // quad_perm [2,3,0,1]
-    if (lanes_log2 > 2) v = dpp_max<0x141>(v);   // row_half_mirror
-    if (lanes_log2 > 3) v = dpp_max<0x140>(v);   // row_mirror
-    return v;
+    v = dpp_max<0xB1>(v);                                     // quad_perm [1,0,3,2]
+    v = dpp_max<0x4E>(v);                                     // quad_perm [2,3,0,1]
+    v = dpp_max<0x141>(v, lanes_log2 > 2 ? ~0u : 0u);         // row_half_mirror
+    return dpp_max<0x140>(v, lanes_log2 > 3 ? ~0u : 0u);      // row_mirror
 }
+__device__ inline uint32_t row16_max(uint32_t v) { return group_max(v, 4); }
 
 // ---- codes ------------------------------------------------------------------------------------------------------
 struct int8_code {
@@ -127,26 +148,25 @@ struct e4m3_code {
 };
 
 struct Scale {
-    float s, r;                              // r = 0 where s is NaN
+    float s, r;                              // both NaN where the group holds an infinity or a NaN
     bool good;
 };
 
-// s and r of a group.  A division costs a dozen instructions; these two are a product and two or four fused steps:
+// s and r of a group.  A division costs a dozen instructions; these two are a product, a reciprocal and four fused steps:
 // with c = fp32(1/Q), q = a*c and the exact remainder a - Q q, q + c (a - Q q) is the correctly rounded a / Q (Markstein's
-// theorem on division by fused multiply-add; for Q = 127 and 448 checked for every significand of a), and two Newton steps on
-// the hardware's reciprocal give the correctly rounded 1 / s (checked for every significand of s).
+// theorem on division by fused multiply-add; for Q = 127 and 448 checked for every significand of a), and one Newton step on
+// the hardware's reciprocal gives the correctly rounded 1 / s (checked for every significand of s).  An infinity leaves
+// a - Q q without a value, so s is NaN without being asked for.
 template <typename C>
 __device__ inline Scale scale_of(uint32_t amax_bits) {
     constexpr float Q = C::kLargest, c = 1.0f / Q;
-    const bool good = amax_bits < 0x7f800000u;
-    float a = __builtin_bit_cast(float, amax_bits);
-    a = good ? (a > 0x1p-100f ? a : 0x1p-100f) : 1.0f;
+    constexpr uint32_t kFloor = 0x0d800000u;                 // 2^-100
+    const float a = __builtin_bit_cast(float, amax_bits > kFloor ? amax_bits : kFloor);
     const float q = a * c;
     const float s = __builtin_fmaf(__builtin_fmaf(-Q, q, a), c, q);
     float r = __builtin_amdgcn_rcpf(s);
     r = __builtin_fmaf(__builtin_fmaf(-s, r, 1.0f), r, r);
-    r = __builtin_fmaf(__builtin_fmaf(-s, r, 1.0f), r, r);
-    return Scale{good ? s : __builtin_nanf(""), good ? r : 0.0f, good};
+    return Scale{s, r, amax_bits < 0x7f800000u};
 }
 
 template <typename C> __device__ u32x2 encode(const float (&v)[8], const Scale& sc);

@@ -59,24 +59,27 @@ __global__ __launch_bounds__(kQuantWaves* kWave) void quant_kernel(const QuantAr
         u32x2 code[BACK ? V : 1];
         float s[BACK ? V : 1];
     };
-    const auto live = [&](const Pieces<V>& p, int i) {
-        const uint32_t u = static_cast<uint32_t>(p.col[i]) * kWave + lane;
-        return p.row[i] < a.rows && u < static_cast<uint32_t>(a.units) && p.row[i] * a.units + u < a.total;
+    // units of piece i, 0 beyond the last row
+    const auto units_at = [&](const Pieces<V>& p, int i) -> uint32_t {
+        if (p.row[i] >= a.rows) return 0;
+        const int64_t left = a.total - (p.row[i] * a.units + static_cast<int64_t>(p.col[i]) * kWave);
+        const int32_t of_row = a.units - p.col[i] * kWave;
+        const int64_t n = left < of_row ? left : of_row;
+        return n < kWave ? static_cast<uint32_t>(n) : kWave;
+    };
+    const auto scales_at = [&](const Pieces<V>& p, int i) {
+        return row_of(a.scales, (p.row[i] * a.groups) * 4, units_at(p, i) == 0 ? 0u : static_cast<uint32_t>(a.groups) * 4u);
     };
     const auto fetch = [&](const Pieces<V>& p, Step& q) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int64_t at = p.row[i] * a.units + static_cast<int64_t>(p.col[i]) * kWave;
+            const uint32_t n = units_at(p, i);
             if constexpr (BACK) {
-                q.code[i] = u32x2{0u, 0u};
-                q.s[i] = 0.0f;
-                if (live(p, i)) {
-                    q.code[i] = load_codes(a.codes, at * 8, lane);
-                    q.s[i] = a.scales[uniform64(p.row[i] * a.groups) + ((static_cast<uint32_t>(p.col[i]) * kWave + lane) >> a.lanes_log2)];
-                }
+                q.code[i] = load_codes(row_of(a.codes, at * 8, n * 8), lane);
+                q.s[i] = load_float(scales_at(p, i), ((static_cast<uint32_t>(p.col[i]) * kWave + lane) >> a.lanes_log2) * 4u);
             } else {
-                clear(q.x[i]);
-                if (live(p, i)) load_unit<Tag>(a.x, at * Unit<Tag>::kBytes, lane, q.x[i]);
+                load_unit<Tag>(row_of(a.x, at * Unit<Tag>::kBytes, n * Unit<Tag>::kBytes), lane, q.x[i]);
             }
         }
     };
@@ -102,26 +105,22 @@ __global__ __launch_bounds__(kQuantWaves* kWave) void quant_kernel(const QuantAr
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int64_t at = cur.row[i] * a.units + static_cast<int64_t>(cur.col[i]) * kWave;
+            const uint32_t n = units_at(cur, i);
             float v[8];
             if constexpr (BACK) {
                 decode<C>(now.code[i], v);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] *= now.s[i];
-                if (live(cur, i)) {
-                    u32x4 o[NV];
-                    Unit<Tag>::pack(v, o);
-                    store_unit<Tag>(a.x, at * Unit<Tag>::kBytes, lane, o);
-                }
+                u32x4 o[NV];
+                Unit<Tag>::pack(v, o);
+                store_unit<Tag>(row_of(a.x, at * Unit<Tag>::kBytes, n * Unit<Tag>::kBytes), lane, o);
             } else {
                 const Scale sc = scale_of<C>(group_max(Unit<Tag>::amax_bits(now.x[i]), a.lanes_log2));
                 Unit<Tag>::unpack(now.x[i], v);
-                const u32x2 w = encode<C>(v, sc);
-                if (live(cur, i)) {
-                    store_codes(a.codes, at * 8, lane, w);
-                    const uint32_t u = static_cast<uint32_t>(cur.col[i]) * kWave + lane;
-                    if ((u & ((1u << a.lanes_log2) - 1u)) == 0)
-                        a.scales[uniform64(cur.row[i] * a.groups) + (u >> a.lanes_log2)] = sc.s;
-                }
+                store_codes(row_of(a.codes, at * 8, n * 8), lane, encode<C>(v, sc));
+                const uint32_t u = static_cast<uint32_t>(cur.col[i]) * kWave + lane;
+                const bool leads = lane < n && (lane & ((1u << a.lanes_log2) - 1u)) == 0;
+                store_float(scales_at(cur, i), leads ? (u >> a.lanes_log2) * 4u : kNowhere, sc.s);
             }
         }
         cur = next;

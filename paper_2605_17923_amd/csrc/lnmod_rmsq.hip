@@ -71,12 +71,19 @@ hipError_t launch_rmsq_fwd(int dtype, int code, const void* x, const void* r, co
     const dim3 grid(static_cast<unsigned>(a.nb)), block(sh.K * kWave);
     const auto run = [&](auto io, auto cd) {
         return for_shape(sh, [&](auto vpl, auto k, auto rows) {
-            using Tag = decltype(io);
-            using C = decltype(cd);
-            if (r && values) hipLaunchKernelGGL((rmsq_fwd_kernel<Tag, C, vpl, k, rows, true, true>), grid, block, 0, st, a);
-            else if (r) hipLaunchKernelGGL((rmsq_fwd_kernel<Tag, C, vpl, k, rows, true, false>), grid, block, 0, st, a);
-            else if (values) hipLaunchKernelGGL((rmsq_fwd_kernel<Tag, C, vpl, k, rows, false, true>), grid, block, 0, st, a);
-            else hipLaunchKernelGGL((rmsq_fwd_kernel<Tag, C, vpl, k, rows, false, false>), grid, block, 0, st, a);
+            const auto go = [&](auto res, auto row, auto val) {
+                hipLaunchKernelGGL((rmsq_fwd_kernel<decltype(io), decltype(cd), vpl, k, rows, res, row, val>), grid, block, 0, st, a);
+            };
+            const auto with = [&](auto res, auto row) {
+                if (values) go(res, row, std::true_type{});
+                else go(res, row, std::false_type{});
+            };
+            const auto res = [&](auto has) {
+                if (group == 0) with(has, std::true_type{});
+                else with(has, std::false_type{});
+            };
+            if (r) res(std::true_type{});
+            else res(std::false_type{});
         });
     };
     bool ok;

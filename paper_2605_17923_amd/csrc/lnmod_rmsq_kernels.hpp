@@ -41,10 +41,10 @@ constexpr int rmsq_waves(int regs) {
     return w > 4 ? 4 : w < 1 ? 1 : w;
 }
 
-// VALUES: out holds the values that the codes stand for.
-template <typename Tag, typename C, int VPL, int K, int R, bool RES, bool VALUES>
+// ROW: one scale for a row.  VALUES: out holds the values that the codes stand for.
+template <typename Tag, typename C, int VPL, int K, int R, bool RES, bool ROW, bool VALUES>
 __global__ __launch_bounds__(K* kWave)
-LNMOD_OCCUPANCY(rmsq_waves(VPL * (8 + R * 4 * Unit<Tag>::NV * (RES ? 4 : 2)) + 48))
+LNMOD_OCCUPANCY(rmsq_waves(VPL * (8 + kDepth * R * 4 * Unit<Tag>::NV * (RES ? 2 : 1)) + 48))
 void rmsq_fwd_kernel(const RmsqFwdArgs a) {
     using U = Unit<Tag>;
     constexpr int NV = U::NV;
@@ -52,9 +52,16 @@ void rmsq_fwd_kernel(const RmsqFwdArgs a) {
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t row_bytes = static_cast<int64_t>(a.D) * IO<Tag>::kBytes;
+    const uint32_t unit_bytes = static_cast<uint32_t>(row_bytes);
 
-    uint32_t chunk[VPL];
-    bool ok[VPL];
+    uint32_t chunk[VPL], scale_off[VPL];                     // scale_off: the group's first lane stores its scale
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+        chunk[i] = static_cast<uint32_t>((i * K + wave) * kWave + lane);
+        scale_off[i] = chunk[i] < static_cast<uint32_t>(a.nchunks) && (lane & ((1 << a.lanes_log2) - 1)) == 0
+                           ? (chunk[i] >> a.lanes_log2) * 4u : kNowhere;
+    }
+    const uint32_t first_lane = threadIdx.x == 0 ? 0u : kNowhere;
     float W[VPL][8];
     struct Rows {
         u32x4 x[R][VPL][NV], r[RES ? R : 1][RES ? VPL : 1][NV];
@@ -63,41 +70,35 @@ void rmsq_fwd_kernel(const RmsqFwdArgs a) {
 #pragma unroll
         for (int j = 0; j < R; ++j) {
             const int64_t row = base + j;
+            const uint32_t bytes = row < a.N ? unit_bytes : 0u;
+            const Row rx = row_of(a.x, row * row_bytes, bytes);
 #pragma unroll
-            for (int i = 0; i < VPL; ++i) {
-                clear(q.x[j][i]);
-                if constexpr (RES) clear(q.r[j][i]);
-                if (row < a.N && ok[i]) {
-                    load_unit<Tag>(a.x, row * row_bytes, chunk[i], q.x[j][i]);
-                    if constexpr (RES) load_unit<Tag>(a.r, row * row_bytes, chunk[i], q.r[j][i]);
-                }
+            for (int i = 0; i < VPL; ++i) load_unit<Tag>(rx, chunk[i], q.x[j][i]);
+            if constexpr (RES) {
+                const Row rr = row_of(a.r, row * row_bytes, bytes);
+#pragma unroll
+                for (int i = 0; i < VPL; ++i) load_unit<Tag>(rr, chunk[i], q.r[j][i]);
             }
         }
     };
-#pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-        chunk[i] = static_cast<uint32_t>((i * K + wave) * kWave + lane);
-        ok[i] = chunk[i] < static_cast<uint32_t>(a.nchunks);
-    }
     const int64_t first = static_cast<int64_t>(blockIdx.x) * R, step = static_cast<int64_t>(a.nb) * R;
-    Rows now;
-    fetch(first, now);
+    Rows bufs[kDepth];
+#pragma unroll
+    for (int d = 0; d < kDepth - 1; ++d) fetch(first + d * step, bufs[d]);
+    const Row rw = row_of(a.w, 0, unit_bytes);
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
         u32x4 t[NV];
-        clear(t);
-        if (ok[i]) load_unit_cached<Tag>(a.w, 0, chunk[i], t);
+        load_unit<Tag, 0>(rw, chunk[i], t);
         U::unpack(t, W[i]);
     }
     int buf = 0;
-    for (int64_t base = first; base < a.N; base += step) {
-        Rows nxt;
-        fetch(base + step, nxt);
-        __builtin_amdgcn_sched_barrier(0);                   // keep the requests up here
+    const auto compute = [&](int64_t base, Rows& now) {
         float rs[R], big[R];
 #pragma unroll
         for (int j = 0; j < R; ++j) {
             const int64_t row = base + j;
+            const Row rh = row_of(a.h, row * row_bytes, RES && row < a.N ? unit_bytes : 0u);
             float s = 0.0f;
             uint32_t top = 0;
 #pragma unroll
@@ -110,32 +111,33 @@ void rmsq_fwd_kernel(const RmsqFwdArgs a) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] += rv[e];
                     U::pack(v, now.x[j][i]);
-                    if (row < a.N && ok[i]) store_unit<Tag>(a.h, row * row_bytes, chunk[i], now.x[j][i]);
+                    store_unit<Tag>(rh, chunk[i], now.x[j][i]);
                 }
                 U::unpack(now.x[j][i], v);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     s += v[e] * v[e];
-                    const uint32_t b = __builtin_bit_cast(uint32_t, v[e] * W[i][e]) & 0x7fffffffu;
-                    top = b > top ? b : top;
+                    if constexpr (ROW) {
+                        const uint32_t b = __builtin_bit_cast(uint32_t, v[e] * W[i][e]) & 0x7fffffffu;
+                        top = b > top ? b : top;
+                    }
                 }
             }
             rs[j] = wave_sum(s);
-            if (a.lanes_log2 == 0) {
-                top = group_max(top, 4);
+            if constexpr (ROW) {
+                top = row16_max(top);
                 const uint32_t t0 = __builtin_amdgcn_readlane(top, 0), t1 = __builtin_amdgcn_readlane(top, 16);
                 const uint32_t t2 = __builtin_amdgcn_readlane(top, 32), t3 = __builtin_amdgcn_readlane(top, 48);
                 const uint32_t u = t0 > t1 ? t0 : t1, w = t2 > t3 ? t2 : t3;
-                top = u > w ? u : w;
+                big[j] = __builtin_bit_cast(float, u > w ? u : w);
             }
-            big[j] = __builtin_bit_cast(float, top);
         }
         if constexpr (K > 1) {
             if (lane == 0) {
 #pragma unroll
                 for (int j = 0; j < R; ++j) {
                     part[buf][j][wave][0] = rs[j];
-                    part[buf][j][wave][1] = big[j];
+                    if constexpr (ROW) part[buf][j][wave][1] = big[j];
                 }
             }
             __syncthreads();
@@ -146,8 +148,10 @@ void rmsq_fwd_kernel(const RmsqFwdArgs a) {
 #pragma unroll
                 for (int w = 0; w < K; ++w) {
                     s += part[buf][j][w][0];
-                    const uint32_t b = __builtin_bit_cast(uint32_t, part[buf][j][w][1]);
-                    top = b > top ? b : top;
+                    if constexpr (ROW) {
+                        const uint32_t b = __builtin_bit_cast(uint32_t, part[buf][j][w][1]);
+                        top = b > top ? b : top;
+                    }
                 }
                 rs[j] = s;
                 big[j] = __builtin_bit_cast(float, top);
@@ -156,7 +160,7 @@ void rmsq_fwd_kernel(const RmsqFwdArgs a) {
         }
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-            rs[j] = 1.0f / sqrtf(rs[j] * a.inv_D + a.eps);
+            rs[j] = rsqrtf(rs[j] * a.inv_D + a.eps);
 #pragma unroll
             for (int i = 0; i < VPL; ++i) opaque(now.x[j][i]);
         }
@@ -164,48 +168,57 @@ void rmsq_fwd_kernel(const RmsqFwdArgs a) {
         for (int j = 0; j < R; ++j) {
             const int64_t row = base + j;
             if (row < a.N) {
-                if (wave == 0 && lane == 0) a.rstd[row] = rs[j];
+                store_float(row_of(a.rstd, row * 4, 4), first_lane, rs[j]);
                 Scale sc;
-                if (a.lanes_log2 == 0) {
+                if constexpr (ROW) {
                     sc = scale_of<C>(__builtin_bit_cast(uint32_t, big[j] * rs[j]) & 0x7fffffffu);
-                    if (!VALUES && wave == 0 && lane == 0) a.scales[row] = sc.s;
+                    if constexpr (!VALUES) store_float(row_of(a.scales, row * 4, 4), first_lane, sc.s);
                 }
+                const Row rout = VALUES ? row_of(a.out, row * row_bytes, unit_bytes)
+                                        : row_of(a.out, row * a.D, static_cast<uint32_t>(a.D));
+                const Row rcs = row_of(a.scales, row * a.groups * 4, VALUES ? 0u : static_cast<uint32_t>(a.groups) * 4u);
 #pragma unroll
                 for (int i = 0; i < VPL; ++i) {
                     float v[8];
                     U::unpack(now.x[j][i], v);
-                    uint32_t top = 0;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] = (v[e] * rs[j]) * W[i][e];
-                    if (a.lanes_log2 != 0) {
+                    if constexpr (!ROW) {
+                        uint32_t top = 0;
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
                             const uint32_t b = __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu;
                             top = b > top ? b : top;
                         }
-                        // lanes beyond the row hold zeros, or NaN where rstd is NaN
-                        sc = scale_of<C>(group_max(ok[i] ? top : 0u, a.lanes_log2));
+                        // lanes beyond the row: 0, or NaN where rstd is NaN and so every v is
+                        sc = scale_of<C>(group_max(top, a.lanes_log2));
+                        if constexpr (!VALUES) store_float(rcs, scale_off[i], sc.s);
                     }
                     const u32x2 w = encode<C>(v, sc);
-                    if (ok[i]) {
-                        if constexpr (VALUES) {
-                            u32x4 o[NV];
-                            decode<C>(w, v);
+                    if constexpr (VALUES) {
+                        u32x4 o[NV];
+                        decode<C>(w, v);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) v[e] *= sc.s;
-                            U::pack(v, o);
-                            store_unit<Tag>(a.out, row * row_bytes, chunk[i], o);
-                        } else {
-                            store_codes(a.out, row * a.D, chunk[i], w);
-                            if (a.lanes_log2 != 0 && (lane & ((1 << a.lanes_log2) - 1)) == 0)
-                                a.scales[uniform64(row * a.groups) + (chunk[i] >> a.lanes_log2)] = sc.s;
-                        }
+                        for (int e = 0; e < 8; ++e) v[e] *= sc.s;
+                        U::pack(v, o);
+                        store_unit<Tag>(rout, chunk[i], o);
+                    } else {
+                        store_codes(rout, chunk[i], w);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
         }
-        now = nxt;
+    };
+    for (int64_t base = first; base < a.N;) {
+#pragma unroll
+        for (int d = 0; d < kDepth; ++d) {
+            if (base >= a.N) break;
+            fetch(base + (kDepth - 1) * step, bufs[(d + kDepth - 1) % kDepth]);
+            __builtin_amdgcn_sched_barrier(0);               // keep the requests up here
+            compute(base, bufs[d]);
+            base += step;
+        }
     }
 }
 
@@ -226,7 +239,7 @@ struct RmsqBwdArgs {
 
 template <typename Tag, int VPL, int K, int R, bool DH>
 __global__ __launch_bounds__(K* kWave)
-LNMOD_OCCUPANCY(rmsq_waves(VPL * (16 + 2 * R * 4 * Unit<Tag>::NV * (DH ? 3 : 2)) + 56))
+LNMOD_OCCUPANCY(rmsq_waves(VPL * (16 + kDepth * R * 4 * Unit<Tag>::NV * (DH ? 3 : 2)) + 56))
 void rmsq_bwd_kernel(const RmsqBwdArgs a) {
     using U = Unit<Tag>;
     constexpr int NV = U::NV;
@@ -234,9 +247,9 @@ void rmsq_bwd_kernel(const RmsqBwdArgs a) {
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t row_bytes = static_cast<int64_t>(a.D) * IO<Tag>::kBytes;
+    const uint32_t unit_bytes = static_cast<uint32_t>(row_bytes);
 
     uint32_t chunk[VPL];
-    bool ok[VPL];
     float W[VPL][8], acc[VPL][8];
     struct Rows {
         u32x4 dy[R][VPL][NV], h[R][VPL][NV], dh[DH ? R : 1][DH ? VPL : 1][NV];
@@ -247,42 +260,38 @@ void rmsq_bwd_kernel(const RmsqBwdArgs a) {
         for (int j = 0; j < R; ++j) {
             const int64_t row = base + j;
             const bool live = row < a.N;
-            q.rs[j] = live ? a.rstd[row] : 0.0f;
+            q.rs[j] = live ? float_at(a.rstd, live ? row : a.N - 1) : 0.0f;
+            const uint32_t bytes = live ? unit_bytes : 0u;
+            const Row rdy = row_of(a.dy, row * row_bytes, bytes), rh = row_of(a.h, row * row_bytes, bytes);
 #pragma unroll
             for (int i = 0; i < VPL; ++i) {
-                clear(q.dy[j][i]);
-                clear(q.h[j][i]);
-                if constexpr (DH) clear(q.dh[j][i]);
-                if (live && ok[i]) {
-                    load_unit<Tag>(a.dy, row * row_bytes, chunk[i], q.dy[j][i]);
-                    load_unit<Tag>(a.h, row * row_bytes, chunk[i], q.h[j][i]);
-                    if constexpr (DH) load_unit<Tag>(a.dh, row * row_bytes, chunk[i], q.dh[j][i]);
-                }
+                load_unit<Tag>(rdy, chunk[i], q.dy[j][i]);
+                load_unit<Tag>(rh, chunk[i], q.h[j][i]);
+            }
+            if constexpr (DH) {
+                const Row rdh = row_of(a.dh, row * row_bytes, bytes);
+#pragma unroll
+                for (int i = 0; i < VPL; ++i) load_unit<Tag>(rdh, chunk[i], q.dh[j][i]);
             }
         }
     };
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-        chunk[i] = static_cast<uint32_t>((i * K + wave) * kWave + lane);
-        ok[i] = chunk[i] < static_cast<uint32_t>(a.nchunks);
-    }
+    for (int i = 0; i < VPL; ++i) chunk[i] = static_cast<uint32_t>((i * K + wave) * kWave + lane);
     const int64_t first = static_cast<int64_t>(blockIdx.x) * R, step = static_cast<int64_t>(a.nb) * R;
-    Rows now;
-    fetch(first, now);
+    Rows bufs[kDepth];
+#pragma unroll
+    for (int d = 0; d < kDepth - 1; ++d) fetch(first + d * step, bufs[d]);
+    const Row rw = row_of(a.w, 0, unit_bytes);
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
         u32x4 t[NV];
-        clear(t);
-        if (ok[i]) load_unit_cached<Tag>(a.w, 0, chunk[i], t);
+        load_unit<Tag, 0>(rw, chunk[i], t);
         U::unpack(t, W[i]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[i][e] = 0.0f;
     }
     int buf = 0;
-    for (int64_t base = first; base < a.N; base += step) {
-        Rows nxt;
-        fetch(base + step, nxt);
-        __builtin_amdgcn_sched_barrier(0);                   // keep the requests up here
+    const auto compute = [&](int64_t base, Rows& now) {
         float c[R];
 #pragma unroll
         for (int j = 0; j < R; ++j) {
@@ -330,41 +339,41 @@ void rmsq_bwd_kernel(const RmsqBwdArgs a) {
 #pragma unroll
         for (int j = 0; j < R; ++j) {
             const int64_t row = base + j;
-            if (row < a.N) {
-                const float k2 = now.rs[j] * (c[j] * a.inv_D);
+            const Row rdx = row_of(a.dx, row * row_bytes, row < a.N ? unit_bytes : 0u);
+            const float k2 = now.rs[j] * (c[j] * a.inv_D);
 #pragma unroll
-                for (int i = 0; i < VPL; ++i) {
-                    if (ok[i]) {
-                        float dyv[8], hv[8], o[8];
-                        U::unpack(now.dy[j][i], dyv);
-                        U::unpack(now.h[j][i], hv);
+            for (int i = 0; i < VPL; ++i) {
+                float dyv[8], hv[8], o[8];
+                U::unpack(now.dy[j][i], dyv);
+                U::unpack(now.h[j][i], hv);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) o[e] = (dyv[e] * W[i][e]) * now.rs[j] - (hv[e] * now.rs[j]) * k2;
-                        if constexpr (DH) {
-                            float t[8];
-                            U::unpack(now.dh[j][i], t);
+                for (int e = 0; e < 8; ++e) o[e] = (dyv[e] * W[i][e]) * now.rs[j] - (hv[e] * now.rs[j]) * k2;
+                if constexpr (DH) {
+                    float t[8];
+                    U::unpack(now.dh[j][i], t);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) o[e] += t[e];
-                        }
-                        u32x4 t[NV];
-                        U::pack(o, t);
-                        store_unit<Tag>(a.dx, row * row_bytes, chunk[i], t);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
+                    for (int e = 0; e < 8; ++e) o[e] += t[e];
                 }
+                u32x4 t[NV];
+                U::pack(o, t);
+                store_unit<Tag>(rdx, chunk[i], t);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
-        now = nxt;
-    }
-    float* slot = a.ws + static_cast<int64_t>(blockIdx.x) * a.D;
+    };
+    for (int64_t base = first; base < a.N;) {
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-        if (ok[i]) {
-            f32x4* ps = reinterpret_cast<f32x4*>(slot + chunk[i] * kUnit);
-#pragma unroll
-            for (int q = 0; q < 2; ++q) ps[q] = f32x4{acc[i][4 * q], acc[i][4 * q + 1], acc[i][4 * q + 2], acc[i][4 * q + 3]};
+        for (int d = 0; d < kDepth; ++d) {
+            if (base >= a.N) break;
+            fetch(base + (kDepth - 1) * step, bufs[(d + kDepth - 1) % kDepth]);
+            __builtin_amdgcn_sched_barrier(0);               // keep the requests up here
+            compute(base, bufs[d]);
+            base += step;
         }
     }
+    const Row slot = row_of(a.ws, static_cast<int64_t>(blockIdx.x) * a.D * 4, static_cast<uint32_t>(a.D) * 4u);
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) store_sums8(slot, chunk[i], acc[i]);
 }
 
 }  // namespace lnmod
