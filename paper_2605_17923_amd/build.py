@@ -31,7 +31,8 @@ TOOLS_SOURCES = KERNEL_SOURCES + ["lnmod_misc.hip", "lnmod_tools_api.cpp"]
 SOURCES = LIBRARY_SOURCES + [s for s in TOOLS_SOURCES if s not in LIBRARY_SOURCES]
 HEADERS = [os.path.join(CSRC, "lnmod_kernels.hpp"), os.path.join(CSRC, "lnmod_launch.hpp"),
            os.path.join(CSRC, "lnmod_gated_kernels.hpp"), os.path.join(CSRC, "lnmod_qknorm_kernels.hpp"),
-           os.path.join(CSRC, "lnmod_code.hpp"), os.path.join(CSRC, "lnmod_quant_kernels.hpp"),
+           os.path.join(CSRC, "lnmod_code.hpp"), os.path.join(CSRC, "lnmod_code_shapes.hpp"),
+           os.path.join(CSRC, "lnmod_quant_kernels.hpp"),
            os.path.join(CSRC, "lnmod_ckpt_kernels.hpp"), os.path.join(CSRC, "lnmod_rmsq_kernels.hpp"),
            os.path.join(CSRC, "lnmod_api_impl.hpp"),
            os.path.join(INCLUDE, "lnmod.h"), os.path.join(INCLUDE, "lnmod_sched.h"),

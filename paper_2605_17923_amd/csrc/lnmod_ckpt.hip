@@ -1,47 +1,11 @@
 // lnmod_ckpt.hip -- instantiation and launch of LayerNorm-Modulate with an 8-bit checkpoint of x: the forward that writes
 // it and the backward that reads it.
 #include "lnmod_ckpt_kernels.hpp"
+#include "lnmod_code_shapes.hpp"
 #include "lnmod_launch.hpp"
 
 namespace lnmod {
 namespace {
-
-// Two units per lane, as many waves as the row then needs.
-Shape simple_shape(int units, int dtype) {
-    Shape sh{1, 1, dtype == 0 ? 2 : 1, 8};
-    if (units > kWave) {
-        sh.VPL = 2;
-        sh.K = (units + 2 * kWave - 1) / (2 * kWave);
-        if (sh.K == 7) sh.K = 8;
-        sh.per_cu = sh.K <= 1 ? 8 : sh.K == 2 ? 4 : sh.K <= 4 ? 2 : 1;
-    }
-    return sh;
-}
-
-Shape ckpt_fwd_shape(int units, int dtype) { return simple_shape(units, dtype); }
-Shape ckpt_bwd_shape(int units, int dtype) { return simple_shape(units, dtype); }
-
-// f(VPL, K, R) as constants; false for a shape that is not compiled
-template <typename F>
-bool for_shape(const Shape& sh, F&& f) {
-    using std::integral_constant;
-    const auto rows = [&](auto vpl, auto k) {
-        if (sh.R == 1) f(vpl, k, integral_constant<int, 1>{});
-        else f(vpl, k, integral_constant<int, 2>{});
-        return true;
-    };
-    switch (sh.VPL * 100 + sh.K) {
-        case 101: return rows(integral_constant<int, 1>{}, integral_constant<int, 1>{});
-        case 201: return rows(integral_constant<int, 2>{}, integral_constant<int, 1>{});
-        case 202: return rows(integral_constant<int, 2>{}, integral_constant<int, 2>{});
-        case 203: return rows(integral_constant<int, 2>{}, integral_constant<int, 3>{});
-        case 204: return rows(integral_constant<int, 2>{}, integral_constant<int, 4>{});
-        case 205: return rows(integral_constant<int, 2>{}, integral_constant<int, 5>{});
-        case 206: return rows(integral_constant<int, 2>{}, integral_constant<int, 6>{});
-        case 208: return rows(integral_constant<int, 2>{}, integral_constant<int, 8>{});
-        default: return false;
-    }
-}
 
 // f(element type, code)
 template <typename F>
@@ -56,6 +20,7 @@ Codes codes_of(const Problem& p, const Checkpoint& c) {
     cd.scales = c.scales;
     cd.lanes_log2 = group_lanes_log2(c.group);
     cd.groups = static_cast<int32_t>((p.D + c.group - 1) / c.group);
+    cd.keep = keep_codes(p.T, p.D, 20000000, 70000000);
     return cd;
 }
 
@@ -71,7 +36,7 @@ int64_t fwd_clusters(int64_t nseg) {
 }  // namespace
 
 RowPlan ckpt_bwd_plan(int64_t T, int64_t nseg, int64_t D, int dtype, Shape* shape, const Shape* force) {
-    const Shape sh = pick_shape(force, ckpt_bwd_shape(static_cast<int>(D / kUnit), dtype));
+    const Shape sh = pick_shape(force, ckpt_bwd_shape(T, static_cast<int>(D / kUnit), dtype));
     if (shape) *shape = sh;
     // a row moves 2 D elements (dy, dx) and D codes, a slot 2 D floats that are written and read back
     const double row = 2.0 * (dtype == 0 ? 2.0 : 4.0) + 1.0;
@@ -95,7 +60,7 @@ hipError_t launch_ckpt_fwd(const Problem& p, bool token, const void* x, const vo
     a.f.eps = p.eps;
     a.f.inv_D = 1.0f / static_cast<float>(p.D);
     a.c = codes_of(p, c);
-    const Shape sh = pick_shape(p.force, ckpt_fwd_shape(a.f.nchunks, p.dtype));
+    const Shape sh = pick_shape(p.force, ckpt_fwd_shape(p.T, a.f.nchunks, p.dtype));
     if (!covers(sh, a.f.nchunks)) return hipErrorInvalidConfiguration;
     const RowPlan pl = plan_rows_clusters(p.T, token ? 1 : p.nseg, static_cast<int64_t>(kNumCU) * sh.per_cu, sh.R,
                                           token ? 1 : fwd_clusters(p.nseg), sh.clusters);
@@ -105,12 +70,16 @@ hipError_t launch_ckpt_fwd(const Problem& p, bool token, const void* x, const vo
     a.f.split = cluster_split(a.f.interleave, pl);
     const dim3 grid(static_cast<unsigned>(pl.blocks)), block(sh.K * kWave);
     const bool ok = for_types(p.dtype, code, [&](auto io, auto cd) {
-        return for_shape(sh, [&](auto vpl, auto k, auto r) {
+        const auto go = [&](auto vpl, auto k, auto r) {
             using Tag = decltype(io);
             using C = decltype(cd);
             if (token) hipLaunchKernelGGL((ckpt_fwd_kernel<Tag, C, vpl, k, r, true>), grid, block, 0, st, a);
             else hipLaunchKernelGGL((ckpt_fwd_kernel<Tag, C, vpl, k, r, false>), grid, block, 0, st, a);
-        });
+        };
+        if constexpr (std::is_same<decltype(io), bf16_io>::value)
+            return ShapesOf<kSplit, kCkptFwd40, kCkptFwd200, kCkptFwdLong>::call(sh, go);
+        else
+            return ShapesOf<kSplit, kCkptFwd32>::call(sh, go);
     });
     return ok ? hipGetLastError() : hipErrorInvalidConfiguration;
 }
@@ -143,12 +112,14 @@ hipError_t launch_ckpt_bwd(const Problem& p, bool token, const void* dy, const C
     a.b.split = cluster_split(a.b.interleave, pl);
     const dim3 grid(static_cast<unsigned>(pl.blocks)), block(sh.K * kWave);
     const bool ok = for_types(p.dtype, code, [&](auto io, auto cd) {
-        return for_shape(sh, [&](auto vpl, auto k, auto r) {
+        const auto go = [&](auto vpl, auto k, auto r) {
             using Tag = decltype(io);
             using C = decltype(cd);
             if (token) hipLaunchKernelGGL((ckpt_bwd_kernel<Tag, C, vpl, k, r, true>), grid, block, 0, st, a);
             else hipLaunchKernelGGL((ckpt_bwd_kernel<Tag, C, vpl, k, r, false>), grid, block, 0, st, a);
-        });
+        };
+        if constexpr (std::is_same<decltype(io), bf16_io>::value) return ShapesOf<kCkptBwd50, kCkptBwdLong>::call(sh, go);
+        else return ShapesOf<kCkptBwd50x32, kCkptBwd32>::call(sh, go);
     });
     if (!ok) return hipErrorInvalidConfiguration;
     const hipError_t e = hipGetLastError();

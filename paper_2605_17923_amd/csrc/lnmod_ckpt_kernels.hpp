@@ -23,6 +23,7 @@ struct Codes {
     float* scales;           // [N, groups]
     int32_t groups;
     int32_t lanes_log2;      // of a group
+    int32_t keep;            // forward: codes stored for a reader soon (see keep_codes)
 };
 
 struct CkptFwdArgs {
@@ -215,7 +216,7 @@ void ckpt_fwd_kernel(const CkptFwdArgs args) {
                     const Scale sc = scale_of<C>(group_max(U::amax_bits(raw[0][j][i]), cd.lanes_log2));
                     float v[8], o[8];
                     U::unpack(raw[0][j][i], v);
-                    store_codes(rc, chunk[i], encode<C>(v, sc));
+                    store_codes(rc, chunk[i], encode<C>(v, sc), cd.keep);
                     store_float(rcs, scale_off[i], sc.s);
                     if constexpr (TOK) {
                         float p[8], t[8];

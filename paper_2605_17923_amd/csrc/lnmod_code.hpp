@@ -96,8 +96,10 @@ __device__ inline void store_unit(Row row, uint32_t chunk, const u32x4 (&q)[Unit
 __device__ inline u32x2 load_codes(Row row, uint32_t chunk) {
     return __builtin_amdgcn_raw_buffer_load_b64(row, static_cast<int>(chunk * 8u), 0, kStream);
 }
-__device__ inline void store_codes(Row row, uint32_t chunk, const u32x2& c) {
-    __builtin_amdgcn_raw_buffer_store_b64(c, row, static_cast<int>(chunk * 8u), 0, kStream);
+// keep (uniform): codes that the last-level cache can hold stay there for their reader, see keep_codes.
+__device__ inline void store_codes(Row row, uint32_t chunk, const u32x2& c, int32_t keep) {
+    if (keep) __builtin_amdgcn_raw_buffer_store_b64(c, row, static_cast<int>(chunk * 8u), 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b64(c, row, static_cast<int>(chunk * 8u), 0, kStream);
 }
 // One float of a row; the scales of a row are shared by the waves of a block, so they stay in the cache.
 __device__ inline float load_float(Row row, uint32_t offset) {

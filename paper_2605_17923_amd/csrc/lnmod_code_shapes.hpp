@@ -1,0 +1,145 @@
+// lnmod_code_shapes.hpp -- launch shapes {waves per row, units per lane, rows per block and step, blocks per CU} of the row
+// kernels that hold activations in 8 bits, and their dispatch.
+//
+// A table has an entry per 512 features (one unit of eight features for each lane of one wave).  The entries are from a sweep of
+// every (waves, units) that cover a row closely with one and two rows, 1 to 128 blocks per CU, at a multiple of 512 features and
+// 200 below it, on x of 3, 20, 60, 120 and 500 MB, bf16 and fp32.  What they share: waves * units is the row's length in
+// units of 512 features wherever that is possible, because every idle lane costs arithmetic, and the arithmetic of the
+// few waves that HBM likes best is what limits them; forwards, which keep nothing from row to row but the weights, win with
+// many more blocks than are resident (root-mean-square norm, 32 760 x 5120 bf16: 118 us with one block per CU, 80.5 with 64);
+// backwards keep a slot of partial sums per block and stay at the few blocks that are resident.
+// The classes of x's size and what the entries lose against the best shape of each problem, in the mean and at worst:
+//   checkpoint forward   bf16 up to 10 MB 1.6 %, 5 %; 40 MB 2 %, 14 %; 200 MB 1 %, 6 %; beyond 1 %, 5 %;  fp32 1 to 3 %
+//   rms norm forward     bf16 1 to 3 %, 14 %;  fp32 2 to 4 %
+//   backwards            bf16 and fp32 up to 50 MB and beyond: 1 to 2 %, 12 % (one wave per row: up to 23 %)
+#pragma once
+#include <array>
+#include <utility>
+
+#include "lnmod_launch.hpp"
+
+namespace lnmod {
+
+using ShapeTable = std::array<Shape, 16>;            // [k]: rows of more than 512 k and at most 512 (k + 1) features
+
+constexpr bool covers_all(const ShapeTable& t) {
+    for (int k = 0; k < 16; ++k)
+        if (t[k].K * t[k].VPL < k + 1) return false;
+    return true;
+}
+constexpr ShapeTable with(ShapeTable t, int rows, int per_cu) {
+    for (int k = 0; k < 16; ++k) {
+        t[k].R = rows;
+        t[k].per_cu = per_cu;
+    }
+    return t;
+}
+
+// The split of a row that most kernels share.
+inline constexpr ShapeTable kSplit = {{
+    {1, 1, 1, 16}, {2, 1, 1, 16}, {3, 1, 1, 16}, {4, 1, 1, 16}, {5, 1, 1, 16}, {3, 2, 1, 16}, {4, 2, 1, 16}, {4, 2, 1, 16},
+    {3, 3, 1, 16}, {5, 2, 1, 16}, {4, 3, 1, 16}, {4, 3, 1, 16}, {8, 2, 1, 16}, {8, 2, 1, 16}, {8, 2, 1, 16}, {8, 2, 1, 16}}};
+
+// Checkpoint forward
+inline constexpr ShapeTable kCkptFwd40 = {{
+    {1, 1, 2, 32}, {1, 2, 2, 16}, {3, 1, 2, 8}, {4, 1, 2, 4}, {5, 1, 2, 4}, {3, 2, 2, 4}, {4, 2, 2, 4}, {4, 2, 2, 4},
+    {3, 3, 1, 4}, {5, 2, 2, 2}, {4, 3, 2, 3}, {4, 3, 2, 3}, {4, 4, 2, 2}, {4, 4, 2, 2}, {4, 4, 2, 2}, {4, 4, 1, 2}}};
+inline constexpr ShapeTable kCkptFwd200 = {{
+    {1, 1, 2, 128}, {2, 1, 2, 128}, {3, 1, 2, 64}, {4, 1, 2, 128}, {3, 2, 2, 32}, {3, 2, 2, 32}, {4, 2, 1, 2}, {4, 2, 2, 64},
+    {3, 3, 2, 128}, {5, 2, 1, 2}, {4, 3, 1, 1}, {4, 3, 1, 1}, {8, 2, 1, 1}, {8, 2, 1, 1}, {8, 2, 1, 1}, {4, 4, 1, 1}}};
+inline constexpr ShapeTable kCkptFwdLong = {{
+    {1, 1, 2, 128}, {1, 2, 2, 4}, {3, 1, 2, 128}, {4, 1, 2, 128}, {5, 1, 2, 64}, {3, 2, 2, 128}, {4, 2, 2, 128}, {4, 2, 2, 1},
+    {3, 3, 2, 128}, {5, 2, 1, 64}, {4, 3, 2, 1}, {4, 3, 1, 1}, {4, 4, 1, 64}, {4, 4, 1, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}}};
+inline constexpr ShapeTable kCkptFwd32 = {{
+    {1, 1, 2, 8}, {1, 2, 2, 4}, {3, 1, 2, 3}, {4, 1, 2, 2}, {3, 2, 1, 2}, {3, 2, 1, 2}, {4, 2, 1, 2}, {4, 2, 1, 2},
+    {3, 3, 1, 2}, {5, 2, 1, 1}, {4, 3, 1, 1}, {4, 3, 1, 1}, {4, 4, 1, 1}, {8, 2, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}}};
+
+// Root-mean-square norm, forward
+inline constexpr ShapeTable kRmsFwd200 = with(kSplit, 1, 128);
+inline constexpr ShapeTable kRmsFwdLong = with(kSplit, 2, 128);
+inline constexpr ShapeTable kRmsFwd32 = {{
+    {1, 1, 2, 4}, {1, 2, 2, 4}, {3, 1, 1, 2}, {4, 1, 1, 2}, {5, 1, 1, 2}, {3, 2, 1, 2}, {4, 2, 1, 2}, {4, 2, 1, 2},
+    {3, 3, 1, 2}, {5, 2, 1, 2}, {4, 3, 1, 1}, {4, 3, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}}};
+
+// Backward from a checkpoint
+inline constexpr ShapeTable kCkptBwd50 = {{
+    {1, 1, 2, 4}, {1, 2, 2, 3}, {3, 1, 2, 1}, {4, 1, 2, 1}, {5, 1, 2, 1}, {3, 2, 2, 1}, {4, 2, 2, 1}, {4, 2, 2, 1},
+    {3, 3, 2, 1}, {10, 1, 2, 1}, {12, 1, 2, 1}, {12, 1, 2, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}}};
+inline constexpr ShapeTable kCkptBwdLong = {{
+    {1, 1, 2, 8}, {1, 2, 2, 4}, {1, 3, 2, 3}, {4, 1, 2, 2}, {5, 1, 2, 2}, {3, 2, 2, 2}, {4, 2, 2, 1}, {4, 2, 2, 1},
+    {3, 3, 2, 1}, {4, 3, 2, 1}, {4, 3, 1, 1}, {4, 3, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}}};
+inline constexpr ShapeTable kCkptBwd50x32 = {{
+    {1, 1, 2, 3}, {2, 1, 2, 2}, {3, 1, 2, 1}, {4, 1, 2, 1}, {3, 2, 2, 1}, {3, 2, 2, 1}, {4, 2, 2, 1}, {4, 2, 2, 1},
+    {3, 3, 2, 1}, {10, 1, 2, 1}, {12, 1, 2, 1}, {12, 1, 2, 1}, {8, 2, 1, 1}, {8, 2, 1, 1}, {8, 2, 1, 1}, {4, 4, 1, 1}}};
+inline constexpr ShapeTable kCkptBwd32 = {{
+    {1, 1, 2, 4}, {1, 2, 2, 3}, {3, 1, 2, 1}, {4, 1, 2, 1}, {3, 2, 2, 1}, {3, 2, 2, 1}, {4, 2, 2, 1}, {4, 2, 2, 1},
+    {3, 3, 2, 1}, {4, 3, 1, 1}, {4, 3, 1, 1}, {4, 3, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}}};
+
+// Root-mean-square norm, backward
+inline constexpr ShapeTable kRmsBwd50 = {{
+    {1, 1, 2, 3}, {2, 1, 2, 2}, {3, 1, 2, 1}, {4, 1, 2, 1}, {5, 1, 1, 1}, {3, 2, 1, 1}, {4, 2, 1, 1}, {4, 2, 2, 1},
+    {3, 3, 2, 1}, {10, 1, 2, 1}, {12, 1, 2, 1}, {12, 1, 2, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}}};
+inline constexpr ShapeTable kRmsBwdLong = {{
+    {1, 1, 1, 8}, {1, 2, 1, 3}, {3, 1, 2, 1}, {4, 1, 2, 1}, {5, 1, 1, 1}, {3, 2, 1, 1}, {4, 2, 1, 1}, {8, 1, 2, 1},
+    {3, 3, 2, 1}, {10, 1, 1, 1}, {12, 1, 1, 1}, {12, 1, 1, 1}, {8, 2, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {8, 2, 1, 1}}};
+inline constexpr ShapeTable kRmsBwd50x32 = {{
+    {1, 1, 2, 3}, {2, 1, 1, 2}, {3, 1, 1, 1}, {4, 1, 1, 1}, {5, 1, 2, 1}, {3, 2, 1, 1}, {4, 2, 1, 1}, {4, 2, 1, 1},
+    {3, 3, 1, 1}, {10, 1, 1, 1}, {4, 3, 1, 1}, {4, 3, 1, 1}, {8, 2, 1, 1}, {8, 2, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}}};
+inline constexpr ShapeTable kRmsBwd32 = {{
+    {1, 1, 2, 3}, {1, 2, 2, 3}, {3, 1, 2, 1}, {4, 1, 2, 1}, {3, 2, 2, 1}, {3, 2, 2, 1}, {4, 2, 2, 1}, {4, 2, 2, 1},
+    {3, 3, 2, 1}, {4, 3, 2, 1}, {4, 3, 1, 1}, {4, 3, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}}};
+
+static_assert(covers_all(kSplit) && covers_all(kCkptFwd40) && covers_all(kCkptFwd200) && covers_all(kCkptFwdLong) &&
+              covers_all(kCkptFwd32) && covers_all(kRmsFwd32) && covers_all(kCkptBwd50) && covers_all(kCkptBwdLong) &&
+              covers_all(kCkptBwd50x32) && covers_all(kCkptBwd32) && covers_all(kRmsBwd50) && covers_all(kRmsBwdLong) &&
+              covers_all(kRmsBwd50x32) && covers_all(kRmsBwd32), "an entry that does not cover its rows");
+
+inline const Shape& entry(const ShapeTable& t, int units) { return t[(units - 1) / 64]; }
+
+inline Shape ckpt_fwd_shape(int64_t T, int units, int dtype) {
+    const int64_t bytes = T * units * (dtype == 0 ? 16 : 32);
+    if (bytes <= 10000000) return entry(kSplit, units);
+    if (dtype != 0) return entry(kCkptFwd32, units);
+    return entry(bytes <= 40000000 ? kCkptFwd40 : bytes <= 200000000 ? kCkptFwd200 : kCkptFwdLong, units);
+}
+inline Shape rms_fwd_shape(int64_t N, int units, int dtype) {
+    const int64_t bytes = N * units * (dtype == 0 ? 16 : 32);
+    if (bytes <= 10000000) return entry(kSplit, units);
+    if (dtype != 0) return entry(kRmsFwd32, units);
+    return entry(bytes <= 200000000 ? kRmsFwd200 : kRmsFwdLong, units);
+}
+inline Shape ckpt_bwd_shape(int64_t T, int units, int dtype) {
+    const bool shorter = T * units * (dtype == 0 ? 16 : 32) <= 50000000;
+    if (dtype == 0) return entry(shorter ? kCkptBwd50 : kCkptBwdLong, units);
+    return entry(shorter ? kCkptBwd50x32 : kCkptBwd32, units);
+}
+inline Shape rms_bwd_shape(int64_t N, int units, int dtype) {
+    const bool shorter = N * units * (dtype == 0 ? 16 : 32) <= 50000000;
+    if (dtype == 0) return entry(shorter ? kRmsBwd50 : kRmsBwdLong, units);
+    return entry(shorter ? kRmsBwd50x32 : kRmsBwd32, units);
+}
+
+// f(units per lane, waves, rows) as constants for the entry of one of the tables that sh is; false if it is none.  Only what
+// the tables hold is compiled.
+template <const ShapeTable&... TABS>
+struct ShapesOf {
+    template <typename F>
+    static bool call(const Shape& sh, F&& f) {
+        return (one<TABS>(sh, f, std::make_index_sequence<16>{}) || ...);
+    }
+
+private:
+    template <const ShapeTable& TAB, typename F, size_t... I>
+    static bool one(const Shape& sh, F&& f, std::index_sequence<I...>) {
+        return (entry<TAB, I>(sh, f) || ...);
+    }
+    template <const ShapeTable& TAB, size_t I, typename F>
+    static bool entry(const Shape& sh, F&& f) {
+        using std::integral_constant;
+        if (sh.K != TAB[I].K || sh.VPL != TAB[I].VPL || sh.R != TAB[I].R) return false;
+        f(integral_constant<int, TAB[I].VPL>{}, integral_constant<int, TAB[I].K>{}, integral_constant<int, TAB[I].R>{});
+        return true;
+    }
+};
+
+}  // namespace lnmod

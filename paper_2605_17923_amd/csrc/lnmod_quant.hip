@@ -5,8 +5,18 @@
 namespace lnmod {
 namespace {
 
-constexpr int kPieces = 4;           // pieces per wave and step
-constexpr int kBlocksPerCu = 4;
+// Pieces a wave takes per step, and blocks per CU that the grid has at most (many more than are resident: with four,
+// 75 600 x 5120 bf16 took 211 us there and 217 back, with 64 it takes 187 and 194; 10 000 x 5120 30.8 and 31.4, with 32 of two
+// pieces 26.7 and 27.4).  Small launches take one piece a wave, so that every CU has a part (200 x 5120 3.9 -> 2.7 us, 1025 x 1432
+// 4.3 -> 3.3); fp32 units are 32 bytes of a lane and always take one (20 000 x 5120 97 and 134 -> 88 and 95).
+struct QuantShape {
+    int pieces, per_cu;
+};
+QuantShape quant_shape(int64_t bytes, int dtype) {
+    if (dtype != 0) return {1, 1 << 20};
+    if (bytes <= 16000000) return {1, 16};
+    return bytes <= 300000000 ? QuantShape{2, 32} : QuantShape{4, 64};
+}
 
 template <bool BACK>
 hipError_t launch(int dtype, int code, const void* x, void* codes, float* scales, int64_t N, int64_t D, int64_t group,
@@ -17,6 +27,7 @@ hipError_t launch(int dtype, int code, const void* x, void* codes, float* scales
     a.scales = scales;
     // group 0 (the way back only): one scale for a row, every unit of which then has the group number 0
     a.lanes_log2 = group == 0 ? 31 : group_lanes_log2(group);
+    a.keep = keep_codes(N, D, 0, 4000000);
     const int64_t units = D / kUnit;
     a.total = N * units;
     if (group != 0 && D % group == 0) {
@@ -28,17 +39,26 @@ hipError_t launch(int dtype, int code, const void* x, void* codes, float* scales
     }
     a.per_row = (a.units + kWave - 1) / kWave;
     a.groups = group == 0 ? 1 : (a.units + (1 << a.lanes_log2) - 1) >> a.lanes_log2;
-    const int64_t steps = (a.rows * a.per_row + kPieces - 1) / kPieces;      // of a wave
+    const QuantShape sh = quant_shape(N * D * (dtype == 0 ? 2 : 4), dtype);
+    const int64_t steps = (a.rows * a.per_row + sh.pieces - 1) / sh.pieces;  // of a wave
     int64_t blocks = (steps + kQuantWaves - 1) / kQuantWaves;
-    if (blocks > kNumCU * kBlocksPerCu) blocks = kNumCU * kBlocksPerCu;
-    const int64_t stride = blocks * kQuantWaves * kPieces;                   // pieces
+    if (blocks > int64_t(kNumCU) * sh.per_cu) blocks = int64_t(kNumCU) * sh.per_cu;
+    const int64_t stride = blocks * kQuantWaves * sh.pieces;                 // pieces
     a.row_step = stride / a.per_row;
     a.piece_step = static_cast<int32_t>(stride % a.per_row);
     const dim3 grid(static_cast<unsigned>(blocks)), block(kQuantWaves * kWave);
-    if (dtype == 0 && code == 0) hipLaunchKernelGGL((quant_kernel<bf16_io, int8_code, kPieces, BACK>), grid, block, 0, st, a);
-    else if (dtype == 0) hipLaunchKernelGGL((quant_kernel<bf16_io, e4m3_code, kPieces, BACK>), grid, block, 0, st, a);
-    else if (code == 0) hipLaunchKernelGGL((quant_kernel<f32_io, int8_code, kPieces, BACK>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((quant_kernel<f32_io, e4m3_code, kPieces, BACK>), grid, block, 0, st, a);
+    const auto run = [&](auto io, auto cd, auto pieces) {
+        hipLaunchKernelGGL((quant_kernel<decltype(io), decltype(cd), pieces, BACK>), grid, block, 0, st, a);
+    };
+    const auto coded = [&](auto io, auto pieces) {
+        if (code == 0) run(io, int8_code{}, pieces);
+        else run(io, e4m3_code{}, pieces);
+    };
+    using std::integral_constant;
+    if (dtype != 0) coded(f32_io{}, integral_constant<int, 1>{});
+    else if (sh.pieces == 1) coded(bf16_io{}, integral_constant<int, 1>{});
+    else if (sh.pieces == 2) coded(bf16_io{}, integral_constant<int, 2>{});
+    else coded(bf16_io{}, integral_constant<int, 4>{});
     return hipGetLastError();
 }
 

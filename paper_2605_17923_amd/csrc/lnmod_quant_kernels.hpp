@@ -21,6 +21,7 @@ struct QuantArgs {
     int32_t per_row;         // pieces of a row
     int32_t groups;          // of a row
     int32_t lanes_log2;      // of a group
+    int32_t keep;            // see keep_codes
     int64_t row_step;        // rows and pieces that lie between two steps of a wave
     int32_t piece_step;
 };
@@ -117,7 +118,7 @@ __global__ __launch_bounds__(kQuantWaves* kWave) void quant_kernel(const QuantAr
             } else {
                 const Scale sc = scale_of<C>(group_max(Unit<Tag>::amax_bits(now.x[i]), a.lanes_log2));
                 Unit<Tag>::unpack(now.x[i], v);
-                store_codes(row_of(a.codes, at * 8, n * 8), lane, encode<C>(v, sc));
+                store_codes(row_of(a.codes, at * 8, n * 8), lane, encode<C>(v, sc), a.keep);
                 const uint32_t u = static_cast<uint32_t>(cur.col[i]) * kWave + lane;
                 const bool leads = lane < n && (lane & ((1u << a.lanes_log2) - 1u)) == 0;
                 store_float(scales_at(cur, i), leads ? (u >> a.lanes_log2) * 4u : kNowhere, sc.s);

@@ -1,49 +1,12 @@
 // lnmod_rmsq.hip -- instantiation and launch of the root-mean-square norm with the residual's addition and an output in
 // 8 bits, and of its backward.
-#include "lnmod_launch.hpp"
+#include "lnmod_code_shapes.hpp"
 #include "lnmod_rmsq_kernels.hpp"
 
 namespace lnmod {
 namespace {
 
-// Two units per lane, as many waves as the row then needs.
-Shape rmsq_shape(int units, int dtype) {
-    Shape sh{1, 1, dtype == 0 ? 2 : 1, 8};
-    if (units > kWave) {
-        sh.VPL = 2;
-        sh.K = (units + 2 * kWave - 1) / (2 * kWave);
-        if (sh.K == 7) sh.K = 8;
-        sh.per_cu = sh.K <= 1 ? 8 : sh.K == 2 ? 4 : sh.K <= 4 ? 2 : 1;
-    }
-    return sh;
-}
-
-Shape rmsq_fwd_shape(int units, int dtype, int64_t) { return rmsq_shape(units, dtype); }
-Shape rmsq_bwd_shape(int units, int dtype) { return rmsq_shape(units, dtype); }
-
 int64_t blocks_for(int64_t N, const Shape& sh) { return grid_blocks(N, static_cast<int64_t>(kNumCU) * sh.per_cu, sh.R); }
-
-// f(VPL, K, R) as constants; false for a shape that is not compiled
-template <typename F>
-bool for_shape(const Shape& sh, F&& f) {
-    using std::integral_constant;
-    const auto rows = [&](auto vpl, auto k) {
-        if (sh.R == 1) f(vpl, k, integral_constant<int, 1>{});
-        else f(vpl, k, integral_constant<int, 2>{});
-        return true;
-    };
-    switch (sh.VPL * 100 + sh.K) {
-        case 101: return rows(integral_constant<int, 1>{}, integral_constant<int, 1>{});
-        case 201: return rows(integral_constant<int, 2>{}, integral_constant<int, 1>{});
-        case 202: return rows(integral_constant<int, 2>{}, integral_constant<int, 2>{});
-        case 203: return rows(integral_constant<int, 2>{}, integral_constant<int, 3>{});
-        case 204: return rows(integral_constant<int, 2>{}, integral_constant<int, 4>{});
-        case 205: return rows(integral_constant<int, 2>{}, integral_constant<int, 5>{});
-        case 206: return rows(integral_constant<int, 2>{}, integral_constant<int, 6>{});
-        case 208: return rows(integral_constant<int, 2>{}, integral_constant<int, 8>{});
-        default: return false;
-    }
-}
 
 }  // namespace
 
@@ -63,14 +26,15 @@ hipError_t launch_rmsq_fwd(int dtype, int code, const void* x, const void* r, co
     a.nchunks = static_cast<int32_t>(D / kUnit);
     a.lanes_log2 = group == 0 ? 0 : group_lanes_log2(group);
     a.groups = group == 0 ? 1 : static_cast<int32_t>((D + group - 1) / group);
+    a.keep = keep_codes(N, D, 0, r ? 70000000 : 4000000);
     a.eps = eps;
     a.inv_D = 1.0f / static_cast<float>(D);
-    const Shape sh = pick_shape(force, rmsq_fwd_shape(a.nchunks, dtype, N));
+    const Shape sh = pick_shape(force, rms_fwd_shape(N, a.nchunks, dtype));
     if (!covers(sh, a.nchunks)) return hipErrorInvalidConfiguration;
     a.nb = static_cast<int32_t>(blocks_for(N, sh));
     const dim3 grid(static_cast<unsigned>(a.nb)), block(sh.K * kWave);
     const auto run = [&](auto io, auto cd) {
-        return for_shape(sh, [&](auto vpl, auto k, auto rows) {
+        const auto shaped = [&](auto vpl, auto k, auto rows) {
             const auto go = [&](auto res, auto row, auto val) {
                 hipLaunchKernelGGL((rmsq_fwd_kernel<decltype(io), decltype(cd), vpl, k, rows, res, row, val>), grid, block, 0, st, a);
             };
@@ -84,7 +48,9 @@ hipError_t launch_rmsq_fwd(int dtype, int code, const void* x, const void* r, co
             };
             if (r) res(std::true_type{});
             else res(std::false_type{});
-        });
+        };
+        if constexpr (std::is_same<decltype(io), bf16_io>::value) return ShapesOf<kRmsFwd200, kRmsFwdLong>::call(sh, shaped);
+        else return ShapesOf<kSplit, kRmsFwd32>::call(sh, shaped);
     };
     bool ok;
     if (dtype == 0) ok = code == 0 ? run(bf16_io{}, int8_code{}) : run(bf16_io{}, e4m3_code{});
@@ -93,7 +59,7 @@ hipError_t launch_rmsq_fwd(int dtype, int code, const void* x, const void* r, co
 }
 
 int64_t rmsq_bwd_blocks(int64_t N, int64_t D, int dtype) {
-    return N <= 0 ? 0 : blocks_for(N, rmsq_bwd_shape(static_cast<int>(D / kUnit), dtype));
+    return N <= 0 ? 0 : blocks_for(N, rms_bwd_shape(N, static_cast<int>(D / kUnit), dtype));
 }
 
 hipError_t launch_rmsq_bwd(int dtype, const void* dy, const void* dh, const void* h, const void* w, int64_t N, int64_t D,
@@ -110,16 +76,18 @@ hipError_t launch_rmsq_bwd(int dtype, const void* dy, const void* dh, const void
     a.D = static_cast<int32_t>(D);
     a.nchunks = static_cast<int32_t>(D / kUnit);
     a.inv_D = 1.0f / static_cast<float>(D);
-    const Shape sh = pick_shape(force, rmsq_bwd_shape(a.nchunks, dtype));
+    const Shape sh = pick_shape(force, rms_bwd_shape(N, a.nchunks, dtype));
     if (!covers(sh, a.nchunks)) return hipErrorInvalidConfiguration;
     a.nb = static_cast<int32_t>(blocks_for(N, sh));
     const dim3 grid(static_cast<unsigned>(a.nb)), block(sh.K * kWave);
     const auto run = [&](auto io) {
-        return for_shape(sh, [&](auto vpl, auto k, auto rows) {
+        const auto go = [&](auto vpl, auto k, auto rows) {
             using Tag = decltype(io);
             if (dh) hipLaunchKernelGGL((rmsq_bwd_kernel<Tag, vpl, k, rows, true>), grid, block, 0, st, a);
             else hipLaunchKernelGGL((rmsq_bwd_kernel<Tag, vpl, k, rows, false>), grid, block, 0, st, a);
-        });
+        };
+        if constexpr (std::is_same<decltype(io), bf16_io>::value) return ShapesOf<kRmsBwd50, kRmsBwdLong>::call(sh, go);
+        else return ShapesOf<kRmsBwd50x32, kRmsBwd32>::call(sh, go);
     };
     if (!(dtype == 0 ? run(bf16_io{}) : run(f32_io{}))) return hipErrorInvalidConfiguration;
     const hipError_t e = hipGetLastError();

@@ -32,6 +32,7 @@ struct RmsqFwdArgs {
     int32_t nchunks;         // units of a row
     int32_t groups;          // of a row
     int32_t lanes_log2;      // of a group; 0: the row is one
+    int32_t keep;            // see keep_codes
     float eps;
     float inv_D;
 };
@@ -203,7 +204,7 @@ void rmsq_fwd_kernel(const RmsqFwdArgs a) {
                         U::pack(v, o);
                         store_unit<Tag>(rout, chunk[i], o);
                     } else {
-                        store_codes(rout, chunk[i], w);
+                        store_codes(rout, chunk[i], w, a.keep);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
