@@ -36,7 +36,7 @@ int64_t fwd_clusters(int64_t nseg) {
 }  // namespace
 
 RowPlan ckpt_bwd_plan(int64_t T, int64_t nseg, int64_t D, int dtype, Shape* shape, const Shape* force) {
-    const Shape sh = pick_shape(force, ckpt_bwd_shape(T, static_cast<int>(D / kUnit), dtype));
+    const Shape sh = pick_shape(force, ckpt_bwd_shape(T, nseg, static_cast<int>(D / kUnit), dtype));
     if (shape) *shape = sh;
     // a row moves 2 D elements (dy, dx) and D codes, a slot 2 D floats that are written and read back
     const double row = 2.0 * (dtype == 0 ? 2.0 : 4.0) + 1.0;
@@ -60,7 +60,7 @@ hipError_t launch_ckpt_fwd(const Problem& p, bool token, const void* x, const vo
     a.f.eps = p.eps;
     a.f.inv_D = 1.0f / static_cast<float>(p.D);
     a.c = codes_of(p, c);
-    const Shape sh = pick_shape(p.force, ckpt_fwd_shape(p.T, a.f.nchunks, p.dtype));
+    const Shape sh = pick_shape(p.force, ckpt_fwd_shape(p.T, token ? 1 : p.nseg, a.f.nchunks, p.dtype));
     if (!covers(sh, a.f.nchunks)) return hipErrorInvalidConfiguration;
     const RowPlan pl = plan_rows_clusters(p.T, token ? 1 : p.nseg, static_cast<int64_t>(kNumCU) * sh.per_cu, sh.R,
                                           token ? 1 : fwd_clusters(p.nseg), sh.clusters);
@@ -77,7 +77,7 @@ hipError_t launch_ckpt_fwd(const Problem& p, bool token, const void* x, const vo
             else hipLaunchKernelGGL((ckpt_fwd_kernel<Tag, C, vpl, k, r, false>), grid, block, 0, st, a);
         };
         if constexpr (std::is_same<decltype(io), bf16_io>::value)
-            return ShapesOf<kSplit, kCkptFwd40, kCkptFwd200, kCkptFwdLong>::call(sh, go);
+            return ShapesOf<kSplit, kCkptFwd40, kCkptFwd200, kCkptFwdLong, kCkptFwdSegs>::call(sh, go);
         else
             return ShapesOf<kSplit, kCkptFwd32>::call(sh, go);
     });
@@ -118,7 +118,7 @@ hipError_t launch_ckpt_bwd(const Problem& p, bool token, const void* dy, const C
             if (token) hipLaunchKernelGGL((ckpt_bwd_kernel<Tag, C, vpl, k, r, true>), grid, block, 0, st, a);
             else hipLaunchKernelGGL((ckpt_bwd_kernel<Tag, C, vpl, k, r, false>), grid, block, 0, st, a);
         };
-        if constexpr (std::is_same<decltype(io), bf16_io>::value) return ShapesOf<kCkptBwd50, kCkptBwdLong>::call(sh, go);
+        if constexpr (std::is_same<decltype(io), bf16_io>::value) return ShapesOf<kCkptBwd50, kCkptBwdLong, kCkptBwdSegs>::call(sh, go);
         else return ShapesOf<kCkptBwd50x32, kCkptBwd32>::call(sh, go);
     });
     if (!ok) return hipErrorInvalidConfiguration;

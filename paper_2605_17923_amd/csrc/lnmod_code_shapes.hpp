@@ -50,6 +50,13 @@ inline constexpr ShapeTable kCkptFwd200 = {{
 inline constexpr ShapeTable kCkptFwdLong = {{
     {1, 1, 2, 128}, {1, 2, 2, 4}, {3, 1, 2, 128}, {4, 1, 2, 128}, {5, 1, 2, 64}, {3, 2, 2, 128}, {4, 2, 2, 128}, {4, 2, 2, 1},
     {3, 3, 2, 128}, {5, 2, 1, 64}, {4, 3, 2, 1}, {4, 3, 1, 1}, {4, 4, 1, 64}, {4, 4, 1, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}}};
+// several samples or segments, x beyond 40 MB: a block of few rows meets few segments, so two rows and as many blocks as they
+// give (24 segments, 39 062 x 5120: 211 us with the entry above, 175; 96 segments 236 and 175)
+inline constexpr ShapeTable kCkptFwdSegs = [] {
+    ShapeTable t = with(kSplit, 2, 128);
+    t[9] = {4, 3, 2, 128};
+    return t;
+}();
 inline constexpr ShapeTable kCkptFwd32 = {{
     {1, 1, 2, 8}, {1, 2, 2, 4}, {3, 1, 2, 3}, {4, 1, 2, 2}, {3, 2, 1, 2}, {3, 2, 1, 2}, {4, 2, 1, 2}, {4, 2, 1, 2},
     {3, 3, 1, 2}, {5, 2, 1, 1}, {4, 3, 1, 1}, {4, 3, 1, 1}, {4, 4, 1, 1}, {8, 2, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}}};
@@ -66,40 +73,47 @@ inline constexpr ShapeTable kCkptBwd50 = {{
     {1, 1, 2, 4}, {1, 2, 2, 3}, {3, 1, 2, 1}, {4, 1, 2, 1}, {5, 1, 2, 1}, {3, 2, 2, 1}, {4, 2, 2, 1}, {4, 2, 2, 1},
     {3, 3, 2, 1}, {10, 1, 2, 1}, {12, 1, 2, 1}, {12, 1, 2, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}}};
 inline constexpr ShapeTable kCkptBwdLong = {{
-    {1, 1, 2, 8}, {1, 2, 2, 4}, {1, 3, 2, 3}, {4, 1, 2, 2}, {5, 1, 2, 2}, {3, 2, 2, 2}, {4, 2, 2, 1}, {4, 2, 2, 1},
+    {1, 1, 2, 6}, {1, 2, 2, 4}, {3, 1, 2, 3}, {1, 4, 2, 3}, {5, 1, 2, 2}, {3, 2, 2, 2}, {4, 2, 2, 1}, {4, 2, 2, 1},
     {3, 3, 2, 1}, {4, 3, 2, 1}, {4, 3, 1, 1}, {4, 3, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}}};
+// several samples or segments: 97 656 x 2048 in 40 segments 219 us with the entry above, 203
+inline constexpr ShapeTable kCkptBwdSegs = [] {
+    ShapeTable t = kCkptBwdLong;
+    t[3] = {4, 1, 2, 2};
+    return t;
+}();
 inline constexpr ShapeTable kCkptBwd50x32 = {{
-    {1, 1, 2, 3}, {2, 1, 2, 2}, {3, 1, 2, 1}, {4, 1, 2, 1}, {3, 2, 2, 1}, {3, 2, 2, 1}, {4, 2, 2, 1}, {4, 2, 2, 1},
+    {1, 1, 2, 3}, {3, 1, 2, 1}, {3, 1, 2, 1}, {4, 1, 2, 1}, {3, 2, 2, 1}, {3, 2, 2, 1}, {4, 2, 2, 1}, {4, 2, 2, 1},
     {3, 3, 2, 1}, {10, 1, 2, 1}, {12, 1, 2, 1}, {12, 1, 2, 1}, {8, 2, 1, 1}, {8, 2, 1, 1}, {8, 2, 1, 1}, {4, 4, 1, 1}}};
 inline constexpr ShapeTable kCkptBwd32 = {{
-    {1, 1, 2, 4}, {1, 2, 2, 3}, {3, 1, 2, 1}, {4, 1, 2, 1}, {3, 2, 2, 1}, {3, 2, 2, 1}, {4, 2, 2, 1}, {4, 2, 2, 1},
+    {1, 1, 2, 4}, {1, 2, 2, 3}, {5, 1, 2, 1}, {4, 1, 2, 1}, {3, 2, 2, 1}, {3, 2, 2, 1}, {4, 2, 2, 1}, {4, 2, 2, 1},
     {3, 3, 2, 1}, {4, 3, 1, 1}, {4, 3, 1, 1}, {4, 3, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}}};
 
 // Root-mean-square norm, backward
 inline constexpr ShapeTable kRmsBwd50 = {{
-    {1, 1, 2, 3}, {2, 1, 2, 2}, {3, 1, 2, 1}, {4, 1, 2, 1}, {5, 1, 1, 1}, {3, 2, 1, 1}, {4, 2, 1, 1}, {4, 2, 2, 1},
-    {3, 3, 2, 1}, {10, 1, 2, 1}, {12, 1, 2, 1}, {12, 1, 2, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}}};
+    {1, 1, 2, 3}, {2, 1, 2, 2}, {3, 1, 2, 1}, {4, 1, 2, 1}, {5, 1, 1, 1}, {6, 1, 1, 1}, {4, 2, 1, 1}, {8, 1, 2, 1},
+    {10, 1, 2, 1}, {10, 1, 2, 1}, {12, 1, 2, 1}, {12, 1, 2, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}}};
 inline constexpr ShapeTable kRmsBwdLong = {{
-    {1, 1, 1, 8}, {1, 2, 1, 3}, {3, 1, 2, 1}, {4, 1, 2, 1}, {5, 1, 1, 1}, {3, 2, 1, 1}, {4, 2, 1, 1}, {8, 1, 2, 1},
+    {1, 1, 1, 8}, {2, 1, 1, 3}, {3, 1, 2, 1}, {4, 1, 2, 1}, {5, 1, 1, 1}, {3, 2, 1, 1}, {3, 3, 1, 1}, {8, 1, 2, 1},
     {3, 3, 2, 1}, {10, 1, 1, 1}, {12, 1, 1, 1}, {12, 1, 1, 1}, {8, 2, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {8, 2, 1, 1}}};
 inline constexpr ShapeTable kRmsBwd50x32 = {{
-    {1, 1, 2, 3}, {2, 1, 1, 2}, {3, 1, 1, 1}, {4, 1, 1, 1}, {5, 1, 2, 1}, {3, 2, 1, 1}, {4, 2, 1, 1}, {4, 2, 1, 1},
+    {1, 1, 2, 3}, {3, 1, 1, 1}, {3, 1, 1, 1}, {4, 1, 1, 1}, {5, 1, 2, 1}, {3, 2, 1, 1}, {4, 2, 1, 1}, {4, 2, 1, 1},
     {3, 3, 1, 1}, {10, 1, 1, 1}, {4, 3, 1, 1}, {4, 3, 1, 1}, {8, 2, 1, 1}, {8, 2, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}}};
 inline constexpr ShapeTable kRmsBwd32 = {{
-    {1, 1, 2, 3}, {1, 2, 2, 3}, {3, 1, 2, 1}, {4, 1, 2, 1}, {3, 2, 2, 1}, {3, 2, 2, 1}, {4, 2, 2, 1}, {4, 2, 2, 1},
+    {1, 1, 2, 3}, {3, 1, 2, 1}, {3, 1, 2, 1}, {4, 1, 2, 1}, {3, 2, 2, 1}, {3, 2, 2, 1}, {4, 2, 2, 1}, {4, 2, 2, 1},
     {3, 3, 2, 1}, {4, 3, 2, 1}, {4, 3, 1, 1}, {4, 3, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}}};
 
 static_assert(covers_all(kSplit) && covers_all(kCkptFwd40) && covers_all(kCkptFwd200) && covers_all(kCkptFwdLong) &&
-              covers_all(kCkptFwd32) && covers_all(kRmsFwd32) && covers_all(kCkptBwd50) && covers_all(kCkptBwdLong) &&
+              covers_all(kCkptFwd32) && covers_all(kCkptFwdSegs) && covers_all(kRmsFwd32) && covers_all(kCkptBwd50) && covers_all(kCkptBwdLong) && covers_all(kCkptBwdSegs) &&
               covers_all(kCkptBwd50x32) && covers_all(kCkptBwd32) && covers_all(kRmsBwd50) && covers_all(kRmsBwdLong) &&
               covers_all(kRmsBwd50x32) && covers_all(kRmsBwd32), "an entry that does not cover its rows");
 
 inline const Shape& entry(const ShapeTable& t, int units) { return t[(units - 1) / 64]; }
 
-inline Shape ckpt_fwd_shape(int64_t T, int units, int dtype) {
+inline Shape ckpt_fwd_shape(int64_t T, int64_t nseg, int units, int dtype) {
     const int64_t bytes = T * units * (dtype == 0 ? 16 : 32);
     if (bytes <= 10000000) return entry(kSplit, units);
     if (dtype != 0) return entry(kCkptFwd32, units);
+    if (nseg > 1 && bytes > 40000000) return entry(kCkptFwdSegs, units);
     return entry(bytes <= 40000000 ? kCkptFwd40 : bytes <= 200000000 ? kCkptFwd200 : kCkptFwdLong, units);
 }
 inline Shape rms_fwd_shape(int64_t N, int units, int dtype) {
@@ -108,9 +122,9 @@ inline Shape rms_fwd_shape(int64_t N, int units, int dtype) {
     if (dtype != 0) return entry(kRmsFwd32, units);
     return entry(bytes <= 200000000 ? kRmsFwd200 : kRmsFwdLong, units);
 }
-inline Shape ckpt_bwd_shape(int64_t T, int units, int dtype) {
+inline Shape ckpt_bwd_shape(int64_t T, int64_t nseg, int units, int dtype) {
     const bool shorter = T * units * (dtype == 0 ? 16 : 32) <= 50000000;
-    if (dtype == 0) return entry(shorter ? kCkptBwd50 : kCkptBwdLong, units);
+    if (dtype == 0) return entry(shorter ? kCkptBwd50 : nseg > 1 ? kCkptBwdSegs : kCkptBwdLong, units);
     return entry(shorter ? kCkptBwd50x32 : kCkptBwd32, units);
 }
 inline Shape rms_bwd_shape(int64_t N, int units, int dtype) {

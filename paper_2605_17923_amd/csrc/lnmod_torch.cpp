@@ -16,6 +16,7 @@
 #include <torch/csrc/autograd/python_cpp_function.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/jit/frontend/tracer.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
 #include <c10/core/impl/LocalDispatchKeySet.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
@@ -296,6 +297,14 @@ struct QkNorm : public torch::autograd::Function<QkNorm> {
 };
 
 // ---- activations in 8 bits -------------------------------------------------------------------------------------
+// at::empty without the dispatcher (one token, four outputs: 7.2 -> 6.4 us on the host)
+Tensor fresh(at::IntArrayRef shape, at::ScalarType type, const Tensor& like) {
+    return at::detail::empty_cuda(shape, type, like.device(), std::nullopt);
+}
+Tensor fresh_like(const Tensor& t) { return fresh(t.sizes(), t.scalar_type(), t); }
+
+Tensor fresh_bytes(size_t bytes, const Tensor& like) { return fresh(static_cast<int64_t>(bytes < 16 ? 16 : bytes), at::kByte, like); }
+
 bool is_group(int64_t group) { return group == 32 || group == 64 || group == 128; }
 
 at::ScalarType type_of_code(int code) { return code == LNMOD_INT8 ? at::kChar : at::kFloat8_e4m3fn; }
@@ -321,8 +330,8 @@ int64_t rows_of(const Tensor& t) {
 
 variable_list quantize_call(const Tensor& x, int code, int64_t group) {
     if (!plain_first(x) || x.dim() < 1 || !is_group(group)) throw NotPlain();
-    Tensor codes = at::empty(x.sizes(), x.options().dtype(type_of_code(code)));
-    Tensor scales = at::empty(scales_shape(x.sizes(), group), f32_like(x));
+    Tensor codes = fresh(x.sizes(), type_of_code(code), x);
+    Tensor scales = fresh(scales_shape(x.sizes(), group), at::kFloat, x);
     if (lnmod_quantize(ptr(x), rows_of(x), x.size(-1), group, stream_of(x), out(codes), f32_out(scales), code_of(x), code) != LNMOD_OK)
         throw NotPlain();
     return {codes, scales};
@@ -333,7 +342,7 @@ variable_list dequantize_call(const Tensor& codes, const Tensor& scales, at::Sca
         !plain_codes(codes, codes.sizes(), codes.device()) || !(group == 0 || is_group(group)) ||
         !plain(scales, scales_shape(codes.sizes(), group), at::kFloat, codes.device()) || (type != at::kBFloat16 && type != at::kFloat))
         throw NotPlain();
-    Tensor x = at::empty(codes.sizes(), codes.options().dtype(type));
+    Tensor x = fresh(codes.sizes(), type, codes);
     if (lnmod_dequantize(ptr(codes), f32(scales), rows_of(codes), codes.size(-1), group, stream_of(codes), out(x), code_of(x),
                          code_of_codes(codes)) != LNMOD_OK)
         throw NotPlain();
@@ -347,9 +356,9 @@ variable_list ckpt_forward(const Tensor& x, const Tensor& shift, const Tensor& s
     bool token;
     if (!is_group(group) || !ln_shapes(x, scale, cu, &b, &token) || !plain(shift, scale.sizes(), x.scalar_type(), x.device()))
         throw NotPlain();
-    Tensor y = at::empty_like(x), codes = at::empty(x.sizes(), x.options().dtype(type_of_code(code)));
-    Tensor scales = at::empty(scales_shape(x.sizes(), group), f32_like(x));
-    Tensor mean = at::empty(x.sizes().slice(0, x.dim() - 1), f32_like(x)), rstd = at::empty_like(mean);
+    Tensor y = fresh_like(x), codes = fresh(x.sizes(), type_of_code(code), x);
+    Tensor scales = fresh(scales_shape(x.sizes(), group), at::kFloat, x);
+    Tensor mean = fresh(x.sizes().slice(0, x.dim() - 1), at::kFloat, x), rstd = fresh_like(mean);
     const int st = lnmod_forward_ckpt(ptr(x), ptr(shift), ptr(scale), cu_ptr(cu), b.n, b.s_or_t, b.D, static_cast<float>(eps),
                                       group, stream_of(x), out(y), out(codes), f32_out(scales), f32_out(mean), f32_out(rstd),
                                       code_of(x), token ? LNMOD_PER_TOKEN : LNMOD_PER_SAMPLE, code);
@@ -378,8 +387,8 @@ struct LnModulateCkpt : public torch::autograd::Function<LnModulateCkpt> {
             plain(scales, scales_shape(dy.sizes(), group), at::kFloat, dy.device()) &&
             plain(mean, dy.sizes().slice(0, dy.dim() - 1), at::kFloat, dy.device()) &&
             plain(rstd, mean.sizes(), at::kFloat, dy.device())) {
-            Tensor dx = at::empty_like(dy), dshift = at::empty_like(scale), dscale = at::empty_like(scale), ws;
-            if (!token) ws = scratch(lnmod_backward_ckpt_workspace_bytes(b.n, b.T, b.D), dy);
+            Tensor dx = fresh_like(dy), dshift = fresh_like(scale), dscale = fresh_like(scale), ws;
+            if (!token) ws = fresh_bytes(lnmod_backward_ckpt_workspace_bytes(b.n, b.T, b.D), dy);
             const int st = lnmod_backward_ckpt(ptr(dy), ptr(codes), f32(scales), ptr(scale), cu_ptr(cu), b.n, b.s_or_t, b.D,
                                                group, stream_of(dy), f32(mean), f32(rstd), out(dx), out(dshift), out(dscale),
                                                token ? nullptr : out(ws), token ? 0 : static_cast<size_t>(ws.numel()),
@@ -408,13 +417,13 @@ variable_list rms_forward(const Tensor& x, const Tensor& w, const Tensor& residu
     if (!(group == 0 || is_group(group)) || !rms_shapes(x, w, residual, &N, &D)) throw NotPlain();
     Tensor codes, scales, y, h;
     if (values) {
-        y = at::empty_like(x);
+        y = fresh_like(x);
     } else {
-        codes = at::empty(x.sizes(), x.options().dtype(type_of_code(code)));
-        scales = at::empty(scales_shape(x.sizes(), group), f32_like(x));
+        codes = fresh(x.sizes(), type_of_code(code), x);
+        scales = fresh(scales_shape(x.sizes(), group), at::kFloat, x);
     }
-    if (residual.defined()) h = at::empty_like(x);
-    Tensor rstd = at::empty({N}, f32_like(x));
+    if (residual.defined()) h = fresh_like(x);
+    Tensor rstd = fresh(N, at::kFloat, x);
     const int st = lnmod_rmsnorm_quant_forward(ptr(x), ptr(residual), ptr(w), N, D, static_cast<float>(eps), group,
                                                stream_of(x), h.defined() ? out(h) : nullptr, values ? nullptr : out(codes),
                                                values ? nullptr : f32_out(scales), values ? out(y) : nullptr, f32_out(rstd),
@@ -430,8 +439,8 @@ variable_list rms_backward(const Tensor& dy, const Tensor& h, const Tensor& w, c
     if (!rms_shapes(h, w, dh, &N, &D) || !plain(dy, h.sizes(), h.scalar_type(), h.device()) ||
         !plain(rstd, at::IntArrayRef(&N, 1), at::kFloat, h.device()))
         return {};
-    Tensor dx = at::empty_like(h), dw = at::empty({D}, io_grads ? h.options() : f32_like(h));
-    const Tensor ws = scratch(lnmod_rmsnorm_quant_backward_workspace_bytes(N, D), h);
+    Tensor dx = fresh_like(h), dw = fresh(D, io_grads ? h.scalar_type() : at::kFloat, h);
+    const Tensor ws = fresh_bytes(lnmod_rmsnorm_quant_backward_workspace_bytes(N, D), h);
     const int st = lnmod_rmsnorm_quant_backward(ptr(dy), ptr(dh), ptr(h), ptr(w), N, D, stream_of(h), f32(rstd), out(dx), out(dw),
                                                 out(ws), static_cast<size_t>(ws.numel()), code_of(h), io_grads);
     return st == LNMOD_OK ? variable_list{dx, dw} : variable_list{};
