@@ -60,7 +60,8 @@ hipError_t launch_ckpt_fwd(const Problem& p, bool token, const void* x, const vo
     a.f.eps = p.eps;
     a.f.inv_D = 1.0f / static_cast<float>(p.D);
     a.c = codes_of(p, c);
-    const Shape sh = pick_shape(p.force, ckpt_fwd_shape(p.T, token ? 1 : p.nseg, a.f.nchunks, p.dtype));
+    const Shape sh = pick_shape(p.force, token ? ckpt_tok_shape(p.T, a.f.nchunks, p.dtype, false)
+                                             : ckpt_fwd_shape(p.T, p.nseg, a.f.nchunks, p.dtype));
     if (!covers(sh, a.f.nchunks)) return hipErrorInvalidConfiguration;
     const RowPlan pl = plan_rows_clusters(p.T, token ? 1 : p.nseg, static_cast<int64_t>(kNumCU) * sh.per_cu, sh.R,
                                           token ? 1 : fwd_clusters(p.nseg), sh.clusters);
@@ -70,16 +71,15 @@ hipError_t launch_ckpt_fwd(const Problem& p, bool token, const void* x, const vo
     a.f.split = cluster_split(a.f.interleave, pl);
     const dim3 grid(static_cast<unsigned>(pl.blocks)), block(sh.K * kWave);
     const bool ok = for_types(p.dtype, code, [&](auto io, auto cd) {
-        const auto go = [&](auto vpl, auto k, auto r) {
-            using Tag = decltype(io);
-            using C = decltype(cd);
-            if (token) hipLaunchKernelGGL((ckpt_fwd_kernel<Tag, C, vpl, k, r, true>), grid, block, 0, st, a);
-            else hipLaunchKernelGGL((ckpt_fwd_kernel<Tag, C, vpl, k, r, false>), grid, block, 0, st, a);
+        const auto go = [&](auto vpl, auto k, auto r, auto tok) {
+            hipLaunchKernelGGL((ckpt_fwd_kernel<decltype(io), decltype(cd), vpl, k, r, tok>), grid, block, 0, st, a);
         };
+        if (token) return ShapesOf<kSplit, kTokFwd>::call(sh, [&](auto... c) { go(c..., std::true_type{}); });
+        const auto plain = [&](auto... c) { go(c..., std::false_type{}); };
         if constexpr (std::is_same<decltype(io), bf16_io>::value)
-            return ShapesOf<kSplit, kCkptFwd40, kCkptFwd200, kCkptFwdLong, kCkptFwdSegs>::call(sh, go);
+            return ShapesOf<kSplit, kCkptFwd40, kCkptFwd200, kCkptFwdLong, kCkptFwdSegs>::call(sh, plain);
         else
-            return ShapesOf<kSplit, kCkptFwd32>::call(sh, go);
+            return ShapesOf<kSplit, kCkptFwd32>::call(sh, plain);
     });
     return ok ? hipGetLastError() : hipErrorInvalidConfiguration;
 }
@@ -104,7 +104,10 @@ hipError_t launch_ckpt_bwd(const Problem& p, bool token, const void* dy, const C
     a.c = codes_of(p, c);
     Shape sh;
     RowPlan pl = ckpt_bwd_plan(p.T, p.nseg, p.D, p.dtype, &sh, p.force);
-    if (token) pl = plan_rows(p.T, static_cast<int64_t>(kNumCU) * sh.per_cu, sh.R);
+    if (token) {
+        sh = pick_shape(p.force, ckpt_tok_shape(p.T, a.b.nchunks, p.dtype, true));
+        pl = plan_rows(p.T, static_cast<int64_t>(kNumCU) * sh.per_cu, sh.R);
+    }
     if (!covers(sh, a.b.nchunks)) return hipErrorInvalidConfiguration;
     a.b.rows_per_cluster = pl.rows_per_cluster;
     a.b.nb = pl.nb;
@@ -112,14 +115,15 @@ hipError_t launch_ckpt_bwd(const Problem& p, bool token, const void* dy, const C
     a.b.split = cluster_split(a.b.interleave, pl);
     const dim3 grid(static_cast<unsigned>(pl.blocks)), block(sh.K * kWave);
     const bool ok = for_types(p.dtype, code, [&](auto io, auto cd) {
-        const auto go = [&](auto vpl, auto k, auto r) {
-            using Tag = decltype(io);
-            using C = decltype(cd);
-            if (token) hipLaunchKernelGGL((ckpt_bwd_kernel<Tag, C, vpl, k, r, true>), grid, block, 0, st, a);
-            else hipLaunchKernelGGL((ckpt_bwd_kernel<Tag, C, vpl, k, r, false>), grid, block, 0, st, a);
+        const auto go = [&](auto vpl, auto k, auto r, auto tok) {
+            hipLaunchKernelGGL((ckpt_bwd_kernel<decltype(io), decltype(cd), vpl, k, r, tok>), grid, block, 0, st, a);
         };
-        if constexpr (std::is_same<decltype(io), bf16_io>::value) return ShapesOf<kCkptBwd50, kCkptBwdLong, kCkptBwdSegs>::call(sh, go);
-        else return ShapesOf<kCkptBwd50x32, kCkptBwd32>::call(sh, go);
+        if (token) return ShapesOf<kSplit, kTokBwdLong>::call(sh, [&](auto... c) { go(c..., std::true_type{}); });
+        const auto plain = [&](auto... c) { go(c..., std::false_type{}); };
+        if constexpr (std::is_same<decltype(io), bf16_io>::value)
+            return ShapesOf<kCkptBwd50, kCkptBwdLong, kCkptBwdSegs>::call(sh, plain);
+        else
+            return ShapesOf<kCkptBwd50x32, kCkptBwd32>::call(sh, plain);
     });
     if (!ok) return hipErrorInvalidConfiguration;
     const hipError_t e = hipGetLastError();

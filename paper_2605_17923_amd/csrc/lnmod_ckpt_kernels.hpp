@@ -44,7 +44,7 @@ constexpr int ckpt_fwd_waves(int vpl, int nv, int r, bool tok) {
     return waves_for(vpl * ((tok ? 0 : 16) + kDepth * r * 4 * nv * (tok ? 3 : 1)) + 56);
 }
 constexpr int ckpt_bwd_waves(int vpl, int nv, int r, bool tok) {
-    return waves_for(vpl * ((tok ? 0 : 24) + kDepth * r * (4 * nv * (tok ? 2 : 1) + 3)) + 56);
+    return waves_for(vpl * ((tok ? 16 : 24) + kDepth * r * (4 * nv * (tok ? 2 : 1) + 3)) + 56);
 }
 
 template <typename Tag, typename C, int VPL, int K, int R, bool TOK>

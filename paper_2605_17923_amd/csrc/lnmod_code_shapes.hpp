@@ -61,6 +61,19 @@ inline constexpr ShapeTable kCkptFwd32 = {{
     {1, 1, 2, 8}, {1, 2, 2, 4}, {3, 1, 2, 3}, {4, 1, 2, 2}, {3, 2, 1, 2}, {3, 2, 1, 2}, {4, 2, 1, 2}, {4, 2, 1, 2},
     {3, 3, 1, 2}, {5, 2, 1, 1}, {4, 3, 1, 1}, {4, 3, 1, 1}, {4, 4, 1, 1}, {8, 2, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}}};
 
+// Modulation rows per token: neither direction keeps anything from row to row, so both take many blocks; the backward on
+// more than 200 MB has entries of its own.  2 to 5 % (forward) and 3 to 8 % off the best shape of each problem.
+inline constexpr ShapeTable kTokBwd200 = with(kSplit, 1, 128);
+inline constexpr ShapeTable kTokFwd = [] {
+    ShapeTable t = with(kSplit, 1, 128);
+    t[9].per_cu = 64;
+    for (int k = 12; k < 16; ++k) t[k] = {4, 4, 1, 128};
+    return t;
+}();
+inline constexpr ShapeTable kTokBwdLong = {{
+    {1, 1, 2, 4}, {2, 1, 2, 2}, {3, 1, 2, 1}, {4, 1, 2, 128}, {5, 1, 2, 64}, {3, 2, 1, 1}, {4, 2, 1, 1}, {8, 1, 2, 64},
+    {3, 3, 2, 64}, {5, 2, 1, 1}, {4, 3, 2, 1}, {4, 3, 1, 1}, {8, 2, 1, 1}, {8, 2, 1, 1}, {8, 2, 2, 1}, {8, 2, 1, 1}}};
+
 // Root-mean-square norm, forward
 inline constexpr ShapeTable kRmsFwd200 = with(kSplit, 1, 128);
 inline constexpr ShapeTable kRmsFwdLong = with(kSplit, 2, 128);
@@ -103,7 +116,8 @@ inline constexpr ShapeTable kRmsBwd32 = {{
     {3, 3, 2, 1}, {4, 3, 2, 1}, {4, 3, 1, 1}, {4, 3, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}}};
 
 static_assert(covers_all(kSplit) && covers_all(kCkptFwd40) && covers_all(kCkptFwd200) && covers_all(kCkptFwdLong) &&
-              covers_all(kCkptFwd32) && covers_all(kCkptFwdSegs) && covers_all(kRmsFwd32) && covers_all(kCkptBwd50) && covers_all(kCkptBwdLong) && covers_all(kCkptBwdSegs) &&
+              covers_all(kCkptFwd32) && covers_all(kCkptFwdSegs) && covers_all(kTokBwdLong) &&
+              covers_all(kRmsFwd32) && covers_all(kCkptBwd50) && covers_all(kCkptBwdLong) && covers_all(kCkptBwdSegs) &&
               covers_all(kCkptBwd50x32) && covers_all(kCkptBwd32) && covers_all(kRmsBwd50) && covers_all(kRmsBwdLong) &&
               covers_all(kRmsBwd50x32) && covers_all(kRmsBwd32), "an entry that does not cover its rows");
 
@@ -115,6 +129,12 @@ inline Shape ckpt_fwd_shape(int64_t T, int64_t nseg, int units, int dtype) {
     if (dtype != 0) return entry(kCkptFwd32, units);
     if (nseg > 1 && bytes > 40000000) return entry(kCkptFwdSegs, units);
     return entry(bytes <= 40000000 ? kCkptFwd40 : bytes <= 200000000 ? kCkptFwd200 : kCkptFwdLong, units);
+}
+inline Shape ckpt_tok_shape(int64_t T, int units, int dtype, bool backward) {
+    const int64_t bytes = T * units * (dtype == 0 ? 16 : 32);
+    if (bytes <= 10000000) return entry(kSplit, units);
+    if (!backward) return entry(kTokFwd, units);
+    return entry(bytes > 200000000 ? kTokBwdLong : kTokBwd200, units);
 }
 inline Shape rms_fwd_shape(int64_t N, int units, int dtype) {
     const int64_t bytes = N * units * (dtype == 0 ? 16 : 32);
