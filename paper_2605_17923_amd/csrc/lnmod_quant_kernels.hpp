@@ -8,6 +8,7 @@
 // into pieces of its own, and the last one has idle lanes.
 #pragma once
 #include "lnmod_code.hpp"
+#include "lnmod_code_shapes.hpp"
 
 namespace lnmod {
 
@@ -25,8 +26,6 @@ struct QuantArgs {
     int64_t row_step;        // rows and pieces that lie between two steps of a wave
     int32_t piece_step;
 };
-
-constexpr int kQuantWaves = 4;
 
 // Where a wave is: V consecutive pieces from (row, piece) on.
 template <int V>
