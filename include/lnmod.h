@@ -35,7 +35,7 @@
  *       LNMOD_EINVAL        NULL required pointer; negative size; eps not finite or <= 0;
  *                           unknown dtype or mod; token count at or above 2^31; more than
  *                           2^24 - 1 samples or segments
- *       LNMOD_EUNSUPPORTED  D outside the supported set
+ *       LNMOD_EUNSUPPORTED  D outside the supported set, or a combination that a call excludes
  *       LNMOD_EALIGN        a tensor pointer is not 16-byte aligned
  *       LNMOD_EWORKSPACE    workspace NULL or smaller than lnmod_backward_workspace_bytes()
  *       LNMOD_ELAUNCH       the HIP runtime reported an error for the launch
@@ -323,7 +323,8 @@ size_t lnmod_backward_ckpt_workspace_bytes(int64_t B_or_nseg, int64_t total_toke
  * x, r, h: [N, D]; w: [D]; rstd: float32 [N] (written).  r and h are both NULL where there is no residual; h is x then.
  * Either codes and code_scales are given, and hold the codes of v, or y [N, D] in the I/O dtype, which holds the values that
  * those codes stand for (for training with the rounding in the loop); the other is NULL.  group 0: one scale for a whole
- * row, code_scales [N].  There the largest |v| is formed as rstd_n times the largest |h*w|.
+ * row, code_scales [N].  There the largest |v| is formed as rstd_n times the largest |h*w|, so a row where that product is
+ * beyond float32 counts as one that holds an infinity, and eps is at least 1e-20 (LNMOD_EUNSUPPORTED).
  *
  * Backward, straight through the rounding to codes; dh: gradient that reaches h along the residual stream, or NULL:
  *

@@ -433,7 +433,7 @@ int lnmod_rmsnorm_quant_forward(const void* x, const void* r, const void* w, int
     if ((group != 0 && !valid_group(group)) || !valid_code(code)) return LNMOD_EINVAL;
     const int st = check_shape(1, N, D, eps, dtype, N);
     if (st != LNMOD_OK) return st;
-    if (D % 8 != 0) return LNMOD_EUNSUPPORTED;
+    if (D % 8 != 0 || (group == 0 && eps < 1e-20f)) return LNMOD_EUNSUPPORTED;
     if (N == 0) return LNMOD_OK;
     if (!x || !w || !rstd || (r == nullptr) != (h == nullptr)) return LNMOD_EINVAL;
     if ((codes == nullptr) == (y == nullptr) || (codes == nullptr) != (code_scales == nullptr)) return LNMOD_EINVAL;

@@ -11,7 +11,9 @@
 //
 // With a scale for the whole row, its largest |v| is rstd times the largest |h*w|, so one barrier carries both the sum of
 // squares and the maximum; the maximum then differs from the largest |v| by two roundings at most, and a code whose v*r comes
-// out at Q (1 + 2^-21) still rounds to Q.  A group's maximum is that of v itself, as it is coded.  Layout and pipeline are those
+// out at Q (1 + 2^-21) still rounds to Q.  (eps >= 1e-20 keeps 16 bits of an |h*w| whose v is above the floor of 2^-100; the
+// maximum of v itself in a second pass, for rows whose |h*w| leaves the normal numbers, cost registers that every row
+// pays for.)  A group's maximum is that of v itself, as it is coded.  Layout and pipeline are those
 // of lnmod_ckpt_kernels.hpp.
 #pragma once
 #include "lnmod_code.hpp"

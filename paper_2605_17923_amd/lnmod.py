@@ -928,7 +928,7 @@ def _rms_args(x, w, **like_x):
 
 def rmsnorm_quant_forward(x, w, residual=None, eps=1e-6, code="e4m3", group=0, stream=None):
     """h = x + residual (x itself without one), then the codes of h * rsqrt(mean(h^2) + eps) * w, [..., D], with one scale
-    for each `group` features (32, 64, 128) or for a row (0) -> codes, scales, h, rstd (float32, one per row)."""
+    for each `group` features (32, 64, 128) or for a row (0; eps at least 1e-20) -> codes, scales, h, rstd (float32, one per row)."""
     host = _host(x, stream, eps)
     r = None if host is None else host.rmsnorm_quant_forward(x, w, residual, eps, code, group)
     if r is not None:

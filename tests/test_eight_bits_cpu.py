@@ -180,3 +180,8 @@ def test_rmsnorm_quant_wrapper_rejections():
     rejects(lnmod.rmsnorm_quant_backward, x, x, w, r, t(5, 64, dtype=f32), match="dh must be")
     rejects(lnmod.rmsnorm_quant_backward, x, x, w, r, ws=torch.zeros(8, dtype=torch.uint8), match="bytes")
     rejects(lnmod.rmsnorm_quant_backward, x, x, w, r, match="GPU")
+
+
+def test_a_scale_for_a_row_needs_an_eps_that_bounds_rstd():
+    call = lambda eps, group: lnmod.lnmod_rmsnorm_quant_forward(A, None, A, 0, 64, eps, group, None, None, A, A, None, A, 0, 0)   # noqa: E731
+    assert call(1e-21, 0) == EUNS and call(1e-20, 0) == OK and call(1e-21, 32) == OK

@@ -335,6 +335,24 @@ def test_rms_rows(N, group, residual):
     run_rms(N, 1536, "bf16", "e4m3", group, residual)
 
 
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("D", [264, 5120])
+def test_rms_a_scale_for_rows_of_the_smallest_and_largest_products(D, code):
+    # h*w of 2^-132 is no normal number: 17 of its bits are left, and three roundings, so s and the quotients are within 1e-5 of
+    # the exact ones (and rstd's 1e-5 goes into s); the codes reach the largest one and stay there
+    x, w = make(7, 16, D, dtype="f32") * 2.0 ** -50, make(8, D, dtype="f32", mean=1.0, std=0.1) * 2.0 ** -82
+    codes, scales, _, _ = lnmod.rmsnorm_quant_forward(x, w, None, 1e-20, code, 0)
+    v64, _ = co.rms_forward(to_host64(x), to_host64(w), float(np.float32(1e-20)))
+    s, q = co.quotients(v64, code, 0)
+    assert (np.abs(to_host64(scales).reshape(s.shape) - s) <= 2.2e-5 * s).all()
+    got = to_host64(codes)
+    low, high = (co.round_code(np.clip(q * f, -co.LARGEST[code], co.LARGEST[code]), code) for f in (1 - 1e-5, 1 + 1e-5))
+    assert ((got >= np.minimum(low, high)) & (got <= np.maximum(low, high))).all()
+    # a product beyond float32 counts as an infinity
+    codes, scales, _, rstd = lnmod.rmsnorm_quant_forward(make(9, 3, D, dtype="f32") * 2.0 ** 56, w * 2.0 ** 162, None, 1e-6, code, 0)
+    assert scales.isnan().all() and not codes.float().any() and bool((rstd > 0).all())
+
+
 def test_rms_rows_with_values_that_are_no_numbers():
     x, w = acts(4, 6, 264), make(5, 264, mean=1.0, std=0.2)
     r = make(6, 6, 264)
