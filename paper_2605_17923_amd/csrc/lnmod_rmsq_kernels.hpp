@@ -15,6 +15,11 @@
 // maximum of v itself in a second pass, for rows whose |h*w| leaves the normal numbers, cost registers that every row
 // pays for.)  A group's maximum is that of v itself, as it is coded.  Layout and pipeline are those
 // of lnmod_ckpt_kernels.hpp.
+//
+// Bound by HBM (17.4 vector operations per feature forward).  Measured, bf16 with a residual:
+//   32 760 x 5120, codes, a scale for a row     forward 195 us, 6.0 TB/s
+//   32 760 x 1536, values, groups of 128        forward 66 us, 6.1 TB/s     backward 65 to 72 us, 5.6 to 6.2 TB/s (+ 5 us second pass)
+//   1 x 5120 2.3 us, 96 x 4096 3.2 us: a launch and one pass through the memory's latency
 #pragma once
 #include "lnmod_code.hpp"
 
