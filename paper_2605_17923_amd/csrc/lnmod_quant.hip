@@ -9,36 +9,36 @@ namespace {
 template <bool BACK>
 hipError_t launch(int dtype, int code, const void* x, void* codes, float* scales, int64_t N, int64_t D, int64_t group,
                   hipStream_t st) {
-    QuantArgs a;
+    QuantArgs a{};
     a.x = const_cast<void*>(x);
     a.codes = codes;
     a.scales = scales;
     // group 0 (the way back only): one scale for a row, every unit of which then has the group number 0
     a.lanes_log2 = group == 0 ? 31 : group_lanes_log2(group);
     a.keep = keep_codes(N, D, 0, 4000000);
-    const int64_t units = D / kUnit;
-    a.total = N * units;
-    if (group != 0 && D % group == 0) {
-        a.units = kWave;
-        a.rows = (a.total + kWave - 1) / kWave;
-    } else {
-        a.units = static_cast<int32_t>(units);
-        a.rows = N;
-    }
-    a.per_row = (a.units + kWave - 1) / kWave;
+    const bool pad = group == 0 || D % group != 0;
+    a.units = static_cast<int32_t>(D / kUnit);
+    a.total = N * a.units;
     a.groups = group == 0 ? 1 : (a.units + (1 << a.lanes_log2) - 1) >> a.lanes_log2;
+    a.slots = pad && !BACK ? a.groups << a.lanes_log2 : a.units;
+    const int64_t pieces = (N * a.slots + kWave - 1) / kWave;
+    a.rows = pad ? N : pieces;
+    a.rows_in_64 = kWave / a.slots;
+    a.left_in_64 = kWave % a.slots;
+    a.over_slots = (65536u + static_cast<uint32_t>(a.slots) - 1u) / static_cast<uint32_t>(a.slots);
     const QuantShape sh = quant_shape(N * D * (dtype == 0 ? 2 : 4), dtype);
-    const int64_t blocks = quant_blocks(a.rows * a.per_row, sh);
+    const int64_t blocks = quant_blocks(pieces, sh);
     const int64_t stride = blocks * kQuantWaves * sh.pieces;                 // pieces
-    a.row_step = stride / a.per_row;
-    a.piece_step = static_cast<int32_t>(stride % a.per_row);
+    a.row_step = pad ? stride * kWave / a.slots : stride;
+    a.slot_step = pad ? static_cast<int32_t>(stride * kWave % a.slots) : 0;
     const dim3 grid(static_cast<unsigned>(blocks)), block(kQuantWaves * kWave);
-    const auto run = [&](auto io, auto cd, auto pieces) {
-        hipLaunchKernelGGL((quant_kernel<decltype(io), decltype(cd), pieces, BACK>), grid, block, 0, st, a);
+    const auto run = [&](auto io, auto cd, auto v) {
+        if (pad) hipLaunchKernelGGL((quant_kernel<decltype(io), decltype(cd), v, BACK, true>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((quant_kernel<decltype(io), decltype(cd), v, BACK, false>), grid, block, 0, st, a);
     };
-    const auto coded = [&](auto io, auto pieces) {
-        if (code == 0) run(io, int8_code{}, pieces);
-        else run(io, e4m3_code{}, pieces);
+    const auto coded = [&](auto io, auto v) {
+        if (code == 0) run(io, int8_code{}, v);
+        else run(io, e4m3_code{}, v);
     };
     using std::integral_constant;
     if (dtype != 0) coded(f32_io{}, integral_constant<int, 1>{});

@@ -212,3 +212,30 @@ def test_two_streams_at_once():
         for out in got[k]:
             for a, b in zip(out, want[k]):
                 assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+# rows that end inside a group: several to a wave, or lengthened; the codes and scales are those of the rows with zeros behind
+# them, and codes of such rows stand for the same values.  Sizes of each launch rule (1, 2 and 4 pieces a wave).
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype,N,D,group", [("bf16", 70001, 8, 32), ("bf16", 4001, 24, 128), ("bf16", 300, 40, 32), ("bf16", 9000, 72, 64),
+                                             ("bf16", 130003, 72, 128), ("bf16", 50001, 200, 32), ("bf16", 20011, 504, 128),
+                                             ("bf16", 9001, 1000, 64), ("bf16", 800017, 200, 128), ("bf16", 33001, 5000, 128),
+                                             ("f32", 70001, 8, 64), ("f32", 50001, 200, 128), ("f32", 7001, 520, 32),
+                                             ("f32", 1025, 1432, 128), ("bf16", 3, 1 << 20, 128), ("bf16", 5, (1 << 20) - 8, 128)])
+def test_quantize_rows_that_end_inside_a_group(dtype, N, D, group, code):
+    g = torch.Generator(device="cuda").manual_seed(D + N)
+    x = (torch.randn(N, D, generator=g, device="cuda") * torch.rand(N, 1, generator=g, device="cuda") * 8).to(DT[dtype])
+    wide = -(-D // group) * group
+    padded = torch.zeros(N, wide, dtype=DT[dtype], device="cuda")
+    padded[:, :D] = x
+    codes, scales = lnmod.quantize(x, code, group)
+    want, wscales = lnmod.quantize(padded, code, group)
+    assert torch.equal(scales, wscales)
+    assert torch.equal(codes.view(torch.uint8), want.view(torch.uint8)[:, :D].contiguous())
+    assert torch.equal(lnmod.dequantize(codes, scales, DT[dtype], group),
+                       lnmod.dequantize(want, wscales, DT[dtype], group)[:, :D].contiguous())
+    # one scale for a row: the same values from groups that share it
+    row = torch.rand(N, generator=g, device="cuda") + 0.5
+    shared = row[:, None].expand(N, wscales.shape[1]).contiguous()
+    assert torch.equal(lnmod.dequantize(codes, row, DT[dtype], 0),
+                       lnmod.dequantize(want, shared, DT[dtype], group)[:, :D].contiguous())
