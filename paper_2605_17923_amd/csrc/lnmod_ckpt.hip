@@ -41,7 +41,7 @@ RowPlan ckpt_bwd_plan(int64_t T, int64_t nseg, int64_t D, int dtype, Shape* shap
     // a row moves 2 D elements (dy, dx) and D codes, a slot 2 D floats that are written and read back
     const double row = 2.0 * (dtype == 0 ? 2.0 : 4.0) + 1.0;
     const double stream_us = static_cast<double>(T) * static_cast<double>(D) * row / 5.8e6;
-    return plan_rows_slots(T, nseg, static_cast<int64_t>(kNumCU) * sh.per_cu, sh.R, stream_us, 16.0 / row, sh.clusters);
+    return plan_rows_slots(T, nseg, group_blocks_most(sh), sh.R * row_groups(T, sh), stream_us, 16.0 / row, sh.clusters);
 }
 
 hipError_t launch_ckpt_fwd(const Problem& p, bool token, const void* x, const void* shift, const void* scale, void* y,
@@ -113,10 +113,15 @@ hipError_t launch_ckpt_bwd(const Problem& p, bool token, const void* dy, const C
     a.b.nb = pl.nb;
     a.b.interleave = cluster_interleave(p.force, pl);
     a.b.split = cluster_split(a.b.interleave, pl);
-    const dim3 grid(static_cast<unsigned>(pl.blocks)), block(sh.K * kWave);
+    const int groups = token ? 1 : row_groups(p.T, sh);
+    bool fits = true;
+    const dim3 grid(static_cast<unsigned>(pl.blocks)), block(sh.K * groups * kWave);
     const bool ok = for_types(p.dtype, code, [&](auto io, auto cd) {
         const auto go = [&](auto vpl, auto k, auto r, auto tok) {
-            hipLaunchKernelGGL((ckpt_bwd_kernel<decltype(io), decltype(cd), vpl, k, r, tok>), grid, block, 0, st, a);
+            constexpr int waves = ckpt_bwd_waves(vpl, Unit<decltype(io)>::NV, r, tok);
+            const size_t lds = group_lds(groups, units_at_once(vpl, waves), 2);
+            fits = groups <= groups_most(k, waves);
+            if (fits) hipLaunchKernelGGL((ckpt_bwd_kernel<decltype(io), decltype(cd), vpl, k, r, tok>), grid, block, lds, st, a);
         };
         if (token) return ShapesOf<kSplit, kTokBwdLong>::call(sh, [&](auto... c) { go(c..., std::true_type{}); });
         const auto plain = [&](auto... c) { go(c..., std::false_type{}); };
@@ -125,7 +130,7 @@ hipError_t launch_ckpt_bwd(const Problem& p, bool token, const void* dy, const C
         else
             return ShapesOf<kCkptBwd50x32, kCkptBwd32>::call(sh, plain);
     });
-    if (!ok) return hipErrorInvalidConfiguration;
+    if (!ok || !fits) return hipErrorInvalidConfiguration;
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || token) return e;
 

@@ -260,7 +260,7 @@ void ckpt_fwd_kernel(const CkptFwdArgs args) {
 // three roundings leave at most 2^-23 (|x'| + |mean|) rstd, a 2^14-th of half a code's step where the group is not far from the
 // row's mean; x' - mean first would spare those and cost two operations more per feature.
 template <typename Tag, typename C, int VPL, int K, int R, bool TOK>
-__global__ __launch_bounds__(K* kWave)
+__global__ __launch_bounds__(K* kWave* (TOK ? 1 : groups_most(K, ckpt_bwd_waves(VPL, Unit<Tag>::NV, R, TOK))))
 LNMOD_OCCUPANCY(ckpt_bwd_waves(VPL, Unit<Tag>::NV, R, TOK))
 void ckpt_bwd_kernel(const CkptBwdArgs args) {
     using U = Unit<Tag>;
@@ -268,9 +268,12 @@ void ckpt_bwd_kernel(const CkptBwdArgs args) {
     const BwdArgs& a = args.b;
     const Codes& cd = args.c;
     __shared__ float part[2][R][K][2];
+    extern __shared__ f32x4 sums[];          // see add_groups
 
     const int lane = threadIdx.x & (kWave - 1);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int in_block = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = K > 1 ? in_block : 0;   // of the row
+    const int groups = K > 1 || TOK ? 1 : static_cast<int>(blockDim.x) >> 6, group = K > 1 || TOK ? 0 : in_block;
     const int64_t row_bytes = static_cast<int64_t>(a.D) * IO<Tag>::kBytes;
 
     const uint32_t unit_bytes = static_cast<uint32_t>(row_bytes);
@@ -282,7 +285,8 @@ void ckpt_bwd_kernel(const CkptBwdArgs args) {
         scale_off[i] = (chunk[i] >> cd.lanes_log2) * 4u;
     }
     const Place at = place_of(a.split, a.interleave);
-    const int64_t cluster = at.cluster, member = at.member;
+    const int64_t cluster = at.cluster, member = at.member * groups + group;
+    const int32_t members = a.nb * groups;
     int64_t r0 = cluster * a.rows_per_cluster;
     int64_t r1 = r0 + a.rows_per_cluster;
     if (r1 > a.T) r1 = a.T;
@@ -328,13 +332,14 @@ void ckpt_bwd_kernel(const CkptBwdArgs args) {
                 }
             }
         };
-        const int64_t step = static_cast<int64_t>(a.nb) * R;
-        const int64_t first = take_turn<R>(turn, r0, stop, member, a.nb);
+        const int64_t step = static_cast<int64_t>(members) * R;
+        const int64_t first = take_turn<R>(turn, r0, stop, member, members);
         Rows bufs[kDepth];
 #pragma unroll
         for (int d = 0; d < kDepth - 1; ++d) fetch(first + d * step, bufs[d]);
 
-        float A[TOK ? 1 : VPL][8], acc_s[TOK ? 1 : VPL][8], acc_c[TOK ? 1 : VPL][8];
+        float A[TOK ? 1 : VPL][8], acc[2][TOK ? 1 : VPL][8];
+        float(&acc_s)[TOK ? 1 : VPL][8] = acc[0], (&acc_c)[TOK ? 1 : VPL][8] = acc[1];
         if constexpr (!TOK) {
             const Row rsc = row_of(a.scale, m * row_bytes, unit_bytes);
 #pragma unroll
@@ -463,9 +468,11 @@ void ckpt_bwd_kernel(const CkptBwdArgs args) {
 
         if constexpr (!TOK) {
             // this block's partial sums for segment m (slots: see bwd_seg_kernel)
-            const int64_t slot = ((cluster + m) * a.nb + member) * 2 * a.D * 4;
-            const Row ps = row_of(a.ws, slot, static_cast<uint32_t>(a.D) * 4u);
-            const Row pc = row_of(a.ws, slot + static_cast<int64_t>(a.D) * 4, static_cast<uint32_t>(a.D) * 4u);
+            add_groups<units_at_once(VPL, ckpt_bwd_waves(VPL, NV, R, TOK))>(acc, group, groups, sums);
+            const int64_t slot = ((cluster + m) * a.nb + at.member) * 2 * a.D * 4;
+            const uint32_t bytes = group == 0 ? static_cast<uint32_t>(a.D) * 4u : 0u;
+            const Row ps = row_of(a.ws, slot, bytes);
+            const Row pc = row_of(a.ws, slot + static_cast<int64_t>(a.D) * 4, bytes);
 #pragma unroll
             for (int i = 0; i < VPL; ++i) {
                 store_sums8(ps, chunk[i], acc_s[i]);

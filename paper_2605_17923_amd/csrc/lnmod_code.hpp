@@ -116,6 +116,52 @@ __device__ inline void store_sums8(Row row, uint32_t chunk, const float (&v)[8])
         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, t), row, static_cast<int>(chunk * 32u + 16u * h), 0, 0);
     }
 }
+// ---- several rows in a block -----------------------------------------------------------------------------------------------
+// Where one wave holds a row, the waves of a block take rows of their own, and what they have summed meets in LDS at the end: a
+// slot of partial sums per block in place of one per wave, and blocks that the dispatcher spreads over the CUs evenly.  The
+// waves are added in their order.
+constexpr int groups_most(int k, int waves_per_simd) { return k > 1 ? 1 : 4 * waves_per_simd; }
+// units of a lane that meet at a time, so that LDS stays below the 64 KB that a block gets without asking
+constexpr int units_at_once(int vpl, int waves_per_simd) {
+    const int most = waves_per_simd == 1 ? 4 : waves_per_simd == 2 ? 2 : 1;
+    return vpl < most ? vpl : most;
+}
+constexpr size_t group_lds(int groups, int units, int sums) { return static_cast<size_t>(groups - 1) * units * sums * kWave * kUnit * 4; }
+
+// acc[..][i] of the waves beyond the first one are added to the first one's; every wave of the block calls it.
+template <int UNITS, int VPL, int SUMS>
+__device__ inline void add_groups(float (&acc)[SUMS][VPL][8], int group, int groups, f32x4* lds) {
+    if (groups == 1) return;
+    const int lane = threadIdx.x & (kWave - 1);
+    constexpr int kHalves = SUMS * UNITS * 2;
+#pragma unroll
+    for (int i0 = 0; i0 < VPL; i0 += UNITS) {
+        if (group > 0) {
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+                const int i = i0 + h / 2 % UNITS, e = h % 2 * 4;
+                if (i >= VPL) continue;
+                const float(&v)[8] = acc[h / (UNITS * 2)][i];
+                lds[((group - 1) * kHalves + h) * kWave + lane] = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+            }
+        }
+        __syncthreads();
+        if (group == 0) {
+            for (int g = 0; g < groups - 1; ++g) {
+#pragma unroll
+                for (int h = 0; h < kHalves; ++h) {
+                    const int i = i0 + h / 2 % UNITS;
+                    if (i >= VPL) continue;
+                    const f32x4 t = lds[(g * kHalves + h) * kWave + lane];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[h / (UNITS * 2)][i][h % 2 * 4 + e] += t[e];
+                }
+            }
+        }
+        __syncthreads();                                     // before the next sums
+    }
+}
+
 // A float that no kernel of the launch writes, at a uniform address: a scalar load (see table_at).
 typedef const float __attribute__((address_space(4))) * const_f32_ptr;
 __device__ inline float float_at(const float* p, int64_t i) { return ((const_f32_ptr)p)[i]; }

@@ -7,7 +7,10 @@
 // units of 512 features wherever that is possible, because every idle lane costs arithmetic, and the arithmetic of the
 // few waves that HBM likes best is what limits them; forwards, which keep nothing from row to row but the weights, win with
 // many more blocks than are resident (root-mean-square norm, 32 760 x 5120 bf16: 118 us with one block per CU, 80.5 with 64);
-// backwards keep a slot of partial sums per block and stay at the few blocks that are resident.
+// backwards keep a slot of partial sums per block and stay at what is resident.  Up to 2560 features (fp32: 1024) a backward's
+// row belongs to one wave and a block is several of those (K = 1; "blocks per CU" are its waves), which needs no barrier in
+// the loop, a slot per CU, and no luck with where the dispatcher puts blocks of one wave: checkpoint backward, 32 552 x 1536
+// bf16 57 us with three blocks of three waves per row, 51 with one of four; 130 208 x 1536 205 and 168; 78 125 x 2560 191 and 172.
 // The classes of x's size and what the entries lose against the best shape of each problem, in the mean and at worst:
 //   checkpoint forward   bf16 up to 10 MB 1.6 %, 5 %; 40 MB 2 %, 14 %; 200 MB 1 %, 6 %; beyond 1 %, 5 %;  fp32 1 to 3 %
 //   rms norm forward     bf16 1 to 3 %, 14 %;  fp32 2 to 4 %
@@ -83,19 +86,19 @@ inline constexpr ShapeTable kRmsFwd32 = {{
 
 // Backward from a checkpoint
 inline constexpr ShapeTable kCkptBwd50 = {{
-    {1, 1, 2, 4}, {1, 2, 2, 3}, {3, 1, 2, 1}, {4, 1, 2, 1}, {5, 1, 2, 1}, {3, 2, 2, 1}, {4, 2, 2, 1}, {4, 2, 2, 1},
+    {1, 1, 1, 12}, {1, 2, 2, 4}, {1, 3, 1, 4}, {1, 4, 1, 4}, {1, 5, 1, 3}, {3, 2, 2, 1}, {4, 2, 2, 1}, {4, 2, 2, 1},
     {3, 3, 2, 1}, {10, 1, 2, 1}, {12, 1, 2, 1}, {12, 1, 2, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}}};
 inline constexpr ShapeTable kCkptBwdLong = {{
-    {1, 1, 2, 6}, {1, 2, 2, 4}, {3, 1, 2, 3}, {1, 4, 2, 3}, {5, 1, 2, 2}, {3, 2, 2, 2}, {4, 2, 2, 1}, {4, 2, 2, 1},
+    {1, 1, 2, 12}, {1, 2, 2, 4}, {1, 3, 1, 4}, {1, 4, 2, 3}, {1, 5, 1, 4}, {1, 6, 1, 4}, {4, 2, 2, 1}, {4, 2, 2, 1},
     {3, 3, 2, 1}, {4, 3, 2, 1}, {4, 3, 1, 1}, {4, 3, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}}};
-// several samples or segments: 97 656 x 2048 in 40 segments 219 us with the entry above, 203
+// several samples or segments: 58 794 x 2048 in 40 of them, both passes, 250 us with {4, 1, 2, 2}, 231 (19 959 in 40 shorter ones 1 % more)
 inline constexpr ShapeTable kCkptBwdSegs = [] {
     ShapeTable t = kCkptBwdLong;
-    t[3] = {4, 1, 2, 2};
+    t[3] = {1, 4, 1, 4};
     return t;
 }();
 inline constexpr ShapeTable kCkptBwd50x32 = {{
-    {1, 1, 2, 3}, {3, 1, 2, 1}, {3, 1, 2, 1}, {4, 1, 2, 1}, {3, 2, 2, 1}, {3, 2, 2, 1}, {4, 2, 2, 1}, {4, 2, 2, 1},
+    {1, 1, 1, 8}, {1, 2, 1, 4}, {3, 1, 2, 1}, {4, 1, 2, 1}, {3, 2, 2, 1}, {3, 2, 2, 1}, {4, 2, 2, 1}, {4, 2, 2, 1},
     {3, 3, 2, 1}, {10, 1, 2, 1}, {12, 1, 2, 1}, {12, 1, 2, 1}, {8, 2, 1, 1}, {8, 2, 1, 1}, {8, 2, 1, 1}, {4, 4, 1, 1}}};
 inline constexpr ShapeTable kCkptBwd32 = {{
     {1, 1, 2, 4}, {1, 2, 2, 3}, {5, 1, 2, 1}, {4, 1, 2, 1}, {3, 2, 2, 1}, {3, 2, 2, 1}, {4, 2, 2, 1}, {4, 2, 2, 1},
@@ -103,21 +106,27 @@ inline constexpr ShapeTable kCkptBwd32 = {{
 
 // Root-mean-square norm, backward
 inline constexpr ShapeTable kRmsBwd50 = {{
-    {1, 1, 2, 3}, {2, 1, 2, 2}, {3, 1, 2, 1}, {4, 1, 2, 1}, {5, 1, 1, 1}, {6, 1, 1, 1}, {4, 2, 1, 1}, {8, 1, 2, 1},
+    {1, 1, 1, 12}, {1, 2, 1, 4}, {1, 3, 1, 3}, {4, 1, 2, 1}, {5, 1, 1, 1}, {6, 1, 1, 1}, {4, 2, 1, 1}, {8, 1, 2, 1},
     {10, 1, 2, 1}, {10, 1, 2, 1}, {12, 1, 2, 1}, {12, 1, 2, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}, {8, 2, 2, 1}}};
 inline constexpr ShapeTable kRmsBwdLong = {{
-    {1, 1, 1, 8}, {2, 1, 1, 3}, {3, 1, 2, 1}, {4, 1, 2, 1}, {5, 1, 1, 1}, {3, 2, 1, 1}, {3, 3, 1, 1}, {8, 1, 2, 1},
+    {1, 1, 2, 8}, {1, 2, 1, 4}, {3, 1, 2, 1}, {4, 1, 2, 1}, {1, 5, 1, 2}, {3, 2, 1, 1}, {3, 3, 1, 1}, {8, 1, 2, 1},
     {3, 3, 2, 1}, {10, 1, 1, 1}, {12, 1, 1, 1}, {12, 1, 1, 1}, {8, 2, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {8, 2, 1, 1}}};
+// without a gradient along the residual stream: 32 552 x 1536 60.2 us with the entry above, 54.7
+inline constexpr ShapeTable kRmsBwdLongAlone = [] {
+    ShapeTable t = kRmsBwdLong;
+    t[2] = {1, 3, 1, 3};
+    return t;
+}();
 inline constexpr ShapeTable kRmsBwd50x32 = {{
     {1, 1, 2, 3}, {3, 1, 1, 1}, {3, 1, 1, 1}, {4, 1, 1, 1}, {5, 1, 2, 1}, {3, 2, 1, 1}, {4, 2, 1, 1}, {4, 2, 1, 1},
     {3, 3, 1, 1}, {10, 1, 1, 1}, {4, 3, 1, 1}, {4, 3, 1, 1}, {8, 2, 1, 1}, {8, 2, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}}};
 inline constexpr ShapeTable kRmsBwd32 = {{
-    {1, 1, 2, 3}, {3, 1, 2, 1}, {3, 1, 2, 1}, {4, 1, 2, 1}, {3, 2, 2, 1}, {3, 2, 2, 1}, {4, 2, 2, 1}, {4, 2, 2, 1},
+    {1, 1, 2, 3}, {1, 2, 1, 3}, {1, 3, 2, 2}, {4, 1, 2, 1}, {3, 2, 2, 1}, {3, 2, 2, 1}, {4, 2, 2, 1}, {4, 2, 2, 1},
     {3, 3, 2, 1}, {4, 3, 2, 1}, {4, 3, 1, 1}, {4, 3, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}}};
 
 static_assert(covers_all(kSplit) && covers_all(kCkptFwd40) && covers_all(kCkptFwd200) && covers_all(kCkptFwdLong) &&
               covers_all(kCkptFwd32) && covers_all(kCkptFwdSegs) && covers_all(kTokBwdLong) &&
-              covers_all(kRmsFwd32) && covers_all(kCkptBwd50) && covers_all(kCkptBwdLong) && covers_all(kCkptBwdSegs) &&
+              covers_all(kRmsFwd32) && covers_all(kCkptBwd50) && covers_all(kCkptBwdLong) &&
               covers_all(kCkptBwd50x32) && covers_all(kCkptBwd32) && covers_all(kRmsBwd50) && covers_all(kRmsBwdLong) &&
               covers_all(kRmsBwd50x32) && covers_all(kRmsBwd32), "an entry that does not cover its rows");
 
@@ -147,9 +156,9 @@ inline Shape ckpt_bwd_shape(int64_t T, int64_t nseg, int units, int dtype) {
     if (dtype == 0) return entry(shorter ? kCkptBwd50 : nseg > 1 ? kCkptBwdSegs : kCkptBwdLong, units);
     return entry(shorter ? kCkptBwd50x32 : kCkptBwd32, units);
 }
-inline Shape rms_bwd_shape(int64_t N, int units, int dtype) {
+inline Shape rms_bwd_shape(int64_t N, int units, int dtype, bool dh) {
     const bool shorter = N * units * (dtype == 0 ? 16 : 32) <= 50000000;
-    if (dtype == 0) return entry(shorter ? kRmsBwd50 : kRmsBwdLong, units);
+    if (dtype == 0) return entry(shorter ? kRmsBwd50 : dh ? kRmsBwdLong : kRmsBwdLongAlone, units);
     return entry(shorter ? kRmsBwd50x32 : kRmsBwd32, units);
 }
 
@@ -175,6 +184,15 @@ inline int64_t quant_blocks(int64_t pieces, const QuantShape& sh) {
     const int64_t blocks = (pieces + per_block - 1) / per_block;
     return blocks < most ? blocks : most;
 }
+
+// Waves of a backward block that hold rows of their own (K = 1: the entry's blocks per CU are the waves of one block, fewer
+// where the rows would not give every CU a block).
+inline int row_groups(int64_t T, const Shape& sh) {
+    if (sh.K > 1) return 1;
+    const int64_t all = int64_t(kNumCU) * sh.R, g = (T + all - 1) / all;
+    return g < 1 ? 1 : g < sh.per_cu ? static_cast<int>(g) : sh.per_cu;
+}
+inline int64_t group_blocks_most(const Shape& sh) { return int64_t(kNumCU) * (sh.K > 1 ? sh.per_cu : 1); }
 
 // f(units per lane, waves, rows) as constants for the entry of one of the tables that sh is; false if it is none.  Only what
 // the tables hold is compiled.

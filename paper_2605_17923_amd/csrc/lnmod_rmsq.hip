@@ -1,5 +1,7 @@
 // lnmod_rmsq.hip -- instantiation and launch of the root-mean-square norm with the residual's addition and an output in
 // 8 bits, and of its backward.
+#include <algorithm>
+
 #include "lnmod_code_shapes.hpp"
 #include "lnmod_rmsq_kernels.hpp"
 
@@ -7,6 +9,7 @@ namespace lnmod {
 namespace {
 
 int64_t blocks_for(int64_t N, const Shape& sh) { return grid_blocks(N, static_cast<int64_t>(kNumCU) * sh.per_cu, sh.R); }
+int64_t bwd_blocks_for(int64_t N, const Shape& sh) { return grid_blocks(N, group_blocks_most(sh), sh.R * row_groups(N, sh)); }
 
 }  // namespace
 
@@ -59,7 +62,9 @@ hipError_t launch_rmsq_fwd(int dtype, int code, const void* x, const void* r, co
 }
 
 int64_t rmsq_bwd_blocks(int64_t N, int64_t D, int dtype) {
-    return N <= 0 ? 0 : blocks_for(N, rms_bwd_shape(N, static_cast<int>(D / kUnit), dtype));
+    if (N <= 0) return 0;
+    const int units = static_cast<int>(D / kUnit);
+    return std::max(bwd_blocks_for(N, rms_bwd_shape(N, units, dtype, false)), bwd_blocks_for(N, rms_bwd_shape(N, units, dtype, true)));
 }
 
 hipError_t launch_rmsq_bwd(int dtype, const void* dy, const void* dh, const void* h, const void* w, int64_t N, int64_t D,
@@ -76,20 +81,28 @@ hipError_t launch_rmsq_bwd(int dtype, const void* dy, const void* dh, const void
     a.D = static_cast<int32_t>(D);
     a.nchunks = static_cast<int32_t>(D / kUnit);
     a.inv_D = 1.0f / static_cast<float>(D);
-    const Shape sh = pick_shape(force, rms_bwd_shape(N, a.nchunks, dtype));
+    const Shape sh = pick_shape(force, rms_bwd_shape(N, a.nchunks, dtype, dh != nullptr));
     if (!covers(sh, a.nchunks)) return hipErrorInvalidConfiguration;
-    a.nb = static_cast<int32_t>(blocks_for(N, sh));
-    const dim3 grid(static_cast<unsigned>(a.nb)), block(sh.K * kWave);
+    a.nb = static_cast<int32_t>(bwd_blocks_for(N, sh));
+    const int groups = row_groups(N, sh);
+    bool fits = true;
+    const dim3 grid(static_cast<unsigned>(a.nb)), block(sh.K * groups * kWave);
     const auto run = [&](auto io) {
         const auto go = [&](auto vpl, auto k, auto rows) {
             using Tag = decltype(io);
-            if (dh) hipLaunchKernelGGL((rmsq_bwd_kernel<Tag, vpl, k, rows, true>), grid, block, 0, st, a);
-            else hipLaunchKernelGGL((rmsq_bwd_kernel<Tag, vpl, k, rows, false>), grid, block, 0, st, a);
+            const auto add = [&](auto has) {
+                constexpr int waves = rmsq_bwd_waves(vpl, Unit<Tag>::NV, rows, has);
+                const size_t lds = group_lds(groups, units_at_once(vpl, waves), 1);
+                fits = groups <= groups_most(k, waves);
+                if (fits) hipLaunchKernelGGL((rmsq_bwd_kernel<Tag, vpl, k, rows, has>), grid, block, lds, st, a);
+            };
+            if (dh) add(std::true_type{});
+            else add(std::false_type{});
         };
-        if constexpr (std::is_same<decltype(io), bf16_io>::value) return ShapesOf<kRmsBwd50, kRmsBwdLong>::call(sh, go);
+        if constexpr (std::is_same<decltype(io), bf16_io>::value) return ShapesOf<kRmsBwd50, kRmsBwdLong, kRmsBwdLongAlone>::call(sh, go);
         else return ShapesOf<kRmsBwd50x32, kRmsBwd32>::call(sh, go);
     };
-    if (!(dtype == 0 ? run(bf16_io{}) : run(f32_io{}))) return hipErrorInvalidConfiguration;
+    if (!(dtype == 0 ? run(bf16_io{}) : run(f32_io{})) || !fits) return hipErrorInvalidConfiguration;
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
 

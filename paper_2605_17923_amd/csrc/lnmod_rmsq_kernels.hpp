@@ -245,20 +245,28 @@ struct RmsqBwdArgs {
     float inv_D;
 };
 
+constexpr int rmsq_bwd_waves(int vpl, int nv, int r, bool dh) {
+    return rmsq_waves(vpl * (16 + kDepth * r * 4 * nv * (dh ? 3 : 2)) + 56);
+}
+
 template <typename Tag, int VPL, int K, int R, bool DH>
-__global__ __launch_bounds__(K* kWave)
-LNMOD_OCCUPANCY(rmsq_waves(VPL * (16 + kDepth * R * 4 * Unit<Tag>::NV * (DH ? 3 : 2)) + 56))
+__global__ __launch_bounds__(K* kWave* groups_most(K, rmsq_bwd_waves(VPL, Unit<Tag>::NV, R, DH)))
+LNMOD_OCCUPANCY(rmsq_bwd_waves(VPL, Unit<Tag>::NV, R, DH))
 void rmsq_bwd_kernel(const RmsqBwdArgs a) {
     using U = Unit<Tag>;
     constexpr int NV = U::NV;
     __shared__ float part[2][R][K];
+    extern __shared__ f32x4 sums[];          // see add_groups
     const int lane = threadIdx.x & (kWave - 1);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int in_block = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = K > 1 ? in_block : 0;   // of the row
+    const int groups = K > 1 ? 1 : static_cast<int>(blockDim.x) >> 6, group = K > 1 ? 0 : in_block;
     const int64_t row_bytes = static_cast<int64_t>(a.D) * IO<Tag>::kBytes;
     const uint32_t unit_bytes = static_cast<uint32_t>(row_bytes);
 
     uint32_t chunk[VPL];
-    float W[VPL][8], acc[VPL][8];
+    float W[VPL][8], acc_all[1][VPL][8];
+    float(&acc)[VPL][8] = acc_all[0];
     struct Rows {
         u32x4 dy[R][VPL][NV], h[R][VPL][NV], dh[DH ? R : 1][DH ? VPL : 1][NV];
         float rs[R];
@@ -285,7 +293,7 @@ void rmsq_bwd_kernel(const RmsqBwdArgs a) {
     };
 #pragma unroll
     for (int i = 0; i < VPL; ++i) chunk[i] = static_cast<uint32_t>((i * K + wave) * kWave + lane);
-    const int64_t first = static_cast<int64_t>(blockIdx.x) * R, step = static_cast<int64_t>(a.nb) * R;
+    const int64_t first = (static_cast<int64_t>(blockIdx.x) * groups + group) * R, step = static_cast<int64_t>(a.nb) * groups * R;
     Rows bufs[kDepth];
 #pragma unroll
     for (int d = 0; d < kDepth - 1; ++d) fetch(first + d * step, bufs[d]);
@@ -379,7 +387,8 @@ void rmsq_bwd_kernel(const RmsqBwdArgs a) {
             base += step;
         }
     }
-    const Row slot = row_of(a.ws, static_cast<int64_t>(blockIdx.x) * a.D * 4, static_cast<uint32_t>(a.D) * 4u);
+    add_groups<units_at_once(VPL, rmsq_bwd_waves(VPL, NV, R, DH))>(acc_all, group, groups, sums);
+    const Row slot = row_of(a.ws, static_cast<int64_t>(blockIdx.x) * a.D * 4, group == 0 ? static_cast<uint32_t>(a.D) * 4u : 0u);
 #pragma unroll
     for (int i = 0; i < VPL; ++i) store_sums8(slot, chunk[i], acc[i]);
 }

@@ -11,10 +11,19 @@ static int bad = 0;
 #define CHECK(cond, ...) do { if (!(cond)) { if (bad < 20) { std::printf("FAIL %s: ", #cond); std::printf(__VA_ARGS__); std::printf("\n"); } ++bad; } } while (0)
 
 static void check_shape(const char* which, int dtype, int units, const Shape& s) {
-    CHECK(s.K >= 1 && s.K <= 16 && s.VPL >= 1 && s.VPL <= 4 && (s.R == 1 || s.R == 2), "%s dtype %d units %d: %d %d %d", which, dtype,
+    CHECK(s.K >= 1 && s.K <= 16 && s.VPL >= 1 && s.VPL <= 6 && (s.R == 1 || s.R == 2), "%s dtype %d units %d: %d %d %d", which, dtype,
           units, s.K, s.VPL, s.R);
     CHECK(s.K * s.VPL * 64 >= units, "%s dtype %d units %d: %d x %d", which, dtype, units, s.K, s.VPL);
     CHECK(int64_t(kNumCU) * s.per_cu * s.K * 64 < (int64_t(1) << 32), "%s: a grid of too many threads", which);
+}
+
+// blocks whose waves hold rows of their own: every CU has one where the rows allow it, and never more waves than the entry says
+static void check_rows(const char* which, int dtype, int units, int64_t T, const Shape& s) {
+    check_shape(which, dtype, units, s);
+    const int g = row_groups(T, s);
+    CHECK(g >= 1 && (s.K > 1 ? g == 1 : g <= s.per_cu && g <= 12), "%s T %lld: %d rows", which, (long long)T, g);
+    CHECK(s.K > 1 || g == 1 || (T + int64_t(s.R) * g - 1) / (s.R * g) * 2 >= kNumCU, "%s T %lld: CUs without a block", which, (long long)T);
+    CHECK(group_blocks_most(s) * (s.K > 1 ? 1 : s.per_cu) == int64_t(kNumCU) * s.per_cu, "%s", which);
 }
 
 int main() {
@@ -24,11 +33,11 @@ int main() {
             for (const int64_t T : rows) {
                 for (int64_t nseg = 1; nseg < 100; nseg += 40) {
                     check_shape("checkpoint forward", dtype, units, ckpt_fwd_shape(T, nseg, units, dtype));
-                    check_shape("checkpoint backward", dtype, units, ckpt_bwd_shape(T, nseg, units, dtype));
+                    check_rows("checkpoint backward", dtype, units, T, ckpt_bwd_shape(T, nseg, units, dtype));
                 }
                 for (const bool back : {false, true}) check_shape("per token", dtype, units, ckpt_tok_shape(T, units, dtype, back));
                 check_shape("rms forward", dtype, units, rms_fwd_shape(T, units, dtype));
-                check_shape("rms backward", dtype, units, rms_bwd_shape(T, units, dtype));
+                for (const bool dh : {false, true}) check_rows("rms backward", dtype, units, T, rms_bwd_shape(T, units, dtype, dh));
             }
     // quantize and dequantize: from one piece to more than a card's memory holds; a grid of fewer than 2^32 threads whose blocks
     // all have a piece, and blocks for every piece unless the grid is at its largest

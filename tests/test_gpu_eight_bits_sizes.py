@@ -239,3 +239,23 @@ def test_quantize_rows_that_end_inside_a_group(dtype, N, D, group, code):
     shared = row[:, None].expand(N, wscales.shape[1]).contiguous()
     assert torch.equal(lnmod.dequantize(codes, row, DT[dtype], 0),
                        lnmod.dequantize(want, shared, DT[dtype], group)[:, :D].contiguous())
+
+
+# Backwards where the waves of a block hold rows of their own and add what they have summed: from one row to more than a
+# step of the whole grid, last steps that some waves have no row in, segments shorter than a block's rows.
+@pytest.mark.parametrize("rows", [1, 2, 255, 257, 600, 1025, 3100, 12289])
+@pytest.mark.parametrize("D,dtype", [(200, "bf16"), (1000, "bf16"), (1536, "bf16"), (2000, "bf16"), (2560, "bf16"), (400, "f32"),
+                                     (1024, "f32")])
+def test_rows_of_one_wave(D, dtype, rows):
+    run_ckpt(D, rows, dtype, "int8", 64)
+    run_ckpt(D, rows + 40, dtype, "e4m3", 128, cuts=[0, 0, 1, 2, rows // 2 + 2, rows + 2, rows + 2, rows + 39, rows + 40])
+    run_rms(D, rows, dtype, "e4m3", 64, True)
+    run_rms(D, rows, dtype, "int8", 0, False)
+
+
+@pytest.mark.parametrize("D", [200, 1000, 1496, 2504])
+def test_rows_of_one_wave_in_the_long_launches(D):
+    for residual in (True, False):
+        run_rms(D, rows_of(60, D, "bf16"), "bf16", "e4m3", 128, residual)
+        run_rms(D, rows_of(60, D, "f32"), "f32", "e4m3", 128, residual)
+    run_ckpt(D, rows_of(60, D, "f32"), "f32", "int8", 128, cuts=[0, 700, 700, 701, 3000, rows_of(60, D, "f32")])
