@@ -7,14 +7,15 @@
 // units of 512 features wherever that is possible, because every idle lane costs arithmetic, and the arithmetic of the
 // few waves that HBM likes best is what limits them; forwards, which keep nothing from row to row but the weights, win with
 // many more blocks than are resident (root-mean-square norm, 32 760 x 5120 bf16: 118 us with one block per CU, 80.5 with 64);
-// backwards keep a slot of partial sums per block and stay at what is resident.  Up to 2560 features (fp32: 1024) a backward's
-// row belongs to one wave and a block is several of those (K = 1; "blocks per CU" are its waves), which needs no barrier in
-// the loop, a slot per CU, and no luck with where the dispatcher puts blocks of one wave: checkpoint backward, 32 552 x 1536
-// bf16 57 us with three blocks of three waves per row, 51 with one of four; 130 208 x 1536 205 and 168; 78 125 x 2560 191 and 172.
+// backwards keep a slot of partial sums per block and stay at what is resident.  Up to 2560 features or so (fp32 and the
+// rms norm: 1024 or 1536) a backward's row belongs to one wave and a block is several of those (K = 1; "blocks per CU" are
+// its waves), which needs no barrier in the loop, a slot per CU, and no luck with where the dispatcher puts blocks of one
+// wave: checkpoint backward, 32 552 x 1536 bf16 57 us with three blocks of three waves per row, 51 with one of four; 130 208 x
+// 1536 205 and 168; 78 125 x 2560 191 and 172.
 // The classes of x's size and what the entries lose against the best shape of each problem, in the mean and at worst:
 //   checkpoint forward   bf16 up to 10 MB 1.6 %, 5 %; 40 MB 2 %, 14 %; 200 MB 1 %, 6 %; beyond 1 %, 5 %;  fp32 1 to 3 %
 //   rms norm forward     bf16 1 to 3 %, 14 %;  fp32 2 to 4 %
-//   backwards            bf16 and fp32 up to 50 MB and beyond: 1 to 2 %, 12 % (one wave per row: up to 23 %)
+//   backwards            checkpoint 1 to 3 %, 8 % (3584 features 15 %), rms norm 1 to 3 %, 10 %
 #pragma once
 #include <array>
 #include <utility>
