@@ -63,13 +63,14 @@ hipError_t launch_ckpt_fwd(const Problem& p, bool token, const void* x, const vo
     const Shape sh = pick_shape(p.force, token ? ckpt_tok_shape(p.T, a.f.nchunks, p.dtype, false)
                                              : ckpt_fwd_shape(p.T, p.nseg, a.f.nchunks, p.dtype));
     if (!covers(sh, a.f.nchunks)) return hipErrorInvalidConfiguration;
-    const RowPlan pl = plan_rows_clusters(p.T, token ? 1 : p.nseg, static_cast<int64_t>(kNumCU) * sh.per_cu, sh.R,
+    const int groups = token ? 1 : fwd_row_groups(p.T, sh);
+    const RowPlan pl = plan_rows_clusters(p.T, token ? 1 : p.nseg, static_cast<int64_t>(kNumCU) * sh.per_cu / groups, sh.R * groups,
                                           token ? 1 : fwd_clusters(p.nseg), sh.clusters);
     a.f.rows_per_cluster = pl.rows_per_cluster;
     a.f.nb = pl.nb;
     a.f.interleave = cluster_interleave(p.force, pl);
     a.f.split = cluster_split(a.f.interleave, pl);
-    const dim3 grid(static_cast<unsigned>(pl.blocks)), block(sh.K * kWave);
+    const dim3 grid(static_cast<unsigned>(pl.blocks)), block(sh.K * groups * kWave);
     const bool ok = for_types(p.dtype, code, [&](auto io, auto cd) {
         const auto go = [&](auto vpl, auto k, auto r, auto tok) {
             hipLaunchKernelGGL((ckpt_fwd_kernel<decltype(io), decltype(cd), vpl, k, r, tok>), grid, block, 0, st, a);

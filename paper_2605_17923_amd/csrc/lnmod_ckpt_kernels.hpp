@@ -56,7 +56,7 @@ constexpr int ckpt_bwd_waves(int vpl, int nv, int r, bool tok) {
 }
 
 template <typename Tag, typename C, int VPL, int K, int R, bool TOK>
-__global__ __launch_bounds__(K* kWave)
+__global__ __launch_bounds__(K* kWave* fwd_groups_most(K))
 LNMOD_OCCUPANCY(ckpt_fwd_waves(VPL, Unit<Tag>::NV, R, TOK))
 void ckpt_fwd_kernel(const CkptFwdArgs args) {
     using U = Unit<Tag>;
@@ -66,7 +66,9 @@ void ckpt_fwd_kernel(const CkptFwdArgs args) {
     __shared__ float part[2][R][K][2];
 
     const int lane = threadIdx.x & (kWave - 1);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int in_block = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = K > 1 ? in_block : 0;   // of the row
+    const int groups = K > 1 ? 1 : static_cast<int>(blockDim.x) >> 6, group = K > 1 ? 0 : in_block;
     const int64_t row_bytes = static_cast<int64_t>(a.D) * IO<Tag>::kBytes;
 
     uint32_t chunk[VPL], scale_off[VPL];                     // scale_off: the group's first lane stores its scale
@@ -77,7 +79,7 @@ void ckpt_fwd_kernel(const CkptFwdArgs args) {
         ok[i] = chunk[i] < static_cast<uint32_t>(a.nchunks);
         scale_off[i] = ok[i] && (lane & ((1 << cd.lanes_log2) - 1)) == 0 ? (chunk[i] >> cd.lanes_log2) * 4u : kNowhere;
     }
-    const uint32_t first_lane = threadIdx.x == 0 ? 0u : kNowhere;
+    const uint32_t first_lane = lane == 0 && wave == 0 ? 0u : kNowhere;
     float cnt[K], my_cnt = 0.0f;                             // features each wave holds
 #pragma unroll
     for (int w = 0; w < K; ++w) {
@@ -97,7 +99,7 @@ void ckpt_fwd_kernel(const CkptFwdArgs args) {
     const int64_t r0 = at.cluster * a.rows_per_cluster;
     int64_t stop = r0 + a.rows_per_cluster;
     if (stop > a.T) stop = a.T;
-    const int64_t first = r0 + at.member * R, step = static_cast<int64_t>(a.nb) * R;
+    const int64_t first = r0 + (at.member * groups + group) * R, step = static_cast<int64_t>(a.nb) * groups * R;
 
     const uint32_t unit_bytes = static_cast<uint32_t>(row_bytes);
 

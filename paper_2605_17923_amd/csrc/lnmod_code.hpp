@@ -10,6 +10,7 @@
 // program that follows these lines gets the same codes.  |v*r| stays below Q (1 + 2^-21), which rounds to Q.  The floor
 // of 2^-100 keeps s and r normal numbers; a group of zeros has the codes 0.
 #pragma once
+#include "lnmod_code_shapes.hpp"
 #include "lnmod_kernels.hpp"
 
 namespace lnmod {
@@ -120,6 +121,7 @@ __device__ inline void store_sums8(Row row, uint32_t chunk, const float (&v)[8])
 // Where one wave holds a row, the waves of a block take rows of their own, and what they have summed meets in LDS at the end: a
 // slot of partial sums per block in place of one per wave, and blocks that the dispatcher spreads over the CUs evenly.  The
 // waves are added in their order.
+constexpr int fwd_groups_most(int k) { return k > 1 ? 1 : kFwdGroups; }
 constexpr int groups_most(int k, int waves_per_simd) { return k > 1 ? 1 : 4 * waves_per_simd; }
 // units of a lane that meet at a time, so that LDS stays below the 64 KB that a block gets without asking
 constexpr int units_at_once(int vpl, int waves_per_simd) {

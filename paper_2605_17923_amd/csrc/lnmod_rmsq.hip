@@ -8,7 +8,10 @@
 namespace lnmod {
 namespace {
 
-int64_t blocks_for(int64_t N, const Shape& sh) { return grid_blocks(N, static_cast<int64_t>(kNumCU) * sh.per_cu, sh.R); }
+int64_t fwd_blocks_for(int64_t N, const Shape& sh) {
+    const int groups = fwd_row_groups(N, sh);
+    return grid_blocks(N, static_cast<int64_t>(kNumCU) * sh.per_cu / groups, sh.R * groups);
+}
 int64_t bwd_blocks_for(int64_t N, const Shape& sh) { return grid_blocks(N, group_blocks_most(sh), sh.R * row_groups(N, sh)); }
 
 }  // namespace
@@ -34,8 +37,8 @@ hipError_t launch_rmsq_fwd(int dtype, int code, const void* x, const void* r, co
     a.inv_D = 1.0f / static_cast<float>(D);
     const Shape sh = pick_shape(force, rms_fwd_shape(N, a.nchunks, dtype));
     if (!covers(sh, a.nchunks)) return hipErrorInvalidConfiguration;
-    a.nb = static_cast<int32_t>(blocks_for(N, sh));
-    const dim3 grid(static_cast<unsigned>(a.nb)), block(sh.K * kWave);
+    a.nb = static_cast<int32_t>(fwd_blocks_for(N, sh));
+    const dim3 grid(static_cast<unsigned>(a.nb)), block(sh.K * fwd_row_groups(N, sh) * kWave);
     const auto run = [&](auto io, auto cd) {
         const auto shaped = [&](auto vpl, auto k, auto rows) {
             const auto go = [&](auto res, auto row, auto val) {
@@ -52,7 +55,7 @@ hipError_t launch_rmsq_fwd(int dtype, int code, const void* x, const void* r, co
             if (r) res(std::true_type{});
             else res(std::false_type{});
         };
-        if constexpr (std::is_same<decltype(io), bf16_io>::value) return ShapesOf<kRmsFwd200, kRmsFwdLong>::call(sh, shaped);
+        if constexpr (std::is_same<decltype(io), bf16_io>::value) return ShapesOf<kSplit, kRmsFwd200, kRmsFwdLong>::call(sh, shaped);
         else return ShapesOf<kSplit, kRmsFwd32>::call(sh, shaped);
     };
     bool ok;

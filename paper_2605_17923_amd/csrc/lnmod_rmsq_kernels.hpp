@@ -51,14 +51,16 @@ constexpr int rmsq_waves(int regs) {
 
 // ROW: one scale for a row.  VALUES: out holds the values that the codes stand for.
 template <typename Tag, typename C, int VPL, int K, int R, bool RES, bool ROW, bool VALUES>
-__global__ __launch_bounds__(K* kWave)
+__global__ __launch_bounds__(K* kWave* fwd_groups_most(K))
 LNMOD_OCCUPANCY(rmsq_waves(VPL * (8 + kDepth * R * 4 * Unit<Tag>::NV * (RES ? 2 : 1)) + 48))
 void rmsq_fwd_kernel(const RmsqFwdArgs a) {
     using U = Unit<Tag>;
     constexpr int NV = U::NV;
     __shared__ float part[2][R][K][2];
     const int lane = threadIdx.x & (kWave - 1);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int in_block = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = K > 1 ? in_block : 0;   // of the row
+    const int groups = K > 1 ? 1 : static_cast<int>(blockDim.x) >> 6, group = K > 1 ? 0 : in_block;
     const int64_t row_bytes = static_cast<int64_t>(a.D) * IO<Tag>::kBytes;
     const uint32_t unit_bytes = static_cast<uint32_t>(row_bytes);
 
@@ -69,7 +71,7 @@ void rmsq_fwd_kernel(const RmsqFwdArgs a) {
         scale_off[i] = chunk[i] < static_cast<uint32_t>(a.nchunks) && (lane & ((1 << a.lanes_log2) - 1)) == 0
                            ? (chunk[i] >> a.lanes_log2) * 4u : kNowhere;
     }
-    const uint32_t first_lane = threadIdx.x == 0 ? 0u : kNowhere;
+    const uint32_t first_lane = lane == 0 && wave == 0 ? 0u : kNowhere;
     float W[VPL][8];
     struct Rows {
         u32x4 x[R][VPL][NV], r[RES ? R : 1][RES ? VPL : 1][NV];
@@ -89,7 +91,7 @@ void rmsq_fwd_kernel(const RmsqFwdArgs a) {
             }
         }
     };
-    const int64_t first = static_cast<int64_t>(blockIdx.x) * R, step = static_cast<int64_t>(a.nb) * R;
+    const int64_t first = (static_cast<int64_t>(blockIdx.x) * groups + group) * R, step = static_cast<int64_t>(a.nb) * groups * R;
     Rows bufs[kDepth];
 #pragma unroll
     for (int d = 0; d < kDepth - 1; ++d) fetch(first + d * step, bufs[d]);

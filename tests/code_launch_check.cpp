@@ -15,6 +15,10 @@ static void check_shape(const char* which, int dtype, int units, const Shape& s)
           units, s.K, s.VPL, s.R);
     CHECK(s.K * s.VPL * 64 >= units, "%s dtype %d units %d: %d x %d", which, dtype, units, s.K, s.VPL);
     CHECK(int64_t(kNumCU) * s.per_cu * s.K * 64 < (int64_t(1) << 32), "%s: a grid of too many threads", which);
+    for (const int64_t T : {1, 1000, 5000, 500000}) {
+        const int g = fwd_row_groups(T, s);
+        CHECK(g == 1 || (g == kFwdGroups && s.K == 1 && s.per_cu >= g && T >= int64_t(kNumCU) * s.R * g), "%s T %lld: %d rows", which, (long long)T, g);
+    }
 }
 
 // blocks whose waves hold rows of their own: every CU has one where the rows allow it, and never more waves than the entry says
