@@ -14,10 +14,10 @@
 // are requested before the current step is computed.  Here a lane's unit is eight features in either element type, so that
 // a group of codes is 4, 8 or 16 neighbouring lanes and its scale needs no LDS.
 //
-// Both passes are bound by HBM; their arithmetic (20 to 28 vector operations per feature forward, 15 to 19 backward) keeps the SIMDs
+// Both passes are bound by HBM; their arithmetic (19 to 28 vector operations per feature forward, 15 to 19 backward) keeps the SIMDs
 // issuing for half of the time and more, and has to hide behind the loads.  Measured, int8, groups of 128, bytes that have to move:
-//   75 600 x 5120 bf16   forward 336 us, 5.8 TB/s    backward 315 us, 6.2 TB/s (+ 5 us second pass)
-//   32 760 x 1536 bf16   forward 45 us, 5.6 TB/s     backward 43 us, 5.9 TB/s (+ 4 us)
+//   75 600 x 5120 bf16   forward 337 us, 5.8 TB/s    backward 312 us, 6.2 TB/s (+ 5 us second pass)
+//   32 760 x 1536 bf16   forward 45 us, 5.6 TB/s     backward 44 us, 5.8 TB/s (+ 4 us)
 //   modulation per token, 32 760 x 5120 bf16: forward 252 us, 6.0 TB/s, backward 328 us, 5.6 TB/s
 // (a copy reaches 6.1 TB/s).  Three or four steps in registers in place of two, and waves with neighbouring chunks in place of
 // chunks K*64 apart, brought nothing.
