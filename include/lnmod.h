@@ -299,8 +299,8 @@ int lnmod_dequantize(const void* codes, const float* code_scales, int64_t N, int
  *     xhat = (x' - mean_n) * rstd_n,     and g, c1, c2, dx, dshift, dscale as at the top
  *
  * LNMOD_PER_SAMPLE: dshift, dscale are [B, D] / [nseg, D], float32, or in the I/O dtype where io_grads is not 0, and the
- * workspace holds lnmod_backward_ckpt_workspace_bytes() bytes (query for each problem).  LNMOD_PER_TOKEN: dshift,
- * dscale are [B, S, D] in the I/O dtype; io_grads and the workspace are not looked at.
+ * workspace holds lnmod_backward_ckpt_workspace_bytes() bytes.  LNMOD_PER_TOKEN: dshift, dscale are [B, S, D] in the I/O
+ * dtype; io_grads and the workspace are not looked at.
  */
 int lnmod_forward_ckpt(const void* x, const void* shift, const void* scale, const int32_t* cu_seqlens,
                        int64_t B_or_nseg, int64_t S_or_T, int64_t D, float eps, int64_t group, void* stream,
@@ -311,7 +311,9 @@ int lnmod_backward_ckpt(const void* dy, const void* codes, const float* code_sca
                         void* stream, const float* mean, const float* rstd, void* dx, void* dshift, void* dscale,
                         void* workspace, size_t workspace_bytes, int dtype, int mod, int code, int io_grads);
 
-/* Bytes of device workspace lnmod_backward_ckpt needs with LNMOD_PER_SAMPLE (0 for invalid arguments).  Host-only. */
+/* Bytes of device workspace lnmod_backward_ckpt needs with LNMOD_PER_SAMPLE (0 for invalid arguments).  Host-only.  For one
+ * sample (B_or_nseg == 1) the size never falls as total_tokens grows at one D, so that one workspace serves every shorter
+ * sample; with several samples or segments query for each problem. */
 size_t lnmod_backward_ckpt_workspace_bytes(int64_t B_or_nseg, int64_t total_tokens, int64_t D);
 
 /*
@@ -341,7 +343,8 @@ int lnmod_rmsnorm_quant_backward(const void* dy, const void* dh, const void* h, 
                                  void* stream, const float* rstd, void* dx, void* dw,
                                  void* workspace, size_t workspace_bytes, int dtype, int io_grads);
 
-/* Bytes of device workspace lnmod_rmsnorm_quant_backward needs (0 for invalid arguments).  Host-only. */
+/* Bytes of device workspace lnmod_rmsnorm_quant_backward needs (0 for invalid arguments).  Host-only.  The size never falls as
+ * N grows at one D, so that one workspace serves every call with fewer rows. */
 size_t lnmod_rmsnorm_quant_backward_workspace_bytes(int64_t N, int64_t D);
 
 #ifdef __cplusplus

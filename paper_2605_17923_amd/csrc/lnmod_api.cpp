@@ -126,22 +126,24 @@ int check_rows(int64_t N, int64_t D, int64_t group, int dtype, int code) {
     return LNMOD_OK;
 }
 
+// For one sample a bound on the plan's slots that does not fall as the rows grow.
 size_t ckpt_workspace_bytes(int64_t nseg, int64_t T, int64_t D) {
     int64_t slots = 0;
     for (int dtype = 0; dtype < 2; ++dtype) {
-        const int64_t s = lnmod::bwd_slots(lnmod::ckpt_bwd_plan(T, nseg, D, dtype), nseg);
+        const int64_t s = nseg == 1 ? lnmod::ckpt_bwd_most_slots(T, D, dtype)
+                                    : lnmod::bwd_slots(lnmod::ckpt_bwd_plan(T, nseg, D, dtype), nseg);
         if (s > slots) slots = s;
     }
     return static_cast<size_t>(slots) * 2u * static_cast<size_t>(D) * sizeof(float);
 }
 
 size_t rmsq_workspace_bytes(int64_t N, int64_t D) {
-    int64_t nb = 0;
+    int64_t slots = 0;
     for (int dtype = 0; dtype < 2; ++dtype) {
-        const int64_t b = lnmod::rmsq_bwd_blocks(N, D, dtype);
-        if (b > nb) nb = b;
+        const int64_t s = lnmod::rmsq_bwd_most_slots(N, D, dtype);
+        if (s > slots) slots = s;
     }
-    return static_cast<size_t>(nb) * static_cast<size_t>(D) * sizeof(float);
+    return static_cast<size_t>(slots) * static_cast<size_t>(D) * sizeof(float);
 }
 
 }  // namespace

@@ -44,6 +44,10 @@ RowPlan ckpt_bwd_plan(int64_t T, int64_t nseg, int64_t D, int dtype, Shape* shap
     return plan_rows_slots(T, nseg, group_blocks_most(sh), sh.R * row_groups(T, sh), stream_us, 16.0 / row, sh.clusters);
 }
 
+int64_t ckpt_bwd_most_slots(int64_t T, int64_t D, int dtype) {
+    return T <= 0 ? 0 : most_slots(T, ckpt_bwd_shape(T, 1, static_cast<int>(D / kUnit), dtype));
+}
+
 hipError_t launch_ckpt_fwd(const Problem& p, bool token, const void* x, const void* shift, const void* scale, void* y,
                            const Checkpoint& c, int code, float* mean, float* rstd, hipStream_t st) {
     CkptFwdArgs a{};

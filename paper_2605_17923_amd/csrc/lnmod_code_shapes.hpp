@@ -199,13 +199,19 @@ inline int64_t quant_blocks(int64_t pieces, const QuantShape& sh) {
 }
 
 // Waves of a backward block that hold rows of their own (K = 1: the entry's blocks per CU are the waves of one block, fewer
-// where the rows would not give every CU a block).
+// where the rows give the CUs fewer).  Rounded up, so that every row is in work at once as far as the entry allows: just
+// beyond a multiple of 256 R rows that leaves up to half of the CUs without a block (257 rows: 129 blocks), and is still the
+// faster side.  Rounded down, which gives every CU a block and some waves a second row, both passes (us): checkpoint
+// 300 x 1536 bf16 7.7 -> 8.5, 300 x 2560 9.4 -> 10.5, 640 x 2560 10.9 -> 11.7; rms norm 300 x 1536 6.2 -> 6.9; from 1024
+// rows on the same.  So the blocks fall as the rows pass such a line, and the workspace queries ask for most_slots.
 inline int row_groups(int64_t T, const Shape& sh) {
     if (sh.K > 1) return 1;
     const int64_t all = int64_t(kNumCU) * sh.R, g = (T + all - 1) / all;
     return g < 1 ? 1 : g < sh.per_cu ? static_cast<int>(g) : sh.per_cu;
 }
 inline int64_t group_blocks_most(const Shape& sh) { return int64_t(kNumCU) * (sh.K > 1 ? sh.per_cu : 1); }
+// Slots of one sample's backward at most: what row_groups makes of T rows or fewer, which does not fall as T grows.
+inline int64_t most_slots(int64_t T, const Shape& sh) { return grid_blocks(T, group_blocks_most(sh), sh.R); }
 
 // The same in a forward, which has nothing to add: blocks of four waves with rows of their own in place of blocks of one
 // (checkpoint forward 32 552 x 1536 bf16 5 % less than with three waves per row, rms norm 19 531 x 2560 without a residual 27 %).

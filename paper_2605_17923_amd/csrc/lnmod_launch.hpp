@@ -894,12 +894,13 @@ hipError_t launch_quantize(int dtype, int code, const void* x, int64_t N, int64_
 hipError_t launch_dequantize(int dtype, int code, const void* codes, const float* scales, int64_t N, int64_t D, int64_t group,
                              void* x, hipStream_t st);
 RowPlan ckpt_bwd_plan(int64_t T, int64_t nseg, int64_t D, int dtype, Shape* shape = nullptr, const Shape* force = nullptr);
+int64_t ckpt_bwd_most_slots(int64_t T, int64_t D, int dtype);    // of one sample
 hipError_t launch_ckpt_fwd(const Problem& p, bool token, const void* x, const void* shift, const void* scale, void* y,
                            const Checkpoint& c, int code, float* mean, float* rstd, hipStream_t st);
 hipError_t launch_ckpt_bwd(const Problem& p, bool token, const void* dy, const Checkpoint& c, int code, const void* scale,
                            const float* mean, const float* rstd, void* dx, void* dshift, void* dscale, bool io_grads,
                            float* ws, hipStream_t st);
-int64_t rmsq_bwd_blocks(int64_t N, int64_t D, int dtype);        // partial-sum slots
+int64_t rmsq_bwd_most_slots(int64_t N, int64_t D, int dtype);
 hipError_t launch_rmsq_fwd(int dtype, int code, const void* x, const void* r, const void* w, int64_t N, int64_t D, float eps,
                            int64_t group, void* h, void* out, float* scales, float* rstd, bool values, hipStream_t st,
                            const Shape* force = nullptr);

@@ -64,10 +64,10 @@ hipError_t launch_rmsq_fwd(int dtype, int code, const void* x, const void* r, co
     return ok ? hipGetLastError() : hipErrorInvalidConfiguration;
 }
 
-int64_t rmsq_bwd_blocks(int64_t N, int64_t D, int dtype) {
+int64_t rmsq_bwd_most_slots(int64_t N, int64_t D, int dtype) {
     if (N <= 0) return 0;
     const int units = static_cast<int>(D / kUnit);
-    return std::max(bwd_blocks_for(N, rms_bwd_shape(N, units, dtype, false)), bwd_blocks_for(N, rms_bwd_shape(N, units, dtype, true)));
+    return std::max(most_slots(N, rms_bwd_shape(N, units, dtype, false)), most_slots(N, rms_bwd_shape(N, units, dtype, true)));
 }
 
 hipError_t launch_rmsq_bwd(int dtype, const void* dy, const void* dh, const void* h, const void* w, int64_t N, int64_t D,
