@@ -253,7 +253,7 @@ const char* lnmod_status_string(int status) {
     switch (status) {
         case LNMOD_OK: return "ok";
         case LNMOD_EINVAL: return "invalid argument";
-        case LNMOD_EUNSUPPORTED: return "unsupported hidden size";
+        case LNMOD_EUNSUPPORTED: return "unsupported hidden size or combination of arguments";
         case LNMOD_EALIGN: return "pointer not 16-byte aligned";
         case LNMOD_EWORKSPACE: return "workspace missing or too small";
         case LNMOD_ELAUNCH: return "kernel launch failed";

@@ -943,6 +943,8 @@ def _rmsnorm_quant(x, w, residual, eps, code, group, stream=None, values=True):
     number, kind = _code_of(code)
     _group_of(group, row=True)
     a, dt, N, D = _rms_args(x, w, residual=residual)
+    if group == 0 and 0.0 < ctypes.c_float(eps).value < ctypes.c_float(1e-20).value:
+        raise ValueError("eps must be at least 1e-20 with one scale for a row (group 0), got %r" % (eps,))
     a.on_gpu()
     with _on_device(x, stream) as handle:
         codes = scales = y = None
