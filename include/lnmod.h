@@ -273,8 +273,9 @@ size_t lnmod_qknorm_backward_workspace_bytes(int64_t N, int64_t D);
  *     LNMOD_INT8   code = v*r rounded to the nearest whole number, ties to even: one rounding; |code| <= 127
  *     LNMOD_E4M3   code = v*r rounded to float32, then to the nearest OCP e4m3, ties to even; at most 448
  *
- * The code stands for code*s.  A group that holds an infinity or a NaN has s = NaN and the codes 0: it stands for NaN in
- * every place.  codes: [N, D] bytes, 16-byte aligned; code_scales: float32 [N, ceil(D / group)], at any float's address.
+ * The code stands for code*s, held to the largest float where a finite s takes it beyond (int8, amax the largest float
+ * itself).  A group that holds an infinity or a NaN has s = NaN and the codes 0: it stands for NaN in every place.
+ * codes: [N, D] bytes, 16-byte aligned; code_scales: float32 [N, ceil(D / group)], at any float's address.
  * In these calls D is a multiple of 8 in either element type, and an unknown `code` or `group` is LNMOD_EINVAL.
  */
 typedef enum { LNMOD_INT8 = 0, LNMOD_E4M3 = 1 } lnmod_code;

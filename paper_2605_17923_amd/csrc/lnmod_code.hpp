@@ -276,4 +276,21 @@ __device__ inline void decode<e4m3_code>(const u32x2& w, float (&v)[8]) {
     }
 }
 
+// What eight codes stand for.  The largest float has s = fp32(max / 127) rounded up, and 127*s is beyond float32 (no other
+// largest value of a group does that, and none in e4m3, 448 = 7 * 2^6 and max = 7 * 2396745 * 2^104): such a product is held
+// to the largest float, so that a finite group, a mask of the type's lowest value among them, stays finite.  Rounded to bf16 it is the
+// infinity that max itself rounds to.  One instruction per feature of fp32 int8: 20 000 x 5120 back 97.9 -> 100.5 us.
+template <typename Tag, typename C>
+__device__ inline void stand_for(const u32x2& w, float s, float (&v)[8]) {
+    decode<C>(w, v);
+    // with two NaN beside it the median is v itself
+    [[maybe_unused]] const float most = __builtin_fabsf(s) < __builtin_inff() ? __FLT_MAX__ : __builtin_nanf("");
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        v[e] *= s;
+        if constexpr (std::is_same<Tag, f32_io>::value && std::is_same<C, int8_code>::value)
+            v[e] = __builtin_amdgcn_fmed3f(v[e], -most, most);
+    }
+}
+
 }  // namespace lnmod

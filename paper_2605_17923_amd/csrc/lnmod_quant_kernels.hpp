@@ -149,9 +149,7 @@ __global__ __launch_bounds__(kQuantWaves* kWave) void quant_kernel(const QuantAr
             const Piece p = piece_at(cur.row[i], cur.slot[i]);
             float v[8];
             if constexpr (BACK) {
-                decode<C>(now.code[i], v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= now.s[i];
+                stand_for<Tag, C>(now.code[i], now.s[i], v);
                 u32x4 o[NV];
                 Unit<Tag>::pack(v, o);
                 store_unit<Tag>(x_of(p), p.unit, o);

@@ -207,9 +207,7 @@ void rmsq_fwd_kernel(const RmsqFwdArgs a) {
                     const u32x2 w = encode<C>(v, sc);
                     if constexpr (VALUES) {
                         u32x4 o[NV];
-                        decode<C>(w, v);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] *= sc.s;
+                        stand_for<Tag, C>(w, sc.s, v);
                         U::pack(v, o);
                         store_unit<Tag>(rout, chunk[i], o);
                     } else {

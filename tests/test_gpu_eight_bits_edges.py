@@ -1,0 +1,67 @@
+"""The 8-bit operators at the edges of what their calls allow: values next to the largest float, gradients that share a
+consumer, transforms, threads, another stream.  Compared bit for bit unless said otherwise."""
+import pytest
+import torch
+
+from paper_2605_17923_amd import functional as F
+from paper_2605_17923_amd import lnmod
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def make(seed, *shape, dtype="bf16", mean=0.0, std=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * std + mean).to(DT[dtype]).cuda()
+
+
+def bits(t):
+    return t.contiguous().view({1: torch.uint8, 2: torch.int16, 4: torch.int32}[t.element_size()])
+
+
+def same_bits(a, b):
+    return a.dtype == b.dtype and a.shape == b.shape and torch.equal(bits(a), bits(b))
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_finite_groups_stay_finite(dtype, code):
+    """Masks of the type's lowest value, and the floats next to the largest one, come back finite: the float32 product of
+    code and scale, held to the largest float."""
+    top = torch.finfo(DT[dtype]).max
+    x = make(3, 40, 96, dtype=dtype)
+    x[0, 5:] = -top
+    x[1] = top
+    x[2, 32], x[3, 95] = top, -top
+    steps = torch.tensor([top], dtype=DT[dtype]).view(torch.int16 if dtype == "bf16" else torch.int32).item()
+    for k in range(32):                                                    # the k-th below the largest
+        x[4 + k, ::7] = torch.tensor([steps - k]).to(torch.int16 if dtype == "bf16" else torch.int32).view(DT[dtype]).item()
+    x[36, 0] = float("inf")
+    codes, scales = lnmod.quantize(x, code, 32)
+    back = lnmod.dequantize(codes, scales, x.dtype, 32)
+    s = scales.cpu().double().repeat_interleave(32, 1)
+    want = (codes.cpu().double() * s).float()                              # one rounding; infinite beyond the largest float
+    big = torch.finfo(torch.float32).max
+    want = torch.where(s.isfinite(), want.clamp(-big, big), want).to(x.dtype)
+    assert same_bits(back.cpu().nan_to_num(7.0), want.nan_to_num(7.0)) and torch.equal(back.cpu().isnan(), want.isnan())
+    assert torch.equal(back.isfinite(), scales.isfinite().repeat_interleave(32, 1))
+    assert back[1].eq(top).all() and back[0, 5:].eq(-top).all()
+    # scales of the caller's own: code*s as it is
+    scales[0], scales[1], scales[2, 0] = float("inf"), float("-inf"), float("nan")
+    back = lnmod.dequantize(codes, scales, x.dtype, 32)
+    want = (codes.cpu().double() * scales.cpu().double().repeat_interleave(32, 1)).to(x.dtype)[:3]
+    same = same_bits(back[:2].cpu().nan_to_num(7.0, 8.0, 9.0), want[:2].nan_to_num(7.0, 8.0, 9.0))
+    assert same and back[2, :32].isnan().all()
+
+
+def test_finite_normed_rows_stay_finite():
+    big = torch.finfo(torch.float32).max
+    x = torch.ones(5, 64, device="cuda")
+    w = torch.full((64,), big, device="cuda")
+    w[40:] = -1.0
+    for code in ("int8", "e4m3"):
+        codes, scales, _, rstd = lnmod.rmsnorm_quant_forward(x, w, None, 1e-30, code, 32)
+        assert rstd.eq(1.0).all() and scales.isfinite().all()
+        y = F.rms_norm_quant(x, w, None, 1e-30, code, 32)
+        assert y.isfinite().all() and y[:, :32].eq(big).all()
+        assert same_bits(y, lnmod.dequantize(codes, scales, torch.float32, 32))
