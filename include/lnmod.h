@@ -334,8 +334,10 @@ size_t lnmod_backward_ckpt_workspace_bytes(int64_t B_or_nseg, int64_t total_toke
  *     hhat = h*rstd     g = dy*w     c_n = (1/D) sum_d g*hhat
  *     dx[n,d] = dh[n,d] + rstd_n*(g - hhat*c_n)     dw[d] = sum_n dy[n,d]*hhat[n,d]
  *
- * dx is the gradient of x and of r.  dw: [D], float32 (any float's address), or in the I/O dtype and 16-byte aligned where
- * io_grads is not 0; zeros when N == 0.  workspace: lnmod_rmsnorm_quant_backward_workspace_bytes(N, D) bytes.
+ * dx is the gradient of x and of r.  lnmod_rmsnorm_quant_backward_residual writes it a second time, to dr [N, D], for
+ * callers whose x and r must not share a gradient's memory.  dw: [D], float32 (any float's address), or in the I/O dtype and
+ * 16-byte aligned where io_grads is not 0; zeros when N == 0.  workspace: lnmod_rmsnorm_quant_backward_workspace_bytes(N, D)
+ * bytes in either form.
  */
 int lnmod_rmsnorm_quant_forward(const void* x, const void* r, const void* w, int64_t N, int64_t D, float eps,
                                 int64_t group, void* stream, void* h, void* codes, float* code_scales, void* y,
@@ -343,6 +345,9 @@ int lnmod_rmsnorm_quant_forward(const void* x, const void* r, const void* w, int
 int lnmod_rmsnorm_quant_backward(const void* dy, const void* dh, const void* h, const void* w, int64_t N, int64_t D,
                                  void* stream, const float* rstd, void* dx, void* dw,
                                  void* workspace, size_t workspace_bytes, int dtype, int io_grads);
+int lnmod_rmsnorm_quant_backward_residual(const void* dy, const void* dh, const void* h, const void* w, int64_t N, int64_t D,
+                                          void* stream, const float* rstd, void* dx, void* dr, void* dw,
+                                          void* workspace, size_t workspace_bytes, int dtype, int io_grads);
 
 /* Bytes of device workspace lnmod_rmsnorm_quant_backward needs (0 for invalid arguments).  Host-only.  The size never falls as
  * N grows at one D, so that one workspace serves every call with fewer rows. */

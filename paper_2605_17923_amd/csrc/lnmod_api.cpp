@@ -146,6 +146,30 @@ size_t rmsq_workspace_bytes(int64_t N, int64_t D) {
     return static_cast<size_t>(slots) * static_cast<size_t>(D) * sizeof(float);
 }
 
+// dr: a second copy of dx, or null
+int rmsnorm_quant_backward_impl(const void* dy, const void* dh, const void* h, const void* w, int64_t N, int64_t D, void* stream,
+                                const float* rstd, void* dx, void* dr, void* dw, void* workspace, size_t workspace_size,
+                                int dtype, int io_grads) {
+    const int st = check_shape(1, N, D, 1.0f, dtype, N);
+    if (st != LNMOD_OK) return st;
+    if (D % 8 != 0) return LNMOD_EUNSUPPORTED;
+    const hipStream_t hs = static_cast<hipStream_t>(stream);
+    if (!dw) return LNMOD_EINVAL;
+    if (io_grads && !aligned16(dw)) return LNMOD_EALIGN;
+    if (N == 0) {                                                  // empty sums are zeros
+        const hipError_t e = lnmod::launch_zero_f32(static_cast<float*>(dw), grad_floats(D, dtype, io_grads != 0), hs);
+        return e == hipSuccess ? LNMOD_OK : LNMOD_ELAUNCH;
+    }
+    if (!dy || !h || !w || !rstd || !dx) return LNMOD_EINVAL;
+    if (!aligned16(dy) || !aligned16(dh) || !aligned16(h) || !aligned16(w) || !aligned16(dx) || !aligned16(dr))
+        return LNMOD_EALIGN;
+    if (!workspace || workspace_size < rmsq_workspace_bytes(N, D)) return LNMOD_EWORKSPACE;
+    if (!aligned16(workspace)) return LNMOD_EALIGN;
+    const hipError_t e = lnmod::launch_rmsq_bwd(dtype, dy, dh, h, w, N, D, rstd, dx, dr, dw, io_grads != 0,
+                                                static_cast<float*>(workspace), hs);
+    return e == hipSuccess ? LNMOD_OK : LNMOD_ELAUNCH;
+}
+
 }  // namespace
 
 extern "C" {
@@ -449,23 +473,15 @@ int lnmod_rmsnorm_quant_forward(const void* x, const void* r, const void* w, int
 int lnmod_rmsnorm_quant_backward(const void* dy, const void* dh, const void* h, const void* w, int64_t N, int64_t D,
                                  void* stream, const float* rstd, void* dx, void* dw, void* workspace,
                                  size_t workspace_size, int dtype, int io_grads) {
-    const int st = check_shape(1, N, D, 1.0f, dtype, N);
-    if (st != LNMOD_OK) return st;
-    if (D % 8 != 0) return LNMOD_EUNSUPPORTED;
-    const hipStream_t hs = static_cast<hipStream_t>(stream);
-    if (!dw) return LNMOD_EINVAL;
-    if (io_grads && !aligned16(dw)) return LNMOD_EALIGN;
-    if (N == 0) {                                                  // empty sums are zeros
-        const hipError_t e = lnmod::launch_zero_f32(static_cast<float*>(dw), grad_floats(D, dtype, io_grads != 0), hs);
-        return e == hipSuccess ? LNMOD_OK : LNMOD_ELAUNCH;
-    }
-    if (!dy || !h || !w || !rstd || !dx) return LNMOD_EINVAL;
-    if (!aligned16(dy) || !aligned16(dh) || !aligned16(h) || !aligned16(w) || !aligned16(dx)) return LNMOD_EALIGN;
-    if (!workspace || workspace_size < rmsq_workspace_bytes(N, D)) return LNMOD_EWORKSPACE;
-    if (!aligned16(workspace)) return LNMOD_EALIGN;
-    const hipError_t e = lnmod::launch_rmsq_bwd(dtype, dy, dh, h, w, N, D, rstd, dx, dw, io_grads != 0,
-                                                static_cast<float*>(workspace), hs);
-    return e == hipSuccess ? LNMOD_OK : LNMOD_ELAUNCH;
+    return rmsnorm_quant_backward_impl(dy, dh, h, w, N, D, stream, rstd, dx, nullptr, dw, workspace, workspace_size, dtype,
+                                       io_grads);
+}
+
+int lnmod_rmsnorm_quant_backward_residual(const void* dy, const void* dh, const void* h, const void* w, int64_t N, int64_t D,
+                                          void* stream, const float* rstd, void* dx, void* dr, void* dw, void* workspace,
+                                          size_t workspace_size, int dtype, int io_grads) {
+    if (N > 0 && !dr) return LNMOD_EINVAL;
+    return rmsnorm_quant_backward_impl(dy, dh, h, w, N, D, stream, rstd, dx, dr, dw, workspace, workspace_size, dtype, io_grads);
 }
 
 size_t lnmod_rmsnorm_quant_backward_workspace_bytes(int64_t N, int64_t D) {

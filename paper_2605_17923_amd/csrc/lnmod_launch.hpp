@@ -905,7 +905,7 @@ hipError_t launch_rmsq_fwd(int dtype, int code, const void* x, const void* r, co
                            int64_t group, void* h, void* out, float* scales, float* rstd, bool values, hipStream_t st,
                            const Shape* force = nullptr);
 hipError_t launch_rmsq_bwd(int dtype, const void* dy, const void* dh, const void* h, const void* w, int64_t N, int64_t D,
-                           const float* rstd, void* dx, void* dw, bool io_grads, float* ws, hipStream_t st,
+                           const float* rstd, void* dx, void* dr, void* dw, bool io_grads, float* ws, hipStream_t st,
                            const Shape* force = nullptr);
 
 }  // namespace lnmod

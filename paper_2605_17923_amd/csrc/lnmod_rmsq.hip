@@ -71,7 +71,7 @@ int64_t rmsq_bwd_most_slots(int64_t N, int64_t D, int dtype) {
 }
 
 hipError_t launch_rmsq_bwd(int dtype, const void* dy, const void* dh, const void* h, const void* w, int64_t N, int64_t D,
-                           const float* rstd, void* dx, void* dw, bool io_grads, float* ws, hipStream_t st, const Shape* force) {
+                           const float* rstd, void* dx, void* dr, void* dw, bool io_grads, float* ws, hipStream_t st, const Shape* force) {
     RmsqBwdArgs a{};
     a.dy = dy;
     a.dh = dh;
@@ -79,6 +79,7 @@ hipError_t launch_rmsq_bwd(int dtype, const void* dy, const void* dh, const void
     a.w = w;
     a.rstd = rstd;
     a.dx = dx;
+    a.dr = dr;
     a.ws = ws;
     a.N = N;
     a.D = static_cast<int32_t>(D);

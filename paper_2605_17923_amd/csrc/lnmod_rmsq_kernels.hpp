@@ -237,6 +237,7 @@ struct RmsqBwdArgs {
     const void* w;
     const float* rstd;
     void* dx;
+    void* dr;                // a second copy of dx, or null
     float* ws;               // [nb][D] fp32 partial dw sums
     int64_t N;
     int32_t nb;
@@ -355,7 +356,8 @@ void rmsq_bwd_kernel(const RmsqBwdArgs a) {
 #pragma unroll
         for (int j = 0; j < R; ++j) {
             const int64_t row = base + j;
-            const Row rdx = row_of(a.dx, row * row_bytes, row < a.N ? unit_bytes : 0u);
+            const uint32_t bytes = row < a.N ? unit_bytes : 0u;
+            const Row rdx = row_of(a.dx, row * row_bytes, bytes);
             const float k2 = now.rs[j] * (c[j] * a.inv_D);
 #pragma unroll
             for (int i = 0; i < VPL; ++i) {
@@ -373,6 +375,7 @@ void rmsq_bwd_kernel(const RmsqBwdArgs a) {
                 u32x4 t[NV];
                 U::pack(o, t);
                 store_unit<Tag>(rdx, chunk[i], t);
+                if (a.dr) store_unit<Tag>(row_of(a.dr, row * row_bytes, bytes), chunk[i], t);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }

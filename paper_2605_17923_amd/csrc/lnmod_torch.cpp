@@ -433,17 +433,21 @@ variable_list rms_forward(const Tensor& x, const Tensor& w, const Tensor& residu
     return values ? variable_list{y, h, rstd} : variable_list{codes, scales, h, rstd};
 }
 
-// dx, dw; empty where the call is not the plain case
-variable_list rms_backward(const Tensor& dy, const Tensor& h, const Tensor& w, const Tensor& rstd, const Tensor& dh, bool io_grads) {
+// dx, dw, dr (dx itself unless it has to be a tensor of its own); empty where the call is not the plain case
+variable_list rms_backward(const Tensor& dy, const Tensor& h, const Tensor& w, const Tensor& rstd, const Tensor& dh, bool io_grads,
+                           bool own_dr) {
     int64_t N, D;
     if (!rms_shapes(h, w, dh, &N, &D) || !plain(dy, h.sizes(), h.scalar_type(), h.device()) ||
         !plain(rstd, at::IntArrayRef(&N, 1), at::kFloat, h.device()))
         return {};
-    Tensor dx = fresh_like(h), dw = fresh(D, io_grads ? h.scalar_type() : at::kFloat, h);
+    Tensor dx = fresh_like(h), dw = fresh(D, io_grads ? h.scalar_type() : at::kFloat, h), dr = own_dr ? fresh_like(h) : dx;
     const Tensor ws = fresh_bytes(lnmod_rmsnorm_quant_backward_workspace_bytes(N, D), h);
-    const int st = lnmod_rmsnorm_quant_backward(ptr(dy), ptr(dh), ptr(h), ptr(w), N, D, stream_of(h), f32(rstd), out(dx), out(dw),
-                                                out(ws), static_cast<size_t>(ws.numel()), code_of(h), io_grads);
-    return st == LNMOD_OK ? variable_list{dx, dw} : variable_list{};
+    const size_t bytes = static_cast<size_t>(ws.numel());
+    const int st = own_dr ? lnmod_rmsnorm_quant_backward_residual(ptr(dy), ptr(dh), ptr(h), ptr(w), N, D, stream_of(h), f32(rstd),
+                                                                  out(dx), out(dr), out(dw), out(ws), bytes, code_of(h), io_grads)
+                          : lnmod_rmsnorm_quant_backward(ptr(dy), ptr(dh), ptr(h), ptr(w), N, D, stream_of(h), f32(rstd), out(dx),
+                                                         out(dw), out(ws), bytes, code_of(h), io_grads);
+    return st == LNMOD_OK ? variable_list{dx, dw, dr} : variable_list{};
 }
 
 struct RmsNormQuant : public torch::autograd::Function<RmsNormQuant> {
@@ -461,10 +465,13 @@ struct RmsNormQuant : public torch::autograd::Function<RmsNormQuant> {
         const Tensor &h = s[0], &w = s[1], &rstd = s[2];
         const bool residual = ctx->saved_data["residual"].toBool();
         const Tensor dy = grads.back().contiguous(), dh = residual ? grads[0].contiguous() : Tensor();
+        // x and the residual get gradients in memory of their own: where views lie in front of the operator, two leaves'
+        // .grad would share it, and the next backward, adding to one, would add to both.
+        const bool both = residual && ctx->needs_input_grad(0) && ctx->needs_input_grad(2);
         variable_list r;
-        if (plain_state()) r = rms_backward(dy, h, w, rstd, dh, true);
-        if (r.empty()) r = python_backward("_rms_quant_backward", 2, dy, h, w, rstd, dh);
-        return {r[0], r[1], residual ? r[0] : Tensor(), Tensor(), Tensor(), Tensor()};
+        if (plain_state()) r = rms_backward(dy, h, w, rstd, dh, true, both);
+        if (r.empty()) r = python_backward("_rms_quant_backward", 3, dy, h, w, rstd, dh, static_cast<int64_t>(both));
+        return {r[0], r[1], residual ? r[2] : Tensor(), Tensor(), Tensor(), Tensor()};
     }
 };
 
@@ -582,8 +589,9 @@ py::object rmsnorm_quant_forward(const py::object& x, const py::object& w, const
 py::object rmsnorm_quant_backward(const py::object& dy, const py::object& h, const py::object& w, const py::object& rstd,
                                   const py::object& dh) {
     return attempt({dy, h, w, rstd}, dh, [&] {
-        variable_list r = rms_backward(unpack(dy), unpack(h), unpack(w), unpack(rstd), unpack_or(dh).value_or(Tensor()), false);
+        variable_list r = rms_backward(unpack(dy), unpack(h), unpack(w), unpack(rstd), unpack_or(dh).value_or(Tensor()), false, false);
         if (r.empty()) throw NotPlain();
+        r.pop_back();                        // dr is dx
         return r;
     });
 }

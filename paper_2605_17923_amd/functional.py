@@ -154,8 +154,8 @@ def ln_modulate_ckpt(x, shift, scale, eps=1e-6, cu_seqlens=None, code="int8", gr
     return _LnModulateCkpt.apply(x, shift, scale, cu_seqlens, float(eps), code, group) if y is None else y
 
 
-def _rms_quant_backward(dy, h, w, rstd, dh):
-    return lnmod._rmsnorm_quant_backward(dy, h, w, rstd, dh, io_grads=True)
+def _rms_quant_backward(dy, h, w, rstd, dh, own_dr):
+    return lnmod._rmsnorm_quant_backward(dy, h, w, rstd, dh, io_grads=True, own_dr=bool(own_dr))
 
 
 class _RmsNormQuant(torch.autograd.Function):
@@ -173,15 +173,15 @@ class _RmsNormQuant(torch.autograd.Function):
     def backward(ctx, *grads):
         h, w, rstd = ctx.saved_tensors
         dh = grads[0].contiguous() if ctx.residual else None
-        dx, dw = _rms_quant_backward(grads[-1].contiguous(), h, w, rstd, dh)
-        return dx, dw, dx if ctx.residual else None, None, None, None
+        both = ctx.residual and ctx.needs_input_grad[0] and ctx.needs_input_grad[2]
+        dx, dw, dr = _rms_quant_backward(grads[-1].contiguous(), h, w, rstd, dh, both)
+        return dx, dw, dr if ctx.residual else None, None, None, None
 
 
 def rms_norm_quant(x, w, residual=None, eps=1e-6, code="e4m3", group=0):
     """y = h * rsqrt(mean(h^2) + eps) * w rounded to 8 bits (one scale for each `group` = 32, 64 or 128 features, or 0: for
     a row), as the values that the codes stand for: what a model trains on that is served with lnmod.rmsnorm_quant_forward.
-    h = x; with a residual h = x + residual, and (h, y) is returned.  As with torch's own addition, x and the residual get
-    one and the same gradient tensor from torch.autograd.grad."""
+    h = x; with a residual h = x + residual, and (h, y) is returned."""
     host = lnmod.native()
     r = None if host is None else host.rms_norm_quant(x, w, residual, float(eps), code, group)
     return _RmsNormQuant.apply(x, w, residual, float(eps), code, group) if r is None else r

@@ -30,6 +30,7 @@ EXPORTS = ("lnmod_forward", "lnmod_backward", "lnmod_forward_varlen", "lnmod_bac
            "lnmod_gated_backward_io", "lnmod_qknorm_backward_io", "lnmod_backward_token", "lnmod_quantize",
            "lnmod_dequantize", "lnmod_forward_ckpt", "lnmod_backward_ckpt", "lnmod_backward_ckpt_workspace_bytes",
            "lnmod_rmsnorm_quant_forward", "lnmod_rmsnorm_quant_backward",
+           "lnmod_rmsnorm_quant_backward_residual",
            "lnmod_rmsnorm_quant_backward_workspace_bytes")
 
 _lib = None
@@ -109,6 +110,8 @@ def library() -> ctypes.CDLL:
     lib.lnmod_rmsnorm_quant_forward.argtypes = [vp, vp, vp, i64, i64, f32, i64, vp, vp, vp, vp, vp, vp, cint, cint]
     lib.lnmod_rmsnorm_quant_backward.restype = cint
     lib.lnmod_rmsnorm_quant_backward.argtypes = [vp, vp, vp, vp, i64, i64, vp, vp, vp, vp, vp, sz, cint, cint]
+    lib.lnmod_rmsnorm_quant_backward_residual.restype = cint
+    lib.lnmod_rmsnorm_quant_backward_residual.argtypes = [vp, vp, vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, sz, cint, cint]
     lib.lnmod_rmsnorm_quant_backward_workspace_bytes.restype = sz
     lib.lnmod_rmsnorm_quant_backward_workspace_bytes.argtypes = [i64, i64]
     _lib = lib
@@ -305,6 +308,13 @@ def lnmod_rmsnorm_quant_backward(dy, dh, h, w, N, D, stream, rstd, dx, dw, works
                                  io_grads):
     return library().lnmod_rmsnorm_quant_backward(_p(dy), _p(dh), _p(h), _p(w), N, D, stream, _p(rstd), _p(dx),
                                                   _p(dw), _p(workspace), workspace_bytes, dtype, io_grads)
+
+
+def lnmod_rmsnorm_quant_backward_residual(dy, dh, h, w, N, D, stream, rstd, dx, dr, dw, workspace, workspace_bytes,
+                                          dtype, io_grads):
+    return library().lnmod_rmsnorm_quant_backward_residual(_p(dy), _p(dh), _p(h), _p(w), N, D, stream, _p(rstd),
+                                                           _p(dx), _p(dr), _p(dw), _p(workspace), workspace_bytes,
+                                                           dtype, io_grads)
 
 
 def lnmod_rmsnorm_quant_backward_workspace_bytes(N, D):
@@ -965,11 +975,12 @@ def rmsnorm_quant_backward(dy, h, w, rstd, dh=None, stream=None, ws=None):
     residual stream -> dx (of x and of the residual, I/O dtype) and dw (float32 [D])."""
     host = None if ws is not None else _host(dy, stream)
     r = None if host is None else host.rmsnorm_quant_backward(dy, h, w, rstd, dh)
-    return _rmsnorm_quant_backward(dy, h, w, rstd, dh, stream, ws) if r is None else r
+    return _rmsnorm_quant_backward(dy, h, w, rstd, dh, stream, ws)[:2] if r is None else r
 
 
-def _rmsnorm_quant_backward(dy, h, w, rstd, dh, stream=None, ws=None, io_grads=False):
-    """rmsnorm_quant_backward(); with io_grads dw comes in the I/O dtype."""
+def _rmsnorm_quant_backward(dy, h, w, rstd, dh, stream=None, ws=None, io_grads=False, own_dr=False):
+    """rmsnorm_quant_backward() -> dx, dw, dr; with io_grads dw comes in the I/O dtype, with own_dr dr, the gradient of
+    the residual, is not dx itself."""
     import torch
     a, dt, N, D = _rms_args(h, w, dh=dh)
     a.expect("dy", dy, h.shape)
@@ -980,8 +991,13 @@ def _rmsnorm_quant_backward(dy, h, w, rstd, dh, stream=None, ws=None, io_grads=F
     with _on_device(h, stream) as handle:
         dx = torch.empty_like(h)
         dw = torch.empty(D, dtype=h.dtype if io_grads else torch.float32, device=h.device)
+        dr = torch.empty_like(h) if own_dr else dx
         if ws is None:
             ws = torch.empty(max(need, 16), dtype=torch.uint8, device=h.device)
-        _check(lnmod_rmsnorm_quant_backward(dy, dh, h, w, N, D, handle, rstd, dx, dw, ws, ws.numel(), dt,
-                                            int(io_grads)), "lnmod_rmsnorm_quant_backward")
-    return dx, dw
+        if own_dr:
+            _check(lnmod_rmsnorm_quant_backward_residual(dy, dh, h, w, N, D, handle, rstd, dx, dr, dw, ws, ws.numel(),
+                                                         dt, int(io_grads)), "lnmod_rmsnorm_quant_backward_residual")
+        else:
+            _check(lnmod_rmsnorm_quant_backward(dy, dh, h, w, N, D, handle, rstd, dx, dw, ws, ws.numel(), dt,
+                                                int(io_grads)), "lnmod_rmsnorm_quant_backward")
+    return dx, dw, dr

@@ -65,3 +65,45 @@ def test_finite_normed_rows_stay_finite():
         y = F.rms_norm_quant(x, w, None, 1e-30, code, 32)
         assert y.isfinite().all() and y[:, :32].eq(big).all()
         assert same_bits(y, lnmod.dequantize(codes, scales, torch.float32, 32))
+
+
+@pytest.mark.parametrize("path", ["native", "python"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_gradients_of_x_and_of_the_residual_share_no_memory(dtype, path):
+    """With views in front of the operator the leaves' .grad are made of the very tensors that the backward returns."""
+    N, D = 37, 264
+    call = F.rms_norm_quant if path == "native" else (lambda *t: F._RmsNormQuant.apply(*t, 1e-6, "e4m3", 0))
+    a, b, w = (make(k, *s, dtype=dtype).requires_grad_() for k, s in ((1, (N * D,)), (2, (N * D,)), (3, (D,))))
+    total = 0.0
+    for turn in range(3):
+        dh, dy = make(10 + turn, N, D, dtype=dtype), make(20 + turn, N, D, dtype=dtype)
+        torch.autograd.backward(call(a.view(N, D), w, b.view(N, D)), (dh, dy))
+        h, rstd = lnmod.rmsnorm_quant_forward(a.detach().view(N, D), w.detach(), b.detach().view(N, D))[2:]
+        dx = lnmod.rmsnorm_quant_backward(dy, h, w.detach(), rstd, dh)[0].view(-1)
+        total = dx if turn == 0 else total + dx
+        for leaf in (a, b):
+            assert same_bits(leaf.grad, total), turn
+    a.grad.zero_()
+    assert same_bits(b.grad, total)
+    x, r = (t.detach().view(N, D).requires_grad_() for t in (a, b))
+    gx, gr = torch.autograd.grad(call(x, w, r), (x, r), (dh, dy))
+    assert same_bits(gx, gr) and gx.untyped_storage().data_ptr() != gr.untyped_storage().data_ptr()
+    # one of the two alone, and one tensor in both places
+    for one in (x, r):
+        assert same_bits(torch.autograd.grad(call(x, w, r), one, (dh, dy))[0], gx)
+        frozen = [t if t is one else t.detach() for t in (x, r)]
+        assert same_bits(torch.autograd.grad(call(frozen[0], w, frozen[1]), one, (dh, dy))[0], gx)
+    both, = torch.autograd.grad(call(x, w, x), x, (dh, dy))
+    h, rstd = lnmod.rmsnorm_quant_forward(x.detach(), w.detach(), x.detach())[2:]
+    assert same_bits(both, lnmod.rmsnorm_quant_backward(dy, h, w.detach(), rstd, dh)[0] * 2)
+
+
+@pytest.mark.parametrize("N,D", [(1, 8), (257, 1536), (4099, 2600), (9001, 5120)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_second_copy_is_the_first(N, D, dtype):
+    dy, h, w, dh = (make(k, *s, dtype=dtype) for k, s in ((1, (N, D)), (2, (N, D)), (3, (D,)), (4, (N, D))))
+    rstd = lnmod.rmsnorm_quant_forward(h, w)[3]
+    for along in (dh, None):
+        dx, dw = lnmod.rmsnorm_quant_backward(dy, h, w, rstd, along)
+        got = lnmod._rmsnorm_quant_backward(dy, h, w, rstd, along, own_dr=True)
+        assert all(same_bits(u, v) for u, v in zip(got, (dx, dw, dx)))
