@@ -323,7 +323,8 @@ size_t lnmod_backward_ckpt_workspace_bytes(int64_t B_or_nseg, int64_t total_toke
  *     h[n,d] = x[n,d] + r[n,d]      one float32 addition rounded once to the I/O dtype, and stored
  *     rstd_n = 1/sqrt((1/D) sum_d h[n,d]^2 + eps)     v[n,d] = (h[n,d]*rstd_n) * w[d]
  *
- * x, r, h: [N, D]; w: [D]; rstd: float32 [N] (written).  r and h are both NULL where there is no residual; h is x then.
+ * in float32: a row whose mean of squares is beyond it has rstd 0.  x, r, h: [N, D]; w: [D]; rstd: float32 [N] (written).
+ * r and h are both NULL where there is no residual; h is x then.
  * Either codes and code_scales are given, and hold the codes of v, or y [N, D] in the I/O dtype, which holds the values that
  * those codes stand for (for training with the rounding in the loop); the other is NULL.  group 0: one scale for a whole
  * row, code_scales [N].  There the largest |v| is formed as rstd_n times the largest |h*w|, so a row where that product is

@@ -1,5 +1,7 @@
 """The 8-bit operators at the edges of what their calls allow: values next to the largest float, gradients that share a
 consumer, transforms, threads, another stream.  Compared bit for bit unless said otherwise."""
+import threading
+
 import pytest
 import torch
 
@@ -107,3 +109,95 @@ def test_the_second_copy_is_the_first(N, D, dtype):
         dx, dw = lnmod.rmsnorm_quant_backward(dy, h, w, rstd, along)
         got = lnmod._rmsnorm_quant_backward(dy, h, w, rstd, along, own_dr=True)
         assert all(same_bits(u, v) for u, v in zip(got, (dx, dw, dx)))
+
+
+def test_transforms_are_refused():
+    x, sh, sc = (make(k, 3, *s, dtype="f32") for k, s in ((1, (2, 8, 64)), (2, (2, 64)), (3, (2, 64))))
+    r, w = make(4, 3, 2, 8, 64, dtype="f32"), make(5, 64, dtype="f32")
+    ln = lambda t: F.ln_modulate_ckpt(t, sh[0], sc[0], group=32)
+    rms = lambda t: F.rms_norm_quant(t, w, r[0])[1]
+    with pytest.raises(RuntimeError):
+        torch.func.vmap(F.ln_modulate_ckpt)(x, sh, sc)
+    with pytest.raises(RuntimeError):
+        torch.func.vmap(lambda t, u: F.rms_norm_quant(t, w, u)[1])(x, r)
+    with pytest.raises(RuntimeError):
+        torch.func.vmap(lambda t: lnmod.quantize(t)[0])(x)
+    for call in (ln, rms):
+        with pytest.raises(RuntimeError):
+            torch.func.grad(lambda t: call(t).sum())(x[0])
+        with torch.autograd.forward_ad.dual_level(), pytest.raises(RuntimeError):
+            call(torch.autograd.forward_ad.make_dual(x[0], x[0]))
+        leaf = x[0].clone().requires_grad_()
+        g = torch.randn_like(leaf).requires_grad_()
+        first, = torch.autograd.grad(call(leaf), leaf, g, create_graph=True)
+        assert not first.requires_grad                                     # no half-connected second derivative
+
+
+def test_calls_from_several_threads():
+    """Each thread on a stream of its own, all at once, forwards and backwards: what one thread alone gives."""
+    D, N, turns = 1536, 700, 8
+    sets = [(make(k, N, D), make(k + 10, N, D), make(k + 20, 2, D, std=0.2), make(k + 30, D, mean=1.0, std=0.2), make(k + 40, N, D))
+            for k in range(4)]
+    cu = torch.tensor([0, 300, N], dtype=torch.int32, device="cuda")
+
+    def step(x, r, mod, w, dy):
+        x, r, mod, w = (t.detach().requires_grad_() for t in (x, r, mod, w))
+        y = F.ln_modulate_ckpt(x, mod, mod, 1e-6, cu, "e4m3", 64)
+        h, z = F.rms_norm_quant(y, w, r, code="int8", group=128)
+        grads = torch.autograd.grad((h, z), (x, r, mod, w), (dy, dy))
+        codes, scales = lnmod.quantize(z.detach(), "int8", 32)
+        return [h.detach(), z.detach(), *grads, codes, scales, lnmod.dequantize(codes, scales, torch.bfloat16, 32)]
+
+    want = [step(*s) for s in sets]
+    torch.cuda.synchronize()
+    got, errors = [None] * 4, []
+
+    def work(k):
+        try:
+            torch.cuda.set_device(0)
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                got[k] = [step(*sets[k]) for _ in range(turns)]
+            stream.synchronize()
+        except BaseException as e:                                         # noqa: BLE001  (shown by the assertion below)
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(60)
+    assert not errors and not any(t.is_alive() for t in threads)
+    for k in range(4):
+        for outs in got[k]:
+            assert all(same_bits(u, v) for u, v in zip(outs, want[k]))
+
+
+@pytest.mark.parametrize("op", ["sample", "packed", "rms"])
+def test_a_gradient_that_nobody_asks_for(op):
+    """One output of the norm used, or one leaf frozen: the others' gradients keep their bits."""
+    D = 264
+    cu = torch.tensor([0, 5, 5, 74], dtype=torch.int32, device="cuda") if op == "packed" else None
+    if op == "rms":
+        ts = [make(1, 74, D), make(2, D), make(3, 74, D)]
+        call = lambda *t: F.rms_norm_quant(*t, 1e-6, "int8", 32)[1]
+    else:
+        ts = [make(1, *((74, D) if cu is not None else (1, 74, D))), make(2, 1 if cu is None else 3, D), make(3, 1 if cu is None else 3, D)]
+        call = lambda *t: F.ln_modulate_ckpt(*t, 1e-6, cu, "int8", 32)
+    dy = make(4, *ts[0].shape)
+    leaves = [t.requires_grad_() for t in ts]
+    want = torch.autograd.grad(call(*leaves), leaves, dy)
+    for k in range(3):
+        some = [t if i == k else t.detach() for i, t in enumerate(leaves)]
+        got, = torch.autograd.grad(call(*some), leaves[k], dy)
+        assert same_bits(got, want[k]), k
+
+
+def test_a_mean_of_squares_beyond_float32():
+    """rstd is formed in float32, as the header says: 0 where the mean of squares is beyond it."""
+    x, w = make(1, 3, 64, dtype="f32"), make(2, 64, dtype="f32")
+    x[1] = 1e25
+    for group in (0, 32):
+        codes, scales, _, rstd = lnmod.rmsnorm_quant_forward(x, w, None, 1e-6, "int8", group)
+        assert rstd[1] == 0 and (rstd[[0, 2]] > 0).all() and not codes[1].any() and codes[[0, 2]].any(-1).all()
+        assert scales.isfinite().all()
