@@ -33,6 +33,16 @@ int64_t fwd_clusters(int64_t nseg) {
     return c;
 }
 
+// The waves that an entry puts into a block of rows of one wave fit the kernel's launch bounds.
+template <typename Tag>
+constexpr bool groups_fit(const ShapeTable& t) {
+    for (const Shape& s : t)
+        if (s.K == 1 && s.per_cu > groups_most(1, ckpt_bwd_waves(s.VPL, Unit<Tag>::NV, s.R, false))) return false;
+    return true;
+}
+static_assert(groups_fit<bf16_io>(kCkptBwd50) && groups_fit<bf16_io>(kCkptBwdLong) && groups_fit<bf16_io>(kCkptBwdSegs) &&
+              groups_fit<f32_io>(kCkptBwd50x32) && groups_fit<f32_io>(kCkptBwd32), "more waves than the kernel's launch bounds");
+
 }  // namespace
 
 RowPlan ckpt_bwd_plan(int64_t T, int64_t nseg, int64_t D, int dtype, Shape* shape, const Shape* force) {

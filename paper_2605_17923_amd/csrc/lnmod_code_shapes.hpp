@@ -138,9 +138,10 @@ inline constexpr ShapeTable kRmsBwd32 = {{
     {3, 3, 2, 1}, {4, 3, 2, 1}, {4, 3, 1, 1}, {4, 3, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}}};
 
 static_assert(covers_all(kSplit) && covers_all(kCkptFwd40) && covers_all(kCkptFwd200) && covers_all(kCkptFwdLong) &&
-              covers_all(kCkptFwd32) && covers_all(kCkptFwdSegs) && covers_all(kTokBwdLong) &&
-              covers_all(kRmsFwd32) && covers_all(kCkptBwd50) && covers_all(kCkptBwdLong) &&
-              covers_all(kCkptBwd50x32) && covers_all(kCkptBwd32) && covers_all(kRmsBwd50) && covers_all(kRmsBwdLong) &&
+              covers_all(kCkptFwd32) && covers_all(kCkptFwdSegs) && covers_all(kTokFwd) && covers_all(kTokBwd200) &&
+              covers_all(kTokBwdLong) && covers_all(kRmsFwd200) && covers_all(kRmsFwdLong) && covers_all(kRmsFwd32) &&
+              covers_all(kCkptBwd50) && covers_all(kCkptBwdLong) && covers_all(kCkptBwdSegs) && covers_all(kCkptBwd50x32) &&
+              covers_all(kCkptBwd32) && covers_all(kRmsBwd50) && covers_all(kRmsBwdLong) && covers_all(kRmsBwdLongAlone) &&
               covers_all(kRmsBwd50x32) && covers_all(kRmsBwd32), "an entry that does not cover its rows");
 
 inline const Shape& entry(const ShapeTable& t, int units) { return t[(units - 1) / 64]; }

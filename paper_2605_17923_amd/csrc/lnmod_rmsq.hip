@@ -12,6 +12,17 @@ int64_t fwd_blocks_for(int64_t N, const Shape& sh) {
     const int groups = fwd_row_groups(N, sh);
     return grid_blocks(N, static_cast<int64_t>(kNumCU) * sh.per_cu / groups, sh.R * groups);
 }
+// see groups_fit in lnmod_ckpt.hip
+template <typename Tag>
+constexpr bool groups_fit(const ShapeTable& t, bool dh) {
+    for (const Shape& s : t)
+        if (s.K == 1 && s.per_cu > groups_most(1, rmsq_bwd_waves(s.VPL, Unit<Tag>::NV, s.R, dh))) return false;
+    return true;
+}
+static_assert(groups_fit<bf16_io>(kRmsBwd50, true) && groups_fit<bf16_io>(kRmsBwd50, false) && groups_fit<bf16_io>(kRmsBwdLong, true) &&
+              groups_fit<bf16_io>(kRmsBwdLongAlone, false) && groups_fit<f32_io>(kRmsBwd50x32, true) &&
+              groups_fit<f32_io>(kRmsBwd50x32, false) && groups_fit<f32_io>(kRmsBwd32, true) && groups_fit<f32_io>(kRmsBwd32, false),
+              "more waves than the kernel's launch bounds");
 int64_t bwd_blocks_for(int64_t N, const Shape& sh) { return grid_blocks(N, group_blocks_most(sh), sh.R * row_groups(N, sh)); }
 
 }  // namespace
