@@ -7,11 +7,12 @@
 // units of 512 features wherever that is possible, because every idle lane costs arithmetic, and the arithmetic of the
 // few waves that HBM likes best is what limits them; forwards, which keep nothing from row to row but the weights, win with
 // many more blocks than are resident (root-mean-square norm, 32 760 x 5120 bf16: 118 us with one block per CU, 80.5 with 64);
-// backwards keep a slot of partial sums per block and stay at what is resident.  Up to 2560 features or so (fp32 and the
-// rms norm: 1024 or 1536) a backward's row belongs to one wave and a block is several of those (K = 1; "blocks per CU" are
-// its waves), which needs no barrier in the loop, a slot per CU, and no luck with where the dispatcher puts blocks of one
-// wave: checkpoint backward, 32 552 x 1536 bf16 57 us with three blocks of three waves per row, 51 with one of four; 130 208 x
-// 1536 205 and 168; 78 125 x 2560 191 and 172.
+// backwards keep a slot of partial sums per block and stay at what is resident.  On short rows a backward's row belongs to one
+// wave and a block is several of those (K = 1; "blocks per CU" are its waves): checkpoint bf16 up to five units a lane, six on
+// more than 50 MB, fp32 two; rms norm bf16 three up to 50 MB, then one, two and five (three without a residual's gradient),
+// fp32 one up to 50 MB, then three.  That needs no barrier in the loop, a slot per CU, and no luck with where the dispatcher
+// puts blocks of one wave: checkpoint backward, 32 552 x 1536 bf16 57 us with three blocks of three waves per row, 51 with one of
+// four; 130 208 x 1536 205 and 168; 78 125 x 2560 191 and 172.
 // The classes of x's size and what the entries lose against the best shape of each problem, in the mean and at worst:
 //   checkpoint forward   bf16 up to 10 MB 1.6 %, 5 %; 40 MB 2 %, 14 %; 200 MB 1 %, 6 %; beyond 1 %, 5 %;  fp32 1 to 3 %
 //   rms norm forward     bf16 1 to 3 %, 14 %;  fp32 2 to 4 %
@@ -104,7 +105,8 @@ inline constexpr ShapeTable kCkptBwd50 = {{
 inline constexpr ShapeTable kCkptBwdLong = {{
     {1, 1, 2, 12}, {1, 2, 2, 4}, {1, 3, 1, 4}, {1, 4, 2, 3}, {1, 5, 1, 4}, {1, 6, 1, 4}, {4, 2, 2, 1}, {4, 2, 2, 1},
     {3, 3, 2, 1}, {4, 3, 2, 1}, {4, 3, 1, 1}, {4, 3, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}}};
-// several samples or segments: 58 794 x 2048 in 40 of them, both passes, 250 us with {4, 1, 2, 2}, 231 (19 959 in 40 shorter ones 1 % more)
+// several samples or segments: 58 794 x 2048 in 40 of them, both passes, 250 us with {4, 1, 2, 2}, 231 (19 959 in 40 shorter ones 1 % more).
+// Only this width was measured with segments; the others keep the entries of one sample.
 inline constexpr ShapeTable kCkptBwdSegs = [] {
     ShapeTable t = kCkptBwdLong;
     t[3] = {1, 4, 1, 4};
@@ -124,7 +126,8 @@ inline constexpr ShapeTable kRmsBwd50 = {{
 inline constexpr ShapeTable kRmsBwdLong = {{
     {1, 1, 2, 8}, {1, 2, 1, 4}, {3, 1, 2, 1}, {4, 1, 2, 1}, {1, 5, 1, 2}, {3, 2, 1, 1}, {3, 3, 1, 1}, {8, 1, 2, 1},
     {3, 3, 2, 1}, {10, 1, 1, 1}, {12, 1, 1, 1}, {12, 1, 1, 1}, {8, 2, 1, 1}, {4, 4, 1, 1}, {4, 4, 1, 1}, {8, 2, 1, 1}}};
-// without a gradient along the residual stream: 32 552 x 1536 60.2 us with the entry above, 54.7
+// without a gradient along the residual stream: 32 552 x 1536 60.2 us with the entry above, 54.7.  Only this width was measured
+// without one; the others keep the entries of the sweep with it.
 inline constexpr ShapeTable kRmsBwdLongAlone = [] {
     ShapeTable t = kRmsBwdLong;
     t[2] = {1, 3, 1, 3};

@@ -2,7 +2,7 @@
 // the codes).  Both move their bytes once and do little with them, so what bounds them is HBM: 3 (bf16) or 5 (fp32) bytes per
 // feature.  The pattern is the plain copy's: a wave takes V pieces of 64 units (eight features a lane), the waves of the
 // grid take consecutive pieces, and the next ones are requested before the current ones are computed.  A group is 4, 8
-// or 16 lanes, so its largest magnitude needs two to four DPP steps and no LDS.  75 600 x 5120 bf16, groups of 128: 187 us, 6.3
+// or 16 lanes, so its largest magnitude needs two to four DPP steps and no LDS.  75 600 x 5120 bf16, groups of 128: 185 us, 6.3
 // TB/s, and 192 us back, 6.1 TB/s, where a copy reaches 6.1.
 //
 // Rows whose length is a whole number of groups are one long row, cut into pieces of 64 units.  Otherwise (PAD) a piece can

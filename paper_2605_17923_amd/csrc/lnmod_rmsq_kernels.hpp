@@ -17,9 +17,10 @@
 // of lnmod_ckpt_kernels.hpp.
 //
 // Bound by HBM (17.4 vector operations per feature forward).  Measured, bf16 with a residual:
-//   32 760 x 5120, codes, a scale for a row     forward 195 us, 6.0 TB/s
-//   32 760 x 1536, values, groups of 128        forward 65 us, 6.2 TB/s     backward 72 us, 5.6 TB/s (+ 5 us second pass)
-//   1 x 5120 2.3 us, 96 x 4096 3.2 us: a launch and one pass through the memory's latency
+//   32 760 x 5120, codes, a scale for a row     forward 198 us, 5.9 TB/s
+//   32 760 x 1536, values, groups of 128        forward 65 us, 6.2 TB/s     backward 72 us, 5.6 TB/s (+ 5 us second pass),
+//       with the residual's gradient in memory of its own 83 us, 6.1 TB/s
+//   1 x 5120 2.4 us, 96 x 4096 3.2 us: a launch and one pass through the memory's latency
 #pragma once
 #include "lnmod_code.hpp"
 
