@@ -201,3 +201,36 @@ def test_a_mean_of_squares_beyond_float32():
         codes, scales, _, rstd = lnmod.rmsnorm_quant_forward(x, w, None, 1e-6, "int8", group)
         assert rstd[1] == 0 and (rstd[[0, 2]] > 0).all() and not codes[1].any() and codes[[0, 2]].any(-1).all()
         assert scales.isfinite().all()
+
+
+def test_offsets_beyond_four_gib():
+    """quantize, the norm and its backward (both forms) on rows whose bytes lie beyond 4 GiB: what the same rows give alone."""
+    D, N = 8192, 280000                                                    # 4.6 GB each
+    x, r = (torch.empty(N, D, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    for k, t in enumerate((x, r)):
+        for at in range(0, N, 40000):
+            t[at:at + 40000].normal_(generator=torch.Generator(device="cuda").manual_seed(at + k))
+    w = make(3, D, mean=1.0, std=0.2)
+    parts = [slice(a, a + 5) for a in (0, 131070, 262142, N - 5)]
+    codes, scales = lnmod.quantize(x, "int8", 128)
+    for p in parts:
+        want = lnmod.quantize(x[p].contiguous(), "int8", 128)
+        assert same_bits(codes[p], want[0]) and same_bits(scales[p], want[1]), p
+    del codes, scales
+    codes, scales, h, rstd = lnmod.rmsnorm_quant_forward(x, w, r, 1e-6, "e4m3", 128)
+    alone = [lnmod.rmsnorm_quant_forward(x[p].contiguous(), w, r[p].contiguous(), 1e-6, "e4m3", 128) for p in parts]
+    for p, want in zip(parts, alone):
+        assert same_bits(h[p], want[2])
+        # sums of squares in another order where the launch shape differs: codes and scales as far as rstd is the same
+        rows = rstd[p] == want[3]
+        assert rows.any() and bool(((rstd[p] - want[3]).abs() <= 1e-6 * want[3]).all())
+        assert same_bits(codes[p][rows].float(), want[0][rows].float()) and same_bits(scales[p][rows], want[1][rows])
+    del codes, scales
+    dx, _, dr = lnmod._rmsnorm_quant_backward(x, h, w, rstd, r, own_dr=True)
+    assert same_bits(dx, dr)
+    for p in parts:
+        g, hhat = x[p].double() * w.double(), h[p].double() * rstd[p].double()[:, None]
+        ref = r[p].double() + rstd[p].double()[:, None] * (g - hhat * (g * hhat).mean(-1, keepdim=True))
+        # one rounding to bf16, 2^-8 of the value at most, and fp32 sums
+        assert bool(((dx[p].double() - ref).abs() <= ref.abs() * 2.0 ** -8 + 1e-5 * ref.abs().max()).all())
+    torch.cuda.empty_cache()
