@@ -354,6 +354,98 @@ int lnmod_rmsnorm_quant_backward_residual(const void* dy, const void* dh, const 
  * N grows at one D, so that one workspace serves every call with fewer rows. */
 size_t lnmod_rmsnorm_quant_backward_workspace_bytes(int64_t N, int64_t D);
 
+/*
+ * Codes with one scale for a whole row: x [N, D] in the I/O dtype -> codes [N, D], code_scales [N], as above with the row as
+ * the group.  What lnmod_code_product reads on either side: activations, and weights [features of y, D] once.
+ * D is a multiple of 8, 8 <= D <= 2^20; lnmod_dequantize with group 0 is the way back.
+ */
+int lnmod_quantize_rows(const void* x, int64_t N, int64_t D, void* stream, void* codes, float* code_scales, int dtype,
+                        int code);
+
+/*
+ * Product of codes that have one scale for each row on either side:
+ *
+ *     y[m,n] = (sum_k a[m,k]*w[n,k]) * a_scales[m] * w_scales[n] + bias[n]
+ *
+ * a: [M, K], w: [N, K] (a linear layer's weight as it is stored), both of type `code`; a_scales: float32 [M]; w_scales: float32
+ * [N]; bias: [N] in the I/O dtype or NULL; y: [M, N] in the I/O dtype, rounded once.  The sum is exact for LNMOD_INT8 (32-bit
+ * integers) and float32 for LNMOD_E4M3, where a code that is NaN makes its row or column NaN.  A row with a scale of NaN is
+ * NaN.  K is a multiple of 8, 8 <= K < 2^17 (LNMOD_EUNSUPPORTED); M, N < 2^31; M == 0 or N == 0 does nothing.
+ * a, w and y are 16-byte aligned, the scales and bias at any of their elements' addresses.
+ */
+int lnmod_code_product(const void* a, const float* a_scales, const void* w, const float* w_scales, const void* bias,
+                       int64_t M, int64_t N, int64_t K, void* stream, void* y, int dtype, int code);
+
+/*
+ * Rotary positions with several axes (time, height, width of a video's patches), of queries and keys in one launch.
+ *
+ * The first R features of a head are R/2 pairs, shared out over the axes in order: axis a has features[a] of the R.  Pair j of
+ * a token whose position on the pair's axis is p turns by the angle whose cosine and sine are table[p][j]:
+ *
+ *     (u, v) -> (u*cos - v*sin, u*sin + v*cos)        turned back (inverse != 0): (u*cos + v*sin, v*cos - u*sin)
+ *
+ * Pair j is the features 2j and 2j + 1 (interleaved != 0), or j and j + R/2.  Features from R on pass as they are.  A position
+ * outside 0 ... table_rows - 1 has no angle: the features of its axis are NaN.
+ */
+typedef struct {
+    const int32_t* positions; /* device, [position_rows, axes] */
+    int64_t position_rows;    /* S: the samples share them; or B*S */
+    const float* table;       /* device, [table_rows, R/2, 2], 8-byte aligned */
+    int64_t table_rows;       /* 1 ... 2^31 - 1 */
+    int32_t axes;             /* 1 ... LNMOD_MAX_AXES */
+    int32_t features[4];      /* even; R = their sum <= head_dim, and a multiple of 8 where pairs are not interleaved */
+    int32_t interleaved;
+} lnmod_rotation;
+#define LNMOD_MAX_AXES 4
+
+/*
+ * A tensor [B, S, heads, head_dim] with dense features: element (b, s, h, d) at data[b*batch + s*token + h*head + d].  Strides
+ * count elements; each is a multiple of 16 bytes and not negative (a dimension of 0 repeats a row).  So q and k may be views of
+ * a fused projection's output, and gradients may come with the heads in front of the tokens.  The descriptors, as
+ * lnmod_rotation, are host memory that the call reads before it returns.
+ */
+typedef struct {
+    const void* data;
+    int64_t batch, token, head;
+} lnmod_heads;
+
+/*
+ * q_out [B, S, q_heads, head_dim] and k_out [B, S, k_heads, head_dim] are dense.  k and k_out are NULL and k_heads 0 where
+ * there is one tensor only.  head_dim is a multiple of 8, 8 <= head_dim <= 256; heads*head_dim <= 2^20 for each tensor
+ * (LNMOD_EUNSUPPORTED).  Its backward is the call with `inverse` turned over, on the gradients.
+ */
+int lnmod_rotary(const lnmod_heads* q, const lnmod_heads* k, int64_t B, int64_t S, int64_t q_heads, int64_t k_heads,
+                 int64_t head_dim, const lnmod_rotation* rotation, int inverse, void* stream, void* q_out, void* k_out,
+                 int dtype);
+
+/*
+ * Q-Norm + K-Norm and the rotation in one pass, rounded once: per tensor
+ *
+ *     rstd = 1/sqrt(mean x^2 + eps)      y = rotation of (x*rstd)*w
+ *
+ * over all heads of a token (per_head 0; w [heads*head_dim], rstd float32 [B*S], heads*head_dim <= 8192) or over each head
+ * (w [head_dim], rstd float32 [B*S, heads]).  Both tensors are required.
+ *
+ * Backward: g' is the gradient turned back;  xhat = x*rstd   g = g'*w   c = mean g*xhat
+ *     dx = rstd*(g - xhat*c)      dw = sum g'*xhat over tokens (per_head: and heads), in a fixed order
+ * dq [B, S, q_heads, head_dim] and dk are dense; dwq, dwk: float32, or in the I/O dtype where io_grads is not 0; zeros where
+ * there is no token.  workspace: lnmod_qknorm_rotary_backward_workspace_bytes() bytes, 16-byte aligned.
+ */
+int lnmod_qknorm_rotary_forward(const lnmod_heads* q, const lnmod_heads* k, const void* wq, const void* wk, int64_t B,
+                                int64_t S, int64_t q_heads, int64_t k_heads, int64_t head_dim,
+                                const lnmod_rotation* rotation, float eps, int per_head, void* stream, void* q_out,
+                                void* k_out, float* rstd_q, float* rstd_k, int dtype);
+int lnmod_qknorm_rotary_backward(const lnmod_heads* dq_out, const lnmod_heads* dk_out, const lnmod_heads* q,
+                                 const lnmod_heads* k, const void* wq, const void* wk, int64_t B, int64_t S,
+                                 int64_t q_heads, int64_t k_heads, int64_t head_dim, const lnmod_rotation* rotation,
+                                 int per_head, void* stream, const float* rstd_q, const float* rstd_k, void* dq, void* dk,
+                                 void* dwq, void* dwk, void* workspace, size_t workspace_bytes, int dtype, int io_grads);
+
+/* Bytes of device workspace lnmod_qknorm_rotary_backward needs for `tokens` = B*S (0 for invalid arguments).  Host-only.  The
+ * size never falls as the tokens grow, so that one workspace serves every call with fewer. */
+size_t lnmod_qknorm_rotary_backward_workspace_bytes(int64_t tokens, int64_t q_heads, int64_t k_heads, int64_t head_dim,
+                                                    int per_head);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,6 +1,7 @@
 // lnmod_api.cpp -- the C ABI declared in include/lnmod.h: the operator entry points, nothing else.
 // The library keeps no mutable state: a call's result depends on its arguments alone.
 #include "lnmod_api_impl.hpp"
+#include "lnmod_rotary.hpp"
 
 static_assert(LNMOD_STATIC_WORKSPACE_BYTES == lnmod::kStaticWorkspaceBytes, "header and library disagree");
 
@@ -168,6 +169,74 @@ int rmsnorm_quant_backward_impl(const void* dy, const void* dh, const void* h, c
     const hipError_t e = lnmod::launch_rmsq_bwd(dtype, dy, dh, h, w, N, D, rstd, dx, dr, dw, io_grads != 0,
                                                 static_cast<float*>(workspace), hs);
     return e == hipSuccess ? LNMOD_OK : LNMOD_ELAUNCH;
+}
+
+// ---- rotary positions ------------------------------------------------------------------------------------------
+static_assert(LNMOD_MAX_AXES == lnmod::kMaxAxes && sizeof(lnmod_rotation::features) == sizeof(int32_t) * LNMOD_MAX_AXES, "axes");
+
+// one tensor's heads; 0 of them are a tensor that is not there
+bool valid_heads(int64_t heads, int64_t head_dim) {
+    return heads >= 0 && head_dim >= 8 && head_dim <= 256 && head_dim % 8 == 0 && heads <= (int64_t(1) << 20) / head_dim;
+}
+
+// What both tensors share: sizes, positions, table.
+int rotary_args(lnmod::RotaryArgs& a, int64_t B, int64_t S, int64_t q_heads, int64_t k_heads, int64_t head_dim,
+                const lnmod_rotation& r, int dtype) {
+    if (dtype != LNMOD_BF16 && dtype != LNMOD_F32) return LNMOD_EINVAL;
+    const int64_t N = total_tokens(B, S);
+    if (N < 0 || N >= (int64_t(1) << 31) || q_heads < 1 || k_heads < 0) return LNMOD_EINVAL;
+    if (r.axes < 1 || r.axes > LNMOD_MAX_AXES) return LNMOD_EINVAL;
+    int64_t width = 0;
+    for (int i = 0; i < r.axes; ++i) {
+        if (r.features[i] < 0) return LNMOD_EINVAL;
+        width += r.features[i];
+    }
+    if (!valid_heads(q_heads, head_dim) || !valid_heads(k_heads, head_dim)) return LNMOD_EUNSUPPORTED;
+    for (int i = 0; i < r.axes; ++i)
+        if (r.features[i] < 2 || r.features[i] % 2 != 0) return LNMOD_EUNSUPPORTED;
+    if (width > head_dim || (!r.interleaved && width % 8 != 0)) return LNMOD_EUNSUPPORTED;
+    a.N = N;
+    a.S = static_cast<int32_t>(S);
+    a.head_dim = static_cast<int32_t>(head_dim);
+    a.side[0].heads = static_cast<int32_t>(q_heads);
+    a.side[1].heads = static_cast<int32_t>(k_heads);
+    if (N == 0) return LNMOD_OK;
+    if (!r.positions || !r.table || r.table_rows < 1 || r.table_rows >= (int64_t(1) << 31)) return LNMOD_EINVAL;
+    if (r.position_rows != S && r.position_rows != N) return LNMOD_EINVAL;
+    if ((reinterpret_cast<uintptr_t>(r.table) & 7u) != 0 || (reinterpret_cast<uintptr_t>(r.positions) & 3u) != 0) return LNMOD_EALIGN;
+    a.rot.positions = r.positions;
+    a.rot.table = r.table;
+    a.rot.table_rows = static_cast<uint32_t>(r.table_rows);
+    a.rot.half = static_cast<int32_t>(width / 2);
+    a.rot.axes = r.axes;
+    a.rot.per_token = r.position_rows != S;
+    for (int i = 0, first = 0; i < LNMOD_MAX_AXES; ++i) {
+        a.rot.first[i] = i < r.axes ? first : INT32_MAX;
+        if (i < r.axes) first += r.features[i] / 2;
+    }
+    return LNMOD_OK;
+}
+
+int heads_view(lnmod::HeadsView& v, const lnmod_heads& h, int dtype) {
+    if (!h.data) return LNMOD_EINVAL;
+    const int64_t size = dtype == LNMOD_BF16 ? 2 : 4;
+    for (const int64_t s : {h.batch, h.token, h.head}) {
+        if (s < 0 || s > (int64_t(1) << 48)) return LNMOD_EINVAL;
+        if (s * size % 16 != 0) return LNMOD_EALIGN;
+    }
+    if (!aligned16(h.data)) return LNMOD_EALIGN;
+    v = {static_cast<const char*>(h.data), h.batch * size, h.token * size, h.head * size};
+    return LNMOD_OK;
+}
+
+// The features that a norm is over; false where a row is too wide for one.
+bool norm_widths(lnmod::RotaryArgs& a, int per_head) {
+    for (lnmod::RotarySide& s : a.side) {
+        s.width = per_head ? a.head_dim : a.head_dim * s.heads;
+        if (s.width > lnmod::kMaxD) return false;
+        s.inv_width = 1.0f / static_cast<float>(s.width);
+    }
+    return true;
 }
 
 }  // namespace
@@ -488,6 +557,145 @@ size_t lnmod_rmsnorm_quant_backward_workspace_bytes(int64_t N, int64_t D) {
     if (N < 0 || N >= (int64_t(1) << 31)) return 0;
     if (D < 8 || D > lnmod::kMaxD || D % 8 != 0) return 0;
     return rmsq_workspace_bytes(N, D);
+}
+
+int lnmod_quantize_rows(const void* x, int64_t N, int64_t D, void* stream, void* codes, float* code_scales, int dtype,
+                        int code) {
+    const int st = check_rows(N, D, 32, dtype, code);
+    if (st != LNMOD_OK) return st;
+    if (N == 0) return LNMOD_OK;
+    if (!x || !codes || !code_scales) return LNMOD_EINVAL;
+    if (!aligned16(x) || !aligned16(codes)) return LNMOD_EALIGN;
+    const hipError_t e = lnmod::launch_row_codes(dtype, code, x, N, D, codes, code_scales, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LNMOD_OK : LNMOD_ELAUNCH;
+}
+
+int lnmod_code_product(const void* a, const float* a_scales, const void* w, const float* w_scales, const void* bias,
+                       int64_t M, int64_t N, int64_t K, void* stream, void* y, int dtype, int code) {
+    constexpr int64_t kMost = int64_t(1) << 31;
+    if (M < 0 || M >= kMost || N < 0 || N >= kMost || K < 0 || !valid_code(code)) return LNMOD_EINVAL;
+    if (dtype != LNMOD_BF16 && dtype != LNMOD_F32) return LNMOD_EINVAL;
+    if (K < 8 || K >= (int64_t(1) << 17) || K % 8 != 0) return LNMOD_EUNSUPPORTED;
+    if (M == 0 || N == 0) return LNMOD_OK;
+    if (!a || !a_scales || !w || !w_scales || !y) return LNMOD_EINVAL;
+    if (!aligned16(a) || !aligned16(w) || !aligned16(y)) return LNMOD_EALIGN;
+    lnmod::ProductArgs p{a, a_scales, w, w_scales, bias, y, M, N, static_cast<int32_t>(K), 0, 0};
+    const hipError_t e = lnmod::launch_product(dtype, code, p, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LNMOD_OK : LNMOD_ELAUNCH;
+}
+
+int lnmod_rotary(const lnmod_heads* q, const lnmod_heads* k, int64_t B, int64_t S, int64_t q_heads, int64_t k_heads,
+                 int64_t head_dim, const lnmod_rotation* rotation, int inverse, void* stream, void* q_out, void* k_out,
+                 int dtype) {
+    const bool both = k_heads != 0;
+    if (!q || !rotation || (k != nullptr) != both || (k_out != nullptr) != both) return LNMOD_EINVAL;
+    lnmod::RotaryArgs a{};
+    const int st = rotary_args(a, B, S, q_heads, k_heads, head_dim, *rotation, dtype);
+    if (st != LNMOD_OK || a.N == 0) return st;
+    if (!q_out) return LNMOD_EINVAL;
+    const lnmod_heads* x[2] = {q, k};
+    void* y[2] = {q_out, k_out};
+    for (int t = 0; t < (both ? 2 : 1); ++t) {
+        const int v = heads_view(a.side[t].x, *x[t], dtype);
+        if (v != LNMOD_OK) return v;
+        if (!aligned16(y[t])) return LNMOD_EALIGN;
+        a.side[t].y = y[t];
+    }
+    a.sign = inverse ? -1.0f : 1.0f;
+    const hipError_t e = lnmod::launch_rotary_fwd(dtype, lnmod::kNoNorm, !rotation->interleaved, a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LNMOD_OK : LNMOD_ELAUNCH;
+}
+
+int lnmod_qknorm_rotary_forward(const lnmod_heads* q, const lnmod_heads* k, const void* wq, const void* wk, int64_t B,
+                                int64_t S, int64_t q_heads, int64_t k_heads, int64_t head_dim,
+                                const lnmod_rotation* rotation, float eps, int per_head, void* stream, void* q_out,
+                                void* k_out, float* rstd_q, float* rstd_k, int dtype) {
+    if (!q || !k || !rotation || q_heads == 0 || k_heads == 0) return LNMOD_EINVAL;
+    if (!(std::isfinite(eps) && eps > 0.0f)) return LNMOD_EINVAL;
+    lnmod::RotaryArgs a{};
+    const int st = rotary_args(a, B, S, q_heads, k_heads, head_dim, *rotation, dtype);
+    if (st != LNMOD_OK) return st;
+    if (!norm_widths(a, per_head)) return LNMOD_EUNSUPPORTED;
+    if (a.N == 0) return LNMOD_OK;
+    const lnmod_heads* x[2] = {q, k};
+    const void* w[2] = {wq, wk};
+    void* y[2] = {q_out, k_out};
+    float* rstd[2] = {rstd_q, rstd_k};
+    for (int t = 0; t < 2; ++t) {
+        if (!w[t] || !y[t] || !rstd[t]) return LNMOD_EINVAL;
+        const int v = heads_view(a.side[t].x, *x[t], dtype);
+        if (v != LNMOD_OK) return v;
+        if (!aligned16(w[t]) || !aligned16(y[t])) return LNMOD_EALIGN;
+        a.side[t].w = w[t];
+        a.side[t].y = y[t];
+        a.side[t].rstd = rstd[t];
+    }
+    a.eps = eps;
+    a.sign = 1.0f;
+    const hipError_t e = lnmod::launch_rotary_fwd(dtype, per_head ? lnmod::kHeadNorm : lnmod::kRowNorm, !rotation->interleaved, a,
+                                                  static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LNMOD_OK : LNMOD_ELAUNCH;
+}
+
+int lnmod_qknorm_rotary_backward(const lnmod_heads* dq_out, const lnmod_heads* dk_out, const lnmod_heads* q,
+                                 const lnmod_heads* k, const void* wq, const void* wk, int64_t B, int64_t S,
+                                 int64_t q_heads, int64_t k_heads, int64_t head_dim, const lnmod_rotation* rotation,
+                                 int per_head, void* stream, const float* rstd_q, const float* rstd_k, void* dq, void* dk,
+                                 void* dwq, void* dwk, void* workspace, size_t workspace_size, int dtype, int io_grads) {
+    if (!q || !k || !dq_out || !dk_out || !rotation || q_heads == 0 || k_heads == 0) return LNMOD_EINVAL;
+    lnmod::RotaryArgs a{};
+    const int st = rotary_args(a, B, S, q_heads, k_heads, head_dim, *rotation, dtype);
+    if (st != LNMOD_OK) return st;
+    if (!norm_widths(a, per_head)) return LNMOD_EUNSUPPORTED;
+    void* dw[2] = {dwq, dwk};
+    if (!dwq || !dwk) return LNMOD_EINVAL;
+    const hipStream_t hs = static_cast<hipStream_t>(stream);
+    if (a.N == 0) {                                           // empty sums are zeros
+        hipError_t e = hipSuccess;
+        for (int t = 0; t < 2; ++t) {
+            if (io_grads && !aligned16(dw[t])) return LNMOD_EALIGN;
+            if (e == hipSuccess) e = lnmod::launch_zero_f32(static_cast<float*>(dw[t]), grad_floats(a.side[t].width, dtype, io_grads != 0), hs);
+        }
+        return e == hipSuccess ? LNMOD_OK : LNMOD_ELAUNCH;
+    }
+    const lnmod_heads *x[2] = {q, k}, *g[2] = {dq_out, dk_out};
+    const void* w[2] = {wq, wk};
+    void* dx[2] = {dq, dk};
+    const float* rstd[2] = {rstd_q, rstd_k};
+    for (int t = 0; t < 2; ++t) {
+        if (!w[t] || !dx[t] || !rstd[t]) return LNMOD_EINVAL;
+        int v = heads_view(a.side[t].x, *x[t], dtype);
+        if (v == LNMOD_OK) v = heads_view(a.side[t].dy, *g[t], dtype);
+        if (v != LNMOD_OK) return v;
+        if (!aligned16(w[t]) || !aligned16(dx[t]) || (io_grads && !aligned16(dw[t]))) return LNMOD_EALIGN;
+        a.side[t].w = w[t];
+        a.side[t].y = dx[t];
+        a.side[t].rstd = const_cast<float*>(rstd[t]);
+    }
+    if (!workspace || workspace_size < lnmod_qknorm_rotary_backward_workspace_bytes(a.N, q_heads, k_heads, head_dim, per_head))
+        return LNMOD_EWORKSPACE;
+    if (!aligned16(workspace)) return LNMOD_EALIGN;
+    const hipError_t e = lnmod::launch_rotary_bwd(dtype, per_head ? lnmod::kHeadNorm : lnmod::kRowNorm, !rotation->interleaved, a, dw,
+                                                  io_grads != 0, static_cast<float*>(workspace), hs);
+    return e == hipSuccess ? LNMOD_OK : LNMOD_ELAUNCH;
+}
+
+size_t lnmod_qknorm_rotary_backward_workspace_bytes(int64_t tokens, int64_t q_heads, int64_t k_heads, int64_t head_dim,
+                                                    int per_head) {
+    if (tokens < 0 || tokens >= (int64_t(1) << 31) || !valid_heads(q_heads, head_dim) || !valid_heads(k_heads, head_dim)) return 0;
+    if (q_heads == 0 || k_heads == 0) return 0;
+    if (!per_head && (q_heads * head_dim > lnmod::kMaxD || k_heads * head_dim > lnmod::kMaxD)) return 0;
+    const int32_t heads[2] = {static_cast<int32_t>(q_heads), static_cast<int32_t>(k_heads)};
+    const int norm = per_head ? lnmod::kHeadNorm : lnmod::kRowNorm;
+    int64_t most = 0;
+    for (int dtype = 0; dtype < 2; ++dtype) {
+        int64_t slots[2];
+        lnmod::rotary_bwd_slots(dtype, tokens, heads, static_cast<int>(head_dim), norm, slots);
+        int64_t floats = 0;
+        for (int t = 0; t < 2; ++t) floats += slots[t] * head_dim * (per_head ? 1 : heads[t]);
+        if (floats > most) most = floats;
+    }
+    return static_cast<size_t>(most) * sizeof(float);
 }
 
 }  // extern "C"

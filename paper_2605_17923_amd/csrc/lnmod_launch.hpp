@@ -908,4 +908,20 @@ hipError_t launch_rmsq_bwd(int dtype, const void* dy, const void* dh, const void
                            const float* rstd, void* dx, void* dr, void* dw, bool io_grads, float* ws, hipStream_t st,
                            const Shape* force = nullptr);
 
+// Codes with one scale for a row, and their product.
+hipError_t launch_row_codes(int dtype, int code, const void* x, int64_t N, int64_t D, void* codes, float* scales, hipStream_t st);
+struct ProductArgs {
+    const void* a;             // [M, K] codes
+    const float* sa;           // [M]
+    const void* w;             // [N, K] codes
+    const float* sw;           // [N]
+    const void* bias;          // [N] in y's type, or nullptr
+    void* y;                   // [M, N]
+    int64_t M, N;
+    int32_t K;
+    int32_t tiles_m;           // set by the launcher
+    int64_t tiles;
+};
+hipError_t launch_product(int dtype, int code, const ProductArgs& a, hipStream_t st);
+
 }  // namespace lnmod

@@ -99,6 +99,7 @@ Tensor scratch(size_t bytes, const Tensor& x) {
 py::object to_python(const Tensor& t) { return t.defined() ? py::cast(t) : py::none(); }
 py::object to_python(double v) { return py::float_(v); }
 py::object to_python(int64_t v) { return py::int_(v); }
+py::object to_python(const std::vector<int64_t>& v) { return py::cast(v); }
 
 // name(args...) of functional.py, with None for an undefined tensor.  Runs on a thread of the autograd engine,
 // without the interpreter lock: no Python object is made before it is taken here.  The function's exception (a ValueError of a check, an LnmodError) is kept
@@ -475,6 +476,213 @@ struct RmsNormQuant : public torch::autograd::Function<RmsNormQuant> {
     }
 };
 
+// ---- codes with one scale for a row, and their product ---------------------------------------------------------
+variable_list quantize_rows_call(const Tensor& x, int code) {
+    if (!plain_first(x) || x.dim() < 1) throw NotPlain();
+    Tensor codes = fresh(x.sizes(), type_of_code(code), x);
+    Tensor scales = fresh(x.sizes().slice(0, x.dim() - 1), at::kFloat, x);
+    if (lnmod_quantize_rows(ptr(x), rows_of(x), x.size(-1), stream_of(x), out(codes), f32_out(scales), code_of(x), code) != LNMOD_OK)
+        throw NotPlain();
+    return {codes, scales};
+}
+
+variable_list code_product_call(const Tensor& codes, const Tensor& scales, const Tensor& w, const Tensor& w_scales,
+                                const Tensor& bias, at::ScalarType type) {
+    if (!codes.defined() || !codes.is_cuda() || codes.device().index() != c10::hip::current_device() || codes.dim() < 1 ||
+        !plain_codes(codes, codes.sizes(), codes.device()) || !w.defined() || w.dim() != 2 || (type != at::kBFloat16 && type != at::kFloat))
+        throw NotPlain();
+    const at::Device dev = codes.device();
+    const int64_t K = codes.size(-1), N = w.size(0);
+    const int64_t weight[] = {N, K};
+    if (!plain(scales, codes.sizes().slice(0, codes.dim() - 1), at::kFloat, dev) || !plain(w, at::IntArrayRef(weight, 2), codes.scalar_type(), dev) ||
+        !plain(w_scales, at::IntArrayRef(&N, 1), at::kFloat, dev) || (bias.defined() && !plain(bias, at::IntArrayRef(&N, 1), type, dev)))
+        throw NotPlain();
+    std::vector<int64_t> shape = codes.sizes().vec();
+    shape.back() = N;
+    Tensor y = fresh(shape, type, codes);
+    if (lnmod_code_product(ptr(codes), f32(scales), ptr(w), f32(w_scales), ptr(bias), rows_of(codes), N, K, stream_of(codes),
+                           out(y), code_of(y), code_of_codes(codes)) != LNMOD_OK)
+        throw NotPlain();
+    return {y};
+}
+
+// ---- rotary positions ------------------------------------------------------------------------------------------
+// A tensor [.., tokens, heads, features] as the kernels can read it, or false.
+bool heads_of(const Tensor& t, at::IntArrayRef shape, at::ScalarType type, const at::Device& dev, lnmod_heads* h) {
+    if (!t.defined() || t.layout() != at::kStrided || t.device() != dev || t.scalar_type() != type ||
+        (t.key_set() & kSpecial).has_any(kSpecial) || t.sizes() != shape)
+        return false;
+    if (t.numel() == 0) {
+        *h = {nullptr, 0, 0, 0};
+        return true;
+    }
+    const int64_t step = 16 / static_cast<int64_t>(t.element_size()), n = t.dim();
+    if (t.size(-1) > 1 && t.stride(-1) != 1) return false;
+    int64_t stride[3] = {0, 0, 0};
+    for (int64_t d = 0; d < n - 1; ++d) {
+        const int64_t s = t.size(d) == 1 ? 0 : t.stride(d);
+        if (s % step != 0) return false;
+        stride[d + 4 - n] = s;
+    }
+    h->data = t.const_data_ptr();
+    if (reinterpret_cast<uintptr_t>(h->data) % 16 != 0) return false;
+    h->batch = stride[0];
+    h->token = stride[1];
+    h->head = stride[2];
+    return true;
+}
+
+// What both operators share.
+struct RotaryCall {
+    lnmod_heads q, k;
+    lnmod_rotation rot;
+    int64_t B, S, heads, kv, hd;
+};
+
+bool rotary_of(const Tensor& q, const Tensor& k, const Tensor& positions, const Tensor& table, const std::vector<int64_t>& axes,
+               bool interleaved, RotaryCall* c) {
+    if (!q.defined() || !q.is_cuda() || (q.scalar_type() != at::kBFloat16 && q.scalar_type() != at::kFloat) ||
+        q.device().index() != c10::hip::current_device() || (q.dim() != 3 && q.dim() != 4) || axes.empty() || axes.size() > LNMOD_MAX_AXES)
+        return false;
+    const at::Device dev = q.device();
+    std::vector<int64_t> shape = q.sizes().vec();
+    c->hd = shape.back();
+    c->heads = shape[shape.size() - 2];
+    c->kv = 0;
+    if (!heads_of(q, shape, q.scalar_type(), dev, &c->q)) return false;
+    if (k.defined()) {
+        if (k.dim() != q.dim()) return false;
+        c->kv = shape[shape.size() - 2] = k.size(-2);
+        if (c->kv == 0 || !heads_of(k, shape, q.scalar_type(), dev, &c->k)) return false;
+    }
+    c->B = q.dim() == 4 ? q.size(0) : 1;
+    c->S = q.size(-3);
+    if (!positions.defined() || positions.dim() < 2) return false;
+    const bool shared = q.dim() == 4 && positions.dim() == 2;
+    std::vector<int64_t> rows = q.sizes().slice(shared ? 1 : 0, shared ? 1 : q.dim() - 2).vec();
+    rows.push_back(static_cast<int64_t>(axes.size()));
+    int64_t width = 0;
+    for (const int64_t d : axes) {
+        if (d < 2 || d > c->hd) return false;
+        width += d;
+    }
+    if (!plain(positions, rows, at::kInt, dev) || !table.defined() || table.dim() != 3) return false;
+    const int64_t entries[] = {table.size(0), width / 2, 2};
+    if (!plain(table, at::IntArrayRef(entries, 3), at::kFloat, dev)) return false;
+    c->rot = {positions.const_data_ptr<int32_t>(), shared ? c->S : c->B * c->S, f32(table), table.size(0),
+              static_cast<int32_t>(axes.size()), {0, 0, 0, 0}, interleaved ? 1 : 0};
+    for (size_t i = 0; i < axes.size(); ++i) c->rot.features[i] = static_cast<int32_t>(axes[i]);
+    return true;
+}
+
+// A gradient as the kernels can read it.
+Tensor readable(const Tensor& t) {
+    lnmod_heads h;
+    return t.defined() && t.layout() == at::kStrided && heads_of(t, t.sizes(), t.scalar_type(), t.device(), &h) ? t : t.contiguous();
+}
+
+// both results (the second undefined without k); empty where the call is not the plain case
+variable_list rotary_run(const Tensor& q, const Tensor& k, const Tensor& positions, const Tensor& table,
+                         const std::vector<int64_t>& axes, bool interleaved, bool inverse) {
+    RotaryCall c;
+    if (!rotary_of(q, k, positions, table, axes, interleaved, &c)) return {};
+    Tensor qo = fresh_like(q), ko = k.defined() ? fresh_like(k) : Tensor();
+    const int st = lnmod_rotary(&c.q, k.defined() ? &c.k : nullptr, c.B, c.S, c.heads, c.kv, c.hd, &c.rot, inverse ? 1 : 0,
+                                stream_of(q), out(qo), k.defined() ? out(ko) : nullptr, code_of(q));
+    return st == LNMOD_OK ? variable_list{qo, ko} : variable_list{};
+}
+
+c10::List<int64_t> axes_list(const std::vector<int64_t>& axes) { return c10::List<int64_t>(at::IntArrayRef(axes)); }
+
+struct Rotary : public torch::autograd::Function<Rotary> {
+    static variable_list forward(AutogradContext* ctx, const Tensor& q, const std::optional<Tensor>& k, const Tensor& positions,
+                                 const Tensor& table, const std::vector<int64_t>& axes, bool interleaved) {
+        variable_list r = rotary_run(q, k.value_or(Tensor()), positions, table, axes, interleaved, false);
+        if (r.empty()) throw NotPlain();
+        ctx->saved_data["axes"] = axes_list(axes);
+        ctx->saved_data["interleaved"] = interleaved;
+        ctx->save_for_backward({positions, table});
+        if (!r[1].defined()) r.pop_back();
+        return r;
+    }
+
+    static variable_list backward(AutogradContext* ctx, variable_list grads) {
+        const variable_list s = ctx->get_saved_variables();
+        const std::vector<int64_t> axes = ctx->saved_data["axes"].toIntVector();
+        const bool interleaved = ctx->saved_data["interleaved"].toBool();
+        const Tensor dq = readable(grads[0]), dk = grads.size() > 1 ? readable(grads[1]) : Tensor();
+        variable_list r;
+        if (plain_state()) r = rotary_run(dq, dk, s[0], s[1], axes, interleaved, true);
+        if (r.empty()) {
+            r = python_backward("_rotary_backward", dk.defined() ? 2 : 1, dq, dk, s[0], s[1], axes, static_cast<int64_t>(interleaved));
+            r.resize(2);
+        }
+        return {r[0], r[1], Tensor(), Tensor(), Tensor(), Tensor()};
+    }
+};
+
+// whether each head has the norm, or its tokens; false where the weights are neither's
+bool qk_weights(const Tensor& q, const Tensor& wq, const Tensor& wk, const RotaryCall& c, bool* per_head) {
+    if (!wq.defined() || !wk.defined() || wq.dim() != 1 || wk.dim() != 1) return false;
+    *per_head = wq.size(0) == c.hd && wk.size(0) == c.hd;
+    const int64_t nq = *per_head ? c.hd : c.heads * c.hd, nk = *per_head ? c.hd : c.kv * c.hd;
+    return plain(wq, at::IntArrayRef(&nq, 1), q.scalar_type(), q.device()) && plain(wk, at::IntArrayRef(&nk, 1), q.scalar_type(), q.device());
+}
+
+// q and k, normed and turned, and 1 / root of both; throws NotPlain
+variable_list qk_rotary_forward(const Tensor& q, const Tensor& k, const Tensor& wq, const Tensor& wk, const Tensor& positions,
+                                const Tensor& table, const std::vector<int64_t>& axes, bool interleaved, double eps) {
+    RotaryCall c;
+    bool per_head;
+    if (!k.defined() || !rotary_of(q, k, positions, table, axes, interleaved, &c) || !qk_weights(q, wq, wk, c, &per_head)) throw NotPlain();
+    const int64_t lead = q.dim() - (per_head ? 1 : 2);
+    Tensor qo = fresh_like(q), ko = fresh_like(k);
+    Tensor rq = fresh(q.sizes().slice(0, lead), at::kFloat, q), rk = fresh(k.sizes().slice(0, lead), at::kFloat, q);
+    const int st = lnmod_qknorm_rotary_forward(&c.q, &c.k, ptr(wq), ptr(wk), c.B, c.S, c.heads, c.kv, c.hd, &c.rot,
+                                               static_cast<float>(eps), per_head, stream_of(q), out(qo), out(ko), f32_out(rq),
+                                               f32_out(rk), code_of(q));
+    if (st != LNMOD_OK) throw NotPlain();
+    return {qo, ko, rq, rk};
+}
+
+struct QkNormRotary : public torch::autograd::Function<QkNormRotary> {
+    static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& wq, const Tensor& wk,
+                                 const Tensor& positions, const Tensor& table, const std::vector<int64_t>& axes, bool interleaved,
+                                 double eps) {
+        const variable_list r = qk_rotary_forward(q, k, wq, wk, positions, table, axes, interleaved, eps);
+        ctx->saved_data["axes"] = axes_list(axes);
+        ctx->saved_data["interleaved"] = interleaved;
+        ctx->save_for_backward({q, k, wq, wk, r[2], r[3], positions, table});
+        return {r[0], r[1]};
+    }
+
+    static variable_list backward(AutogradContext* ctx, variable_list grads) {
+        const variable_list s = ctx->get_saved_variables();
+        const Tensor &q = s[0], &k = s[1], &wq = s[2], &wk = s[3], &rq = s[4], &rk = s[5], &positions = s[6], &table = s[7];
+        const std::vector<int64_t> axes = ctx->saved_data["axes"].toIntVector();
+        const bool interleaved = ctx->saved_data["interleaved"].toBool();
+        const Tensor dqr = readable(grads[0]), dkr = readable(grads[1]);
+        RotaryCall c;
+        lnmod_heads gq, gk;
+        bool per_head;
+        if (plain_state() && rotary_of(q, k, positions, table, axes, interleaved, &c) && qk_weights(q, wq, wk, c, &per_head) &&
+            heads_of(dqr, q.sizes(), q.scalar_type(), q.device(), &gq) && heads_of(dkr, k.sizes(), q.scalar_type(), q.device(), &gk) &&
+            plain(rq, q.sizes().slice(0, q.dim() - (per_head ? 1 : 2)), at::kFloat, q.device()) &&
+            plain(rk, k.sizes().slice(0, k.dim() - (per_head ? 1 : 2)), at::kFloat, q.device())) {
+            Tensor dq = fresh_like(q), dk = fresh_like(k), dwq = fresh_like(wq), dwk = fresh_like(wk);
+            const Tensor ws = fresh_bytes(lnmod_qknorm_rotary_backward_workspace_bytes(c.B * c.S, c.heads, c.kv, c.hd, per_head), q);
+            const int st = lnmod_qknorm_rotary_backward(&gq, &gk, &c.q, &c.k, ptr(wq), ptr(wk), c.B, c.S, c.heads, c.kv, c.hd, &c.rot,
+                                                        per_head, stream_of(q), f32(rq), f32(rk), out(dq), out(dk), out(dwq),
+                                                        out(dwk), out(ws), static_cast<size_t>(ws.numel()), code_of(q), 1);
+            if (st == LNMOD_OK) return {dq, dk, dwq, dwk, Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+        }
+        variable_list r = python_backward("_qk_rotary_backward", 4, dqr, dkr, q, k, wq, wk, rq, rk, positions, table, axes,
+                                          static_cast<int64_t>(interleaved));
+        r.resize(9);
+        return r;
+    }
+};
+
 // ---- Python entry points: None where the call is left to the Python path ------------------------------------
 template <typename F>
 py::object attempt(const std::vector<py::object>& tensors, const py::object& cu, F&& call) {
@@ -492,7 +700,7 @@ py::object attempt(const std::vector<py::object>& tensors, const py::object& cu,
     }
     if (r.size() == 1) return py::cast(r[0]);
     py::tuple t(r.size());
-    for (size_t i = 0; i < r.size(); ++i) t[i] = py::cast(r[i]);
+    for (size_t i = 0; i < r.size(); ++i) t[i] = to_python(r[i]);
     return t;
 }
 
@@ -605,6 +813,79 @@ py::object rms_norm_quant(const py::object& x, const py::object& w, const py::ob
     });
 }
 
+py::object quantize_rows(const py::object& x, const py::object& code) {
+    const int c = code_number(code);
+    if (c < 0) return py::none();
+    return attempt({x}, py::none(), [&] { return quantize_rows_call(unpack(x), c); });
+}
+
+// attempt() checks the optional tensor of these calls as it does cu_seqlens
+py::object code_product(const py::object& codes, const py::object& scales, const py::object& w, const py::object& w_scales,
+                        const py::object& bias, const py::object& dtype) {
+    if (!THPDtype_Check(dtype.ptr())) return py::none();
+    const at::ScalarType type = reinterpret_cast<THPDtype*>(dtype.ptr())->scalar_type;
+    return attempt({codes, scales, w, w_scales}, bias, [&] {
+        return code_product_call(unpack(codes), unpack(scales), unpack(w), unpack(w_scales), unpack_or(bias).value_or(Tensor()), type);
+    });
+}
+
+// the features of each axis; empty where they are no tuple of numbers
+std::vector<int64_t> axes_number(const py::object& axes) {
+    std::vector<int64_t> v;
+    if (!PyTuple_CheckExact(axes.ptr())) return v;
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(axes.ptr()); ++i) {
+        PyObject* o = PyTuple_GET_ITEM(axes.ptr(), i);
+        const long d = PyLong_CheckExact(o) ? PyLong_AsLong(o) : -1;
+        if (d == -1 && PyErr_Occurred()) PyErr_Clear();
+        if (d < 2) return {};
+        v.push_back(d);
+    }
+    return v;
+}
+
+py::object rotary_call(const py::object& q, const py::object& k, const py::object& positions, const py::object& table,
+                       const py::object& axes, const py::object& interleaved, bool inverse) {
+    const std::vector<int64_t> v = axes_number(axes);
+    if (v.empty() || !PyBool_Check(interleaved.ptr())) return py::none();
+    return attempt({q, positions, table}, k, [&] {
+        variable_list r = rotary_run(unpack(q), unpack_or(k).value_or(Tensor()), unpack(positions), unpack(table), v,
+                                     interleaved.ptr() == Py_True, inverse);
+        if (r.empty()) throw NotPlain();
+        return r;
+    });
+}
+
+py::object rotary(const py::object& q, const py::object& k, const py::object& positions, const py::object& table,
+                  const py::object& axes, const py::object& interleaved) {
+    const std::vector<int64_t> v = axes_number(axes);
+    if (v.empty() || !PyBool_Check(interleaved.ptr())) return py::none();
+    return attempt({q, positions, table}, k, [&] {
+        return Rotary::apply(unpack(q), unpack_or(k), unpack(positions), unpack(table), v, interleaved.ptr() == Py_True);
+    });
+}
+
+py::object qknorm_rotary_forward(const py::object& q, const py::object& k, const py::object& wq, const py::object& wk,
+                                 const py::object& positions, const py::object& table, const py::object& axes,
+                                 const py::object& interleaved, double eps) {
+    const std::vector<int64_t> v = axes_number(axes);
+    if (v.empty() || !PyBool_Check(interleaved.ptr())) return py::none();
+    return attempt({q, k, wq, wk, positions, table}, py::none(), [&] {
+        return qk_rotary_forward(unpack(q), unpack(k), unpack(wq), unpack(wk), unpack(positions), unpack(table), v,
+                                 interleaved.ptr() == Py_True, eps);
+    });
+}
+
+py::object qk_norm_rotary(const py::object& q, const py::object& k, const py::object& wq, const py::object& wk,
+                          const py::object& positions, const py::object& table, const py::object& axes,
+                          const py::object& interleaved, double eps) {
+    const std::vector<int64_t> v = axes_number(axes);
+    if (v.empty() || !PyBool_Check(interleaved.ptr())) return py::none();
+    return attempt({q, k, wq, wk, positions, table}, py::none(), [&] {
+        return QkNormRotary::apply(unpack(q), unpack(k), unpack(wq), unpack(wk), unpack(positions), unpack(table), v,
+                                   interleaved.ptr() == Py_True, eps);
+    });
+}
+
 // ---- what y.grad_fn shows --------------------------------------------------------------------------------------
 // The node's Python type, with the saved tensors that the Python classes' nodes show (the same ones in the same order,
 // None where nothing was saved; an error once the backward has freed them).
@@ -640,6 +921,8 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
     register_node<QkNorm>("QkNormBackward");
     register_node<LnModulateCkpt>("LnModulateCkptBackward");
     register_node<RmsNormQuant>("RmsNormQuantBackward");
+    register_node<Rotary>("RotaryBackward");
+    register_node<QkNormRotary>("QkNormRotaryBackward");
     m.def("forward", &forward);
     m.def("ln_modulate", &ln_modulate);
     m.def("gated_ln_modulate", &gated_ln_modulate);
@@ -651,4 +934,10 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
     m.def("rmsnorm_quant_forward", &rmsnorm_quant_forward);
     m.def("rmsnorm_quant_backward", &rmsnorm_quant_backward);
     m.def("rms_norm_quant", &rms_norm_quant);
+    m.def("quantize_rows", &quantize_rows);
+    m.def("code_product", &code_product);
+    m.def("rotary_call", &rotary_call);
+    m.def("rotary", &rotary);
+    m.def("qknorm_rotary_forward", &qknorm_rotary_forward);
+    m.def("qk_norm_rotary", &qk_norm_rotary);
 }

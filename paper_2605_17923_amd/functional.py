@@ -3,7 +3,7 @@
 Everything numerical runs in the HIP kernels; the functions allocate outputs with torch and
 keep what the backward needs; the kernels round the float32 sums of the parameter gradients to the
 parameters' dtype where they form them.
-Inputs must be contiguous CUDA tensors in bfloat16 or float32; work is enqueued on torch's
+Inputs must be contiguous CUDA tensors in bfloat16 or float32 (q and k of the rotations may be strided views); work is enqueued on torch's
 current stream.  Without the built library every call raises (there is no fallback).
 
 Ordinary calls run the autograd function of the C++ extension module (csrc/lnmod_torch.cpp).  The classes
@@ -17,6 +17,8 @@ the errors), tensor subclasses, functorch transforms, dispatch modes, tracers.
     y        = ln_modulate_ckpt(x, shift, scale)                 ln_modulate that keeps x in 8 bits for the backward
     y        = rms_norm_quant(x, w)                              RMS norm with weight, rounded to 8 bits and back
     h, y     = rms_norm_quant(x, w, residual)                    h = x + residual first
+    qr, kr   = rotary(q, k, positions, table, axes)              rotary positions with several axes
+    qr, kr   = qk_norm_rotary(q, k, wq, wk, positions, table, axes)   qk_norm and the rotation in one pass
 """
 import torch
 
@@ -185,3 +187,66 @@ def rms_norm_quant(x, w, residual=None, eps=1e-6, code="e4m3", group=0):
     host = lnmod.native()
     r = None if host is None else host.rms_norm_quant(x, w, residual, float(eps), code, group)
     return _RmsNormQuant.apply(x, w, residual, float(eps), code, group) if r is None else r
+
+
+def _readable(t):
+    """A gradient as the kernels can read it."""
+    return t if t.layout == torch.strided and lnmod._heads_strides(t) is not None else t.contiguous()
+
+
+def _rotary_backward(dq, dk, positions, table, axes, interleaved):
+    return lnmod.rotary(_readable(dq), None if dk is None else _readable(dk), positions, table, tuple(axes), bool(interleaved),
+                        inverse=True)
+
+
+class _Rotary(torch.autograd.Function):
+    """The rotation; its gradient is the rotation backwards."""
+
+    @staticmethod
+    def forward(ctx, q, k, positions, table, axes, interleaved):
+        qr, kr = lnmod.rotary(q, k, positions, table, axes, interleaved)
+        ctx.save_for_backward(positions, table)
+        ctx.axes, ctx.interleaved = axes, interleaved
+        return qr if k is None else (qr, kr)
+
+    @staticmethod
+    def backward(ctx, dq, dk=None):
+        positions, table = ctx.saved_tensors
+        return _rotary_backward(dq, dk, positions, table, ctx.axes, ctx.interleaved) + (None,) * 4
+
+
+def rotary(q, k, positions, table, axes, interleaved=True):
+    """Rotary positions with several axes of q and k, [B, S, heads, head_dim] or packed [T, heads, head_dim]; k may be None,
+    and one tensor is returned then.  See lnmod.rotary, lnmod.rotary_table and lnmod.rotary_grid."""
+    host = lnmod.native()
+    r = None if host is None else host.rotary(q, k, positions, table, axes, interleaved)
+    return _Rotary.apply(q, k, positions, table, axes, interleaved) if r is None else r
+
+
+def _qk_rotary_backward(dqr, dkr, q, k, wq, wk, rq, rk, positions, table, axes, interleaved):
+    return lnmod._qknorm_rotary_backward(_readable(dqr), _readable(dkr), q, k, wq, wk, rq, rk, positions, table, tuple(axes),
+                                         bool(interleaved), io_grads=True)
+
+
+class _QkNormRotary(torch.autograd.Function):
+    """Q-Norm + K-Norm and the rotation."""
+
+    @staticmethod
+    def forward(ctx, q, k, wq, wk, positions, table, axes, interleaved, eps):
+        qr, kr, rq, rk = lnmod.qknorm_rotary_forward(q, k, wq, wk, positions, table, axes, interleaved, eps)
+        ctx.save_for_backward(q, k, wq, wk, rq, rk, positions, table)
+        ctx.axes, ctx.interleaved = axes, interleaved
+        return qr, kr
+
+    @staticmethod
+    def backward(ctx, dqr, dkr):
+        q, k, wq, wk, rq, rk, positions, table = ctx.saved_tensors
+        return _qk_rotary_backward(dqr, dkr, q, k, wq, wk, rq, rk, positions, table, ctx.axes, ctx.interleaved) + (None,) * 5
+
+
+def qk_norm_rotary(q, k, wq, wk, positions, table, axes, interleaved=True, eps=1e-6):
+    """rotary(qk_norm(...)) in one pass, rounded once.  wq, wk: [heads * head_dim] of each tensor (the norm is over a token's
+    whole row), or both [head_dim] (over each head)."""
+    host = lnmod.native()
+    r = None if host is None else host.qk_norm_rotary(q, k, wq, wk, positions, table, axes, interleaved, float(eps))
+    return _QkNormRotary.apply(q, k, wq, wk, positions, table, axes, interleaved, float(eps)) if r is None else r

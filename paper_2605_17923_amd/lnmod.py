@@ -31,10 +31,25 @@ EXPORTS = ("lnmod_forward", "lnmod_backward", "lnmod_forward_varlen", "lnmod_bac
            "lnmod_dequantize", "lnmod_forward_ckpt", "lnmod_backward_ckpt", "lnmod_backward_ckpt_workspace_bytes",
            "lnmod_rmsnorm_quant_forward", "lnmod_rmsnorm_quant_backward",
            "lnmod_rmsnorm_quant_backward_residual",
-           "lnmod_rmsnorm_quant_backward_workspace_bytes")
+           "lnmod_rmsnorm_quant_backward_workspace_bytes", "lnmod_quantize_rows", "lnmod_code_product",
+           "lnmod_rotary", "lnmod_qknorm_rotary_forward", "lnmod_qknorm_rotary_backward",
+           "lnmod_qknorm_rotary_backward_workspace_bytes")
+MAX_AXES = 4
 
 _lib = None
 _native = None
+
+
+class Heads(ctypes.Structure):
+    """lnmod_heads: a tensor [B, S, heads, head_dim] with dense features, strides in elements."""
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class Rotation(ctypes.Structure):
+    """lnmod_rotation: positions, table and the features of each axis."""
+    _fields_ = [("positions", ctypes.c_void_p), ("position_rows", ctypes.c_int64), ("table", ctypes.c_void_p),
+                ("table_rows", ctypes.c_int64), ("axes", ctypes.c_int32), ("features", ctypes.c_int32 * MAX_AXES),
+                ("interleaved", ctypes.c_int32)]
 
 
 class LnmodError(RuntimeError):
@@ -114,6 +129,21 @@ def library() -> ctypes.CDLL:
     lib.lnmod_rmsnorm_quant_backward_residual.argtypes = [vp, vp, vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, sz, cint, cint]
     lib.lnmod_rmsnorm_quant_backward_workspace_bytes.restype = sz
     lib.lnmod_rmsnorm_quant_backward_workspace_bytes.argtypes = [i64, i64]
+    heads, rot = ctypes.POINTER(Heads), ctypes.POINTER(Rotation)
+    lib.lnmod_quantize_rows.restype = cint
+    lib.lnmod_quantize_rows.argtypes = [vp, i64, i64, vp, vp, vp, cint, cint]
+    lib.lnmod_code_product.restype = cint
+    lib.lnmod_code_product.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, vp, vp, cint, cint]
+    lib.lnmod_rotary.restype = cint
+    lib.lnmod_rotary.argtypes = [heads, heads, i64, i64, i64, i64, i64, rot, cint, vp, vp, vp, cint]
+    lib.lnmod_qknorm_rotary_forward.restype = cint
+    lib.lnmod_qknorm_rotary_forward.argtypes = [heads, heads, vp, vp, i64, i64, i64, i64, i64, rot, f32, cint, vp, vp, vp,
+                                                vp, vp, cint]
+    lib.lnmod_qknorm_rotary_backward.restype = cint
+    lib.lnmod_qknorm_rotary_backward.argtypes = [heads, heads, heads, heads, vp, vp, i64, i64, i64, i64, i64, rot, cint, vp,
+                                                 vp, vp, vp, vp, vp, vp, vp, sz, cint, cint]
+    lib.lnmod_qknorm_rotary_backward_workspace_bytes.restype = sz
+    lib.lnmod_qknorm_rotary_backward_workspace_bytes.argtypes = [i64, i64, i64, i64, cint]
     _lib = lib
     return lib
 
@@ -319,6 +349,44 @@ def lnmod_rmsnorm_quant_backward_residual(dy, dh, h, w, N, D, stream, rstd, dx, 
 
 def lnmod_rmsnorm_quant_backward_workspace_bytes(N, D):
     return int(library().lnmod_rmsnorm_quant_backward_workspace_bytes(N, D))
+
+
+def lnmod_quantize_rows(x, N, D, stream, codes, code_scales, dtype, code):
+    return library().lnmod_quantize_rows(_p(x), N, D, stream, _p(codes), _p(code_scales), dtype, code)
+
+
+def lnmod_code_product(a, a_scales, w, w_scales, bias, M, N, K, stream, y, dtype, code):
+    return library().lnmod_code_product(_p(a), _p(a_scales), _p(w), _p(w_scales), _p(bias), M, N, K, stream, _p(y), dtype,
+                                        code)
+
+
+def _ref(struct):
+    return None if struct is None else ctypes.byref(struct)
+
+
+def lnmod_rotary(q, k, B, S, q_heads, k_heads, head_dim, rotation, inverse, stream, q_out, k_out, dtype):
+    """q, k: Heads or None;  rotation: Rotation."""
+    return library().lnmod_rotary(_ref(q), _ref(k), B, S, q_heads, k_heads, head_dim, _ref(rotation), inverse, stream,
+                                  _p(q_out), _p(k_out), dtype)
+
+
+def lnmod_qknorm_rotary_forward(q, k, wq, wk, B, S, q_heads, k_heads, head_dim, rotation, eps, per_head, stream, q_out,
+                                k_out, rstd_q, rstd_k, dtype):
+    return library().lnmod_qknorm_rotary_forward(_ref(q), _ref(k), _p(wq), _p(wk), B, S, q_heads, k_heads, head_dim,
+                                                 _ref(rotation), eps, per_head, stream, _p(q_out), _p(k_out), _p(rstd_q),
+                                                 _p(rstd_k), dtype)
+
+
+def lnmod_qknorm_rotary_backward(dq_out, dk_out, q, k, wq, wk, B, S, q_heads, k_heads, head_dim, rotation, per_head, stream,
+                                 rstd_q, rstd_k, dq, dk, dwq, dwk, workspace, workspace_bytes, dtype, io_grads):
+    return library().lnmod_qknorm_rotary_backward(_ref(dq_out), _ref(dk_out), _ref(q), _ref(k), _p(wq), _p(wk), B, S,
+                                                  q_heads, k_heads, head_dim, _ref(rotation), per_head, stream, _p(rstd_q),
+                                                  _p(rstd_k), _p(dq), _p(dk), _p(dwq), _p(dwk), _p(workspace),
+                                                  workspace_bytes, dtype, io_grads)
+
+
+def lnmod_qknorm_rotary_backward_workspace_bytes(tokens, q_heads, k_heads, head_dim, per_head):
+    return int(library().lnmod_qknorm_rotary_backward_workspace_bytes(tokens, q_heads, k_heads, head_dim, per_head))
 
 
 # ---- conveniences: check the tensors, allocate outputs with torch, raise on a non-zero status ---
@@ -1001,3 +1069,251 @@ def _rmsnorm_quant_backward(dy, h, w, rstd, dh, stream=None, ws=None, io_grads=F
             _check(lnmod_rmsnorm_quant_backward(dy, dh, h, w, N, D, handle, rstd, dx, dw, ws, ws.numel(), dt,
                                                 int(io_grads)), "lnmod_rmsnorm_quant_backward")
     return dx, dw, dr
+
+
+# ---- codes with one scale for a row, and their product -----------------------------------------------
+def quantize_rows(x, code="int8", stream=None):
+    """Codes of x [..., D] (D a multiple of 8) with one scale for a row, as code_product() reads them -> codes (int8, or
+    float8_e4m3fn for "e4m3", shaped like x) and scales (float32 [...]).  dequantize(..., group=0) is the way back."""
+    import torch
+    host = _host(x, stream)
+    r = None if host is None else host.quantize_rows(x, code)
+    if r is not None:
+        return r
+    number, kind = _code_of(code)
+    a = _Args(x)
+    dt = _dtype_code(x)
+    N, D = _rows(x, "x")
+    a.expect("x", x, x.shape)
+    a.on_gpu()
+    with _on_device(x, stream) as handle:
+        codes = torch.empty(x.shape, dtype=kind, device=x.device)
+        scales = torch.empty(_scales_shape(x.shape, 0), dtype=torch.float32, device=x.device)
+        _check(lnmod_quantize_rows(x, N, D, handle, codes, scales, dt, number), "lnmod_quantize_rows")
+    return codes, scales
+
+
+def code_product(codes, scales, w, w_scales, bias=None, dtype=None, stream=None):
+    """A linear layer in 8 bits: codes [..., K] with scales [...] (rmsnorm_quant_forward with group 0, quantize_rows) times
+    w [N, K] with w_scales [N] (quantize_rows of the layer's weight, once), both int8 or both float8_e4m3fn ->
+    y [..., N] = (sum_k codes * w) * scales * w_scales + bias, in `dtype` (bfloat16, the default, or float32).
+    bias: [N] in y's type.  K is a multiple of 8 below 2^17.  For serving: nothing is differentiated."""
+    import torch
+    dtype = torch.bfloat16 if dtype is None else dtype
+    host = _host(codes, stream)
+    r = None if host is None else host.code_product(codes, scales, w, w_scales, bias, dtype)
+    if r is not None:
+        return r
+    number = _code_number(codes)
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("dtype must be torch.bfloat16 or torch.float32, got %r" % (dtype,))
+    dt = LNMOD_BF16 if dtype == torch.bfloat16 else LNMOD_F32
+    M, K = _rows(codes, "codes")
+    a = _Args(codes)
+    a.expect("codes", codes, codes.shape)
+    a.expect("scales", scales, _scales_shape(codes.shape, 0), torch.float32)
+    if not isinstance(w, torch.Tensor) or w.dim() != 2:
+        raise ValueError("w must be [N, K]")
+    N = w.shape[0]
+    a.expect("w", w, (N, K))
+    a.expect("w_scales", w_scales, (N,), torch.float32)
+    if bias is not None:
+        a.expect("bias", bias, (N,), dtype)
+    a.on_gpu()
+    with _on_device(codes, stream) as handle:
+        y = torch.empty(codes.shape[:-1] + (N,), dtype=dtype, device=codes.device)
+        _check(lnmod_code_product(codes, scales, w, w_scales, bias, M, N, K, handle, y, dt, number), "lnmod_code_product")
+    return y
+
+
+# ---- rotary positions --------------------------------------------------------------------------------
+def rotary_table(positions, axes, base=10000.0, frequencies=None, device="cuda"):
+    """The table of a rotation: cosine and sine of every pair at every position, formed in 64 bits -> float32
+    [positions, R/2, 2].  positions: how many (0, 1, ...), or a sequence of the positions that the rows stand for (numbers of
+    any kind: shifted, scaled, negative).  axes: features of each axis, R in all; pair i of an axis with d features turns by
+    base^(-2i/d) per position, or pair j of all by frequencies[j]."""
+    import torch
+    axes = _axes_of(axes)
+    if frequencies is None:
+        frequencies = torch.cat([float(base) ** (-torch.arange(0, d, 2, dtype=torch.float64) / d) for d in axes])
+    else:
+        frequencies = torch.as_tensor(frequencies, dtype=torch.float64).cpu()
+        if tuple(frequencies.shape) != (sum(axes) // 2,):
+            raise ValueError("frequencies must be %d numbers, one for each pair" % (sum(axes) // 2))
+    if isinstance(positions, int):
+        positions = torch.arange(positions, dtype=torch.float64)
+    positions = torch.as_tensor(positions, dtype=torch.float64).cpu()
+    if positions.dim() != 1:
+        raise ValueError("positions must be a number or one row of numbers")
+    angle = positions.unsqueeze(1) * frequencies
+    return torch.stack([angle.cos(), angle.sin()], -1).float().to(device)
+
+
+def rotary_grid(frames, height, width, device="cuda"):
+    """Positions of the patches of a clip, row by row of each frame: int32 [frames*height*width, 3] (time, height, width).
+    A packed batch's are the clips' one after the other (torch.cat)."""
+    import torch
+    at = torch.meshgrid(*(torch.arange(n, dtype=torch.int32) for n in (frames, height, width)), indexing="ij")
+    return torch.stack(at, -1).reshape(-1, 3).to(device)
+
+
+def _axes_of(axes):
+    try:
+        axes = tuple(axes)
+    except TypeError:
+        axes = ()
+    if not 1 <= len(axes) <= MAX_AXES or any(isinstance(d, bool) or not isinstance(d, int) or d < 2 or d % 2 for d in axes):
+        raise ValueError("axes must be 1 to %d even numbers of features, got %r" % (MAX_AXES, axes))
+    return axes
+
+
+def _heads_strides(t):
+    """(batch, token, head) strides in elements of a tensor [.., tokens, heads, features], 0 where there is one index only;
+    None where the kernels cannot read it as it lies."""
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        return None
+    step = 16 // t.element_size()
+    strides = [0 if t.shape[d] == 1 else t.stride(d) for d in range(t.dim() - 1)]
+    if any(s % step for s in strides) or t.data_ptr() % 16:
+        return None
+    return tuple(strides) if t.dim() == 4 else (0,) + tuple(strides)
+
+
+def _expect_heads(a, name, t, shape):
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise ValueError("%s must be a tensor" % name)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if t.dtype != a.ref.dtype:
+        raise ValueError("%s must be %s, got %s" % (name, a.ref.dtype, t.dtype))
+    if t.layout != torch.strided or (t.numel() and _heads_strides(t) is None):
+        raise ValueError("%s must have dense features and 16-byte aligned rows (strides a multiple of %d elements), got strides %s"
+                         % (name, 16 // t.element_size(), t.stride() if t.layout == torch.strided else t.layout))
+    a.seen.append((name, t))
+
+
+def _heads(t):
+    return None if t is None else Heads(t.data_ptr(), *(_heads_strides(t) if t.numel() else (0, 0, 0)))
+
+
+def _rotary_args(q, k, positions, table, axes, interleaved):
+    """Checks what both operators share -> args, (B, S, q heads, k heads, head_dim), Rotation."""
+    import torch
+    a = _Args(q)
+    dt = _dtype_code(q)
+    if q.dim() not in (3, 4):
+        raise ValueError("q must be [B, S, heads, head_dim] or packed [T, heads, head_dim], got %s" % (tuple(q.shape),))
+    lead, heads, hd = tuple(q.shape[:-2]), q.shape[-2], q.shape[-1]
+    _expect_heads(a, "q", q, q.shape)
+    if k is not None:
+        kv = k.shape[-2] if isinstance(k, torch.Tensor) and k.dim() == q.dim() else 0
+        _expect_heads(a, "k", k, lead + (kv, hd))
+    axes = _axes_of(axes)
+    if sum(axes) > hd:
+        raise ValueError("axes name %d features, a head has %d" % (sum(axes), hd))
+    if not isinstance(interleaved, bool):
+        raise ValueError("interleaved must be True or False, got %r" % (interleaved,))
+    if not interleaved and sum(axes) % 8:
+        raise ValueError("the axes' features must be a multiple of 8 in all where pairs are not interleaved, got %d" % sum(axes))
+    if not isinstance(positions, torch.Tensor) or positions.dim() < 2:
+        raise ValueError("positions must be [.., tokens, axes]")
+    shared = len(lead) == 2 and positions.dim() == 2
+    a.expect("positions", positions, (lead[-1:] if shared else lead) + (len(axes),), torch.int32)
+    if not isinstance(table, torch.Tensor) or table.dim() != 3:
+        raise ValueError("table must be [positions, pairs, 2]")
+    a.expect("table", table, (table.shape[0], sum(axes) // 2, 2), torch.float32)
+    if table.shape[0] < 1:
+        raise ValueError("table must hold a position")
+    if table.data_ptr() % 8:
+        raise ValueError("table must be 8-byte aligned")
+    B, S = lead if len(lead) == 2 else (1, lead[0])
+    rot = Rotation(positions.data_ptr(), S if shared else B * S, table.data_ptr(), table.shape[0], len(axes),
+                   (ctypes.c_int32 * MAX_AXES)(*axes), int(interleaved))
+    return a, dt, (B, S, heads, 0 if k is None else k.shape[-2], hd), rot
+
+
+def rotary(q, k, positions, table, axes, interleaved=True, inverse=False, stream=None):
+    """Rotary positions with several axes of q [B, S, heads, head_dim] and k [B, S, its heads, head_dim] (or packed
+    [T, heads, head_dim]; k may be None) -> both, dense.  q and k may be views with dense features: of a fused projection's
+    output, or with the heads in front of the tokens.  positions: int32 [S, axes] that the samples share, or [B, S, axes] /
+    [T, axes]: rows of `table` (rotary_table).  axes: features of each axis.  Pairs are neighbours (interleaved), or feature j
+    and j + R/2.  inverse: turned back, which is the gradient of the rotation."""
+    import torch
+    host = _host(q, stream)
+    r = None if host is None else host.rotary_call(q, k, positions, table, axes, interleaved, inverse)
+    if r is not None:
+        return r
+    a, dt, (B, S, heads, kv, hd), rot = _rotary_args(q, k, positions, table, axes, interleaved)
+    a.on_gpu()
+    with _on_device(q, stream) as handle:
+        qo = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        ko = None if k is None else torch.empty(k.shape, dtype=q.dtype, device=q.device)
+        if k is not None and kv == 0:
+            k = None
+        _check(lnmod_rotary(_heads(q), _heads(k), B, S, heads, kv, hd, rot, int(bool(inverse)), handle, qo,
+                            ko if k is not None else None, dt), "lnmod_rotary")
+    return qo, ko
+
+
+def _qk_weights(a, wq, wk, heads, kv, hd):
+    """-> whether each head has the norm."""
+    import torch
+    per_head = isinstance(wq, torch.Tensor) and tuple(wq.shape) == (hd,) and isinstance(wk, torch.Tensor) and tuple(wk.shape) == (hd,)
+    a.expect("wq", wq, (hd,) if per_head else (heads * hd,))
+    a.expect("wk", wk, (hd,) if per_head else (kv * hd,))
+    return per_head
+
+
+def qknorm_rotary_forward(q, k, wq, wk, positions, table, axes, interleaved=True, eps=1e-6, stream=None):
+    """qknorm_forward() and rotary() in one pass.  wq, wk: [heads * head_dim] of each tensor (the norm is over a token's whole
+    row), or both [head_dim] (over each head) -> q_out, k_out, rstd_q, rstd_k (float32 [B, S] / [T], with a dimension of
+    heads where each has the norm)."""
+    import torch
+    host = _host(q, stream, eps)
+    r = None if host is None else host.qknorm_rotary_forward(q, k, wq, wk, positions, table, axes, interleaved, eps)
+    if r is not None:
+        return r
+    if k is None:
+        raise ValueError("k must be a tensor")
+    a, dt, (B, S, heads, kv, hd), rot = _rotary_args(q, k, positions, table, axes, interleaved)
+    per_head = _qk_weights(a, wq, wk, heads, kv, hd)
+    a.on_gpu()
+    with _on_device(q, stream) as handle:
+        qo, ko = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+        rq, rk = (torch.empty(t.shape[:-1] if per_head else t.shape[:-2], dtype=torch.float32, device=t.device) for t in (q, k))
+        _check(lnmod_qknorm_rotary_forward(_heads(q), _heads(k), wq, wk, B, S, heads, kv, hd, rot, eps, int(per_head), handle,
+                                           qo, ko, rq, rk, dt), "lnmod_qknorm_rotary_forward")
+    return qo, ko, rq, rk
+
+
+def qknorm_rotary_backward(dq_out, dk_out, q, k, wq, wk, rstd_q, rstd_k, positions, table, axes, interleaved=True, stream=None,
+                           ws=None):
+    """-> dq, dk (I/O dtype, dense) and dwq, dwk (float32).  dq_out and dk_out may be views as q and k may."""
+    return _qknorm_rotary_backward(dq_out, dk_out, q, k, wq, wk, rstd_q, rstd_k, positions, table, axes, interleaved, stream, ws)
+
+
+def _qknorm_rotary_backward(dq_out, dk_out, q, k, wq, wk, rstd_q, rstd_k, positions, table, axes, interleaved, stream=None,
+                            ws=None, io_grads=False):
+    """qknorm_rotary_backward(); with io_grads dwq and dwk come in the I/O dtype."""
+    import torch
+    if k is None:
+        raise ValueError("k must be a tensor")
+    a, dt, (B, S, heads, kv, hd), rot = _rotary_args(q, k, positions, table, axes, interleaved)
+    per_head = _qk_weights(a, wq, wk, heads, kv, hd)
+    _expect_heads(a, "dq_out", dq_out, q.shape)
+    _expect_heads(a, "dk_out", dk_out, k.shape)
+    a.expect("rstd_q", rstd_q, q.shape[:-1] if per_head else q.shape[:-2], torch.float32)
+    a.expect("rstd_k", rstd_k, k.shape[:-1] if per_head else k.shape[:-2], torch.float32)
+    need = lnmod_qknorm_rotary_backward_workspace_bytes(B * S, heads, kv, hd, int(per_head))
+    a.expect_workspace(ws, need)
+    a.on_gpu()
+    with _on_device(q, stream) as handle:
+        dq, dk = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+        dwq, dwk = (torch.empty(w.shape, dtype=w.dtype if io_grads else torch.float32, device=w.device) for w in (wq, wk))
+        if ws is None:
+            ws = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+        _check(lnmod_qknorm_rotary_backward(_heads(dq_out), _heads(dk_out), _heads(q), _heads(k), wq, wk, B, S, heads, kv, hd,
+                                            rot, int(per_head), handle, rstd_q, rstd_k, dq, dk, dwq, dwk, ws, ws.numel(), dt,
+                                            int(io_grads)), "lnmod_qknorm_rotary_backward")
+    return dq, dk, dwq, dwk

@@ -1,0 +1,76 @@
+"""Codes with one scale for a row, and their product, against the definitions in 64 bits.
+
+Bounds.  u = 2^-24.  int8: the sum is exact; its conversion, the two products with the scales and the bias round once each, 4 u of
+|y| + |bias| in all; then half a step of y's type.  e4m3: the products of codes are exact in fp32 (8 bits), their K - 1 additions
+in any order are off by K u of the sum of magnitudes.  With y in bf16 the matrix instruction aligns the products of eight neighbouring
+features to the largest of them and drops what lies 2^-13 below its leading bit: each of the seven others loses less than
+2^-13 of it.  On whole numbers up to 16 (products up to 2^4 beside 1, no bit that low) every step is exact."""
+import pytest
+import torch
+
+from oracle import code_oracle
+from paper_2605_17923_amd import lnmod
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+KIND = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}
+
+
+def codes_of(code, rows, K, g, whole=False):
+    if code == "int8":
+        c = torch.randint(-127, 128, (rows, K), generator=g, dtype=torch.int8)
+        return c // 16 if whole else c
+    v = torch.randint(-4, 5, (rows, K), generator=g).float() if whole else torch.randn(rows, K, generator=g) * 60
+    return v.clamp(-448, 448).to(torch.float8_e4m3fn)
+
+
+def product(code, dtype, M, N, K, bias=True, whole=False, seed=0):
+    g = torch.Generator().manual_seed(seed + M + 7 * N + 13 * K)
+    a, w = codes_of(code, M, K, g, whole), codes_of(code, N, K, g, whole)
+    if whole:
+        sa, sw = (torch.exp2(torch.randint(-3, 4, (n,), generator=g).float()) for n in (M, N))
+    else:
+        sa, sw = (torch.rand(n, generator=g) * 0.01 + 1e-3 for n in (M, N))
+    b = torch.randn(N, generator=g).to(dtype) if bias else None
+    got = lnmod.code_product(a.cuda(), sa.cuda(), w.cuda(), sw.cuda(), None if b is None else b.cuda(), dtype).cpu()
+    ad, wd = a.double(), w.double()
+    scale = sa.double()[:, None] * sw.double()
+    v = (ad @ wd.t()) * scale
+    want = v if b is None else v + b.double()
+    slack = 4 * U * (v.abs() + (0 if b is None else b.double().abs()))
+    if code == "e4m3" and not whole:
+        slack = slack + K * U * (ad.abs() @ wd.abs().t()) * scale
+        if dtype == torch.bfloat16:
+            for k in range(0, K, 8):
+                slack = slack + 7 * 2.0 ** -13 * (ad[:, None, k:k + 8] * wd[:, k:k + 8]).abs().amax(-1) * scale
+    tol = torch.finfo(dtype).eps / 2 * want.abs() + slack
+    err = (got.double() - want).abs()
+    assert got.shape == (M, N)
+    assert bool((err <= tol).all()), "worst %.3g of the bound" % float((err / tol).max())
+
+
+SIZES = [(1, 16, 8), (1, 1, 64), (2, 33, 24), (1, 5120, 512), (3, 257, 1024), (16, 64, 128), (17, 100, 136), (31, 48, 392),
+         (64, 512, 2600), (65, 130, 256), (96, 768, 1024), (128, 256, 1152), (129, 257, 264), (200, 1433, 520), (255, 255, 1000),
+         (256, 256, 256), (257, 513, 384), (300, 2048, 640), (515, 1030, 2048), (1025, 1433, 136), (2050, 24, 72), (700, 8, 128)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("size", SIZES, ids=str)
+def test_product(size, code, dtype):
+    product(code, dtype, *size, bias=size[0] % 2 == 1)
+    product(code, dtype, *size, bias=size[0] % 2 == 0, whole=True)
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(1, 8), (3, 24), (5, 64), (130, 72), (7, 512), (9, 520), (33, 1536), (4, 2048), (3, 5120),
+                                   (2, 8200), (5, 13824), (2, 32768), (3, 32776), (2, 70000)], ids=str)
+def test_rows(shape, dtype, code):
+    g = torch.Generator().manual_seed(shape[0] * shape[1])
+    x = (torch.randn(*shape, generator=g) * torch.exp2(torch.randint(-20, 20, (shape[0], 1), generator=g).float())).to(dtype)
+    codes, scales = lnmod.quantize_rows(x.cuda(), code)
+    q, s = code_oracle.encode(x.double().numpy(), code, 0)
+    assert codes.dtype == KIND[code] and codes.shape == x.shape and scales.shape == shape[:1]
+    assert torch.equal(scales.cpu(), torch.from_numpy(s).float().reshape(-1))
+    assert torch.equal(codes.cpu().float(), torch.from_numpy(q).float().reshape(shape))
