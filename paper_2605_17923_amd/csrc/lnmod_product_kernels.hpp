@@ -71,6 +71,84 @@ template <> struct Mac<e4m3_code, f32_io> {
 
 typedef uint8_t __attribute__((address_space(3))) lds_byte;
 
+// Sixteen codes of a row of which `left` exist (a multiple of 8, or fewer than 1), the others 0.
+__device__ inline u32x4 load_codes16(Row src, uint32_t offset, int uniform, int left) {
+    u32x4 v = {0u, 0u, 0u, 0u};
+    if (left >= 16) v = __builtin_amdgcn_raw_buffer_load_b128(src, offset, uniform, 0);
+    else if (left > 0) {
+        const u32x2 h = __builtin_amdgcn_raw_buffer_load_b64(src, offset, uniform, 0);
+        v[0] = h[0];
+        v[1] = h[1];
+    }
+    return v;
+}
+
+// Which tile a block computes.  Consecutive blocks go to the eight XCDs in turn, each with a cache of its own: an XCD gets a run
+// of tiles, and inside it eight rows of tiles are walked side by side, so that the tiles that its CUs have in hand at a time
+// share their rows of a and of w.
+struct Tile {
+    int64_t m, n;
+};
+__device__ inline Tile tile_of(const ProductArgs& a) {
+    constexpr int64_t kXcds = 8, kRows = 8;
+    const int64_t id = static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x;
+    if (id >= a.tiles) return Tile{-1, 0};
+    const int64_t each = a.tiles / kXcds, more = a.tiles % kXcds, x = id % kXcds;
+    const int64_t seq = x * each + (x < more ? x : more) + id / kXcds;
+    const int64_t tiles_n = a.tiles / a.tiles_m, band = seq / (kRows * tiles_n), at = seq - band * kRows * tiles_n;
+    const int64_t rows = a.tiles_m - band * kRows < kRows ? a.tiles_m - band * kRows : kRows;
+    return Tile{band * kRows + at % rows, at / rows};
+}
+
+// The outputs of a wave's TM x TN fragments, the first of them at (m0, n0).  A lane holds eight consecutive outputs of a row for
+// each pair of fragments of w, four lanes 32: where every row of y starts at a multiple of eight outputs they are stored
+// as they lie.
+template <typename C, typename Tag, int TM, int TN>
+__device__ inline void store_products(const ProductArgs& a, const typename Mac<C, Tag>::Sum (&acc)[TM][TN], int64_t m0, int64_t n0) {
+    constexpr bool kHalf = std::is_same<Tag, bf16_io>::value;
+    const int lane = threadIdx.x & (kWave - 1);
+    const bool whole = a.N % 8 == 0;
+#pragma unroll
+    for (int j = 0; j < TN; j += 2) {
+        const int64_t n = n0 + j * 16 + (lane >> 4) * 8;
+        float sw[8], b[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int64_t at = n + e < a.N ? n + e : a.N - 1;
+            sw[e] = a.sw[at];
+            b[e] = !a.bias ? 0.0f : kHalf ? static_cast<float>(static_cast<const __bf16*>(a.bias)[at]) : static_cast<const float*>(a.bias)[at];
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const int64_t m = m0 + i * 16 + (lane & 15);
+            if (m >= a.M) continue;
+            const float sa = a.sa[m];
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                v[e] = static_cast<float>(acc[i][j + e / 4][e % 4]) * sa * sw[e];
+                if (a.bias) v[e] += b[e];
+            }
+            if (whole) {
+                if (n >= a.N) continue;
+                char* y = static_cast<char*>(a.y) + (m * a.N + n) * IO<Tag>::kBytes;
+                if constexpr (kHalf) *reinterpret_cast<u32x4*>(y) = IO<Tag>::pack(v);
+                else {
+                    *reinterpret_cast<f32x4*>(y) = f32x4{v[0], v[1], v[2], v[3]};
+                    *reinterpret_cast<f32x4*>(y + 16) = f32x4{v[4], v[5], v[6], v[7]};
+                }
+                continue;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (n + e >= a.N) continue;
+                if constexpr (kHalf) static_cast<__bf16*>(a.y)[m * a.N + n + e] = static_cast<__bf16>(v[e]);
+                else static_cast<float*>(a.y)[m * a.N + n + e] = v[e];
+            }
+        }
+    }
+}
+
 // BM x BN outputs per block of WM x WN waves.
 template <typename C, typename Tag, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM* WN* kWave, 1) void product_tile_kernel(const ProductArgs a) {
@@ -82,9 +160,9 @@ __global__ __launch_bounds__(WM* WN* kWave, 1) void product_tile_kernel(const Pr
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WM, wn = wave / WM;
-    const int64_t tile = static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x;
-    if (tile >= a.tiles) return;
-    const int64_t m0 = tile % a.tiles_m * BM, n0 = tile / a.tiles_m * BN;
+    const Tile tile = tile_of(a);
+    if (tile.m < 0) return;
+    const int64_t m0 = tile.m * BM, n0 = tile.n * BN;
     const int K = a.K, steps = (K + kBlockK - 1) / kBlockK;
 
     // what a lane fetches: row slot (i*NW + wave)*8 + lane/8, sixteen features; the slot of eight sixteens is permuted by
@@ -113,16 +191,8 @@ __global__ __launch_bounds__(WM* WN* kWave, 1) void product_tile_kernel(const Pr
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_byte*)(dst + (i * NW + wave) * 1024), 16, off[i], k0, 0, 0);
         } else {
             const int left = K - k0 - c * 16;                  // codes of this lane's sixteen that exist: a multiple of 8
-            for (int i = 0; i < count; ++i) {
-                u32x4 v = {0u, 0u, 0u, 0u};
-                if (left >= 16) v = __builtin_amdgcn_raw_buffer_load_b128(src, off[i], k0, 0);
-                else if (left > 0) {
-                    const u32x2 h = __builtin_amdgcn_raw_buffer_load_b64(src, off[i], k0, 0);
-                    v[0] = h[0];
-                    v[1] = h[1];
-                }
-                *reinterpret_cast<u32x4*>(dst + (i * NW + wave) * 1024 + lane * 16) = v;
-            }
+            for (int i = 0; i < count; ++i)
+                *reinterpret_cast<u32x4*>(dst + (i * NW + wave) * 1024 + lane * 16) = load_codes16(src, off[i], k0, left);
         }
     };
 
@@ -154,29 +224,116 @@ __global__ __launch_bounds__(WM* WN* kWave, 1) void product_tile_kernel(const Pr
         __syncthreads();
     }
 
-    // eight consecutive outputs of a row in a lane, for each pair of fragments of w
+    store_products<C, Tag, TM, TN>(a, acc, m0 + wm * TM * 16, n0 + wn * TN * 16);
+}
+
+// ---- large products ------------------------------------------------------------------------------------------------
+// 1024 bytes from global memory into LDS, sixteen from each lane's address, at dst + 16 lane.  In assembly because the compiler
+// makes every later read of LDS wait for such a load, whatever part of LDS it fills: no register is written here, and whoever
+// reads dst has waited for this wave's vmcnt and met the others at a barrier first.
+__device__ inline void load_lds(Row src, uint32_t offset, int uniform, const uint8_t* dst) {
+    const uint32_t at = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_byte*)dst)));
+    asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(offset), "s"(src), "s"(uniform), "s"(at) : "m0");
+}
+__device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+
+// 256 x 256 outputs by eight waves of 128 x 64, two on each SIMD that take turns: while one reads the fragments of its next 128
+// features from LDS, the other multiplies.
+template <typename C, typename Tag>
+__global__ __launch_bounds__(8 * kWave, 2) void product_large_kernel(const ProductArgs a) {
+    using mac = Mac<C, Tag>;
+    constexpr int BM = 256, BN = 256, NW = 8, TM = 8, TN = 4;
+    constexpr int XI = BM / 8 / NW, WI = BN / 8 / NW;
+    __shared__ __attribute__((aligned(1024))) uint8_t sx[2][BM * kBlockK], sw[2][BN * kBlockK];
+    const Tile tile = tile_of(a);
+    if (tile.m < 0) return;
+    const int64_t m0 = tile.m * BM, n0 = tile.n * BN;
+
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave & 1, wn = wave >> 1;
+    const bool second = wave >= 4;                             // waves w and w + 4 share a SIMD
+    const int K = a.K, steps = (K + kBlockK - 1) / kBlockK;
+
+    const int c = (lane & 7) ^ (lane >> 3);
+    uint32_t xo[XI], wo[WI];
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int64_t m = m0 + (wm * TM + i) * 16 + (lane & 15);
-        if (m >= a.M) continue;
-        const float sa = a.sa[m];
-#pragma unroll
-        for (int j = 0; j < TN; j += 2) {
-            const int64_t n = n0 + (wn * TN + j) * 16 + (lane >> 4) * 8;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (n + e >= a.N) continue;
-                float v = static_cast<float>(acc[i][j + e / 4][e % 4]) * sa * a.sw[n + e];
-                if constexpr (std::is_same<Tag, bf16_io>::value) {
-                    if (a.bias) v += static_cast<float>(static_cast<const __bf16*>(a.bias)[n + e]);
-                    static_cast<__bf16*>(a.y)[m * a.N + n + e] = static_cast<__bf16>(v);
-                } else {
-                    if (a.bias) v += static_cast<const float*>(a.bias)[n + e];
-                    static_cast<float*>(a.y)[m * a.N + n + e] = v;
-                }
-            }
-        }
+    for (int i = 0; i < XI; ++i) {
+        int64_t r = (i * NW + wave) * 8 + (lane >> 3);
+        if (m0 + r >= a.M) r = a.M - 1 - m0;
+        xo[i] = static_cast<uint32_t>(r) * K + c * 16;
     }
+#pragma unroll
+    for (int i = 0; i < WI; ++i) {
+        const int slot = (i * NW + wave) * 8 + (lane >> 3);
+        int64_t r = (slot & ~31) + ((slot >> 2) & 3) * 8 + ((slot >> 4) & 1) * 4 + (slot & 3);
+        if (n0 + r >= a.N) r = a.N - 1 - n0;
+        wo[i] = static_cast<uint32_t>(r) * K + c * 16;
+    }
+    const Row xrow = row_of(a.a, m0 * K, 0x7fffffffu), wrow = row_of(a.w, n0 * K, 0x7fffffffu);
+
+    auto fetch = [&](int t) {
+        if (t >= steps) return;
+        const int k0 = t * kBlockK;
+        uint8_t *dx = sx[t & 1] + wave * 1024, *dw = sw[t & 1] + wave * 1024;
+        if (k0 + kBlockK <= K) {
+#pragma unroll
+            for (int i = 0; i < XI; ++i) load_lds(xrow, xo[i], k0, dx + i * NW * 1024);
+#pragma unroll
+            for (int i = 0; i < WI; ++i) load_lds(wrow, wo[i], k0, dw + i * NW * 1024);
+            return;
+        }
+        const int left = K - k0 - c * 16;                      // codes of this lane's sixteen that exist: a multiple of 8
+#pragma unroll
+        for (int i = 0; i < XI + WI; ++i)
+            *reinterpret_cast<u32x4*>((i < XI ? dx : dw) + (i % XI) * NW * 1024 + lane * 16) =
+                load_codes16(i < XI ? xrow : wrow, i < XI ? xo[i % XI] : wo[i % WI], k0, left);
+    };
+
+    typename mac::Sum acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = mac::zero();
+    const int fo = (lane & 15) * kBlockK + (((lane >> 4) ^ (lane & 7)) << 4);
+    auto frag = [&](const uint8_t* p) {
+        return mac::frag(*reinterpret_cast<const i32x4*>(p + fo), *reinterpret_cast<const i32x4*>(p + (fo ^ 64)));
+    };
+
+    fetch(0);
+    wait_loads();
+    __builtin_amdgcn_s_barrier();
+    if (second) {
+        fetch(1);
+        __builtin_amdgcn_s_barrier();
+    }
+#pragma unroll 1
+    for (int t = 0; t < steps; ++t) {
+        if (!second) fetch(t + 1);
+        typename mac::Frag xf[TM], wf[TN];
+        const uint8_t *px = sx[t & 1] + wm * TM * 16 * kBlockK, *pw = sw[t & 1] + wn * TN * 16 * kBlockK;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) wf[j] = frag(pw + j * 16 * kBlockK);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) xf[i] = frag(px + i * 16 * kBlockK);
+        if (second) wait_loads();
+        else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        if (second) fetch(t + 2);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = mac::add(wf[j], xf[i], acc[i][j]);
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+        if (!second) wait_loads();
+        __builtin_amdgcn_s_barrier();
+    }
+    if (!second) __builtin_amdgcn_s_barrier();
+
+    store_products<C, Tag, TM, TN>(a, acc, m0 + wm * TM * 16, n0 + wn * TN * 16);
 }
 
 }  // namespace lnmod

@@ -62,6 +62,17 @@ def test_product(size, code, dtype):
     product(code, dtype, *size, bias=size[0] % 2 == 0, whole=True)
 
 
+# products that the tiles of 256 x 256 take: sizes that end inside a tile, one step, an odd and an even number of them, a tail
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("size", [(2049, 2056, 128), (4097, 1030, 24), (2305, 1900, 256), (300, 16001, 136), (8200, 520, 384),
+                                  (2048, 2048, 520)], ids=str)
+def test_large_product(size, code, dtype):
+    product(code, dtype, *size, bias=size[0] % 2 == 1, whole=True)
+    if code == "int8" or dtype == torch.float32:
+        product(code, dtype, *size, bias=size[0] % 2 == 0)
+
+
 @pytest.mark.parametrize("code", ["int8", "e4m3"])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("shape", [(1, 8), (3, 24), (5, 64), (130, 72), (7, 512), (9, 520), (33, 1536), (4, 2048), (3, 5120),
