@@ -29,9 +29,10 @@ template <typename Tag> struct Mac<int8_code, Tag> {
     };
     __device__ static inline Sum zero() { return Sum{0, 0, 0, 0}; }
     __device__ static inline Frag frag(const i32x4& lo, const i32x4& hi) { return Frag{{lo, hi}}; }
-    __device__ static inline Sum add(const Frag& a, const Frag& b, Sum c) {
-        c = __builtin_amdgcn_mfma_i32_16x16x64_i8(a.v[0], b.v[0], c, 0, 0, 0);
-        return __builtin_amdgcn_mfma_i32_16x16x64_i8(a.v[1], b.v[1], c, 0, 0, 0);
+    // a product is kParts instructions, taken one after the other of several products: each waits for its sum's last one
+    static constexpr int kParts = 2;
+    __device__ static inline Sum add(const Frag& a, const Frag& b, Sum c, int h) {
+        return __builtin_amdgcn_mfma_i32_16x16x64_i8(a.v[h], b.v[h], c, 0, 0, 0);
     }
 };
 
@@ -40,7 +41,8 @@ template <> struct Mac<e4m3_code, bf16_io> {
     typedef i32x8 Frag;
     __device__ static inline Sum zero() { return Sum{0.0f, 0.0f, 0.0f, 0.0f}; }
     __device__ static inline Frag frag(const i32x4& lo, const i32x4& hi) { return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7); }
-    __device__ static inline Sum add(const Frag& a, const Frag& b, Sum c) {
+    static constexpr int kParts = 1;
+    __device__ static inline Sum add(const Frag& a, const Frag& b, Sum c, int) {
         return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
     }
 };
@@ -62,10 +64,9 @@ template <> struct Mac<e4m3_code, f32_io> {
     __device__ static inline Frag frag(const i32x4& lo, const i32x4& hi) {
         return Frag{{halves(lo[0], lo[1]), halves(lo[2], lo[3]), halves(hi[0], hi[1]), halves(hi[2], hi[3])}};
     }
-    __device__ static inline Sum add(const Frag& a, const Frag& b, Sum c) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v[i], b.v[i], c, 0, 0, 0);
-        return c;
+    static constexpr int kParts = 4;
+    __device__ static inline Sum add(const Frag& a, const Frag& b, Sum c, int h) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v[h], b.v[h], c, 0, 0, 0);
     }
 };
 
@@ -219,7 +220,9 @@ __global__ __launch_bounds__(WM* WN* kWave, 1) void product_tile_kernel(const Pr
             const uint8_t* p = sw[0] + (wn * TN + j) * 16 * kBlockK;
             const typename mac::Frag wf = mac::frag(*reinterpret_cast<const i32x4*>(p + fo), *reinterpret_cast<const i32x4*>(p + (fo ^ 64)));
 #pragma unroll
-            for (int i = 0; i < TM; ++i) acc[i][j] = mac::add(wf, xf[i], acc[i][j]);
+            for (int h = 0; h < mac::kParts; ++h)
+#pragma unroll
+                for (int i = 0; i < TM; ++i) acc[i][j] = mac::add(wf, xf[i], acc[i][j], h);
         }
         __syncthreads();
     }
@@ -238,13 +241,19 @@ __device__ inline void load_lds(Row src, uint32_t offset, int uniform, const uin
 __device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 
 // 256 x 256 outputs by eight waves of 128 x 64, two on each SIMD that take turns: while one reads the fragments of its next 128
-// features from LDS, the other multiplies.
+// features from LDS, the other multiplies.  Waves 0 to 3 bring w, two steps ahead into three buffers, waves 4 to 7 a, one step
+// ahead into two; each while it multiplies, so that a quarter of a CU's loads is in its queue at a time.
+//
+//   phase      2t                                  2t + 1                               2t + 2
+//   waves 0-3  read a(t), w(t)                     multiply t, bring w(t+2)             read a(t+1), w(t+1)
+//   waves 4-7  multiply t-1, bring a(t+1)          read a(t), w(t)                      multiply t, bring a(t+2)
+//
+// A wave waits for what it has brought at the end of the phase after, when it has read.
 template <typename C, typename Tag>
 __global__ __launch_bounds__(8 * kWave, 2) void product_large_kernel(const ProductArgs a) {
     using mac = Mac<C, Tag>;
-    constexpr int BM = 256, BN = 256, NW = 8, TM = 8, TN = 4;
-    constexpr int XI = BM / 8 / NW, WI = BN / 8 / NW;
-    __shared__ __attribute__((aligned(1024))) uint8_t sx[2][BM * kBlockK], sw[2][BN * kBlockK];
+    constexpr int BM = 256, BN = 256, TM = 8, TN = 4, PIECES = 8, kPart = 256 * kBlockK;
+    __shared__ __attribute__((aligned(1024))) uint8_t sx[2 * kPart], sw[3 * kPart];
     const Tile tile = tile_of(a);
     if (tile.m < 0) return;
     const int64_t m0 = tile.m * BM, n0 = tile.n * BN;
@@ -253,41 +262,35 @@ __global__ __launch_bounds__(8 * kWave, 2) void product_large_kernel(const Produ
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave & 1, wn = wave >> 1;
     const bool second = wave >= 4;                             // waves w and w + 4 share a SIMD
-    const int K = a.K, steps = (K + kBlockK - 1) / kBlockK;
+    const int K = a.K, whole = K / kBlockK, steps = (K + kBlockK - 1) / kBlockK;
 
-    const int c = (lane & 7) ^ (lane >> 3);
-    uint32_t xo[XI], wo[WI];
+    // what a lane brings: eight pieces of eight rows, sixteen features of a row; the sixteens of a row are exchanged by the row,
+    // so that the eight rows that a fragment's lanes read at a time lie in different banks
+    const int c = (lane & 7) ^ (lane >> 3), quarter = wave & 3;
+    uint32_t off[PIECES];
 #pragma unroll
-    for (int i = 0; i < XI; ++i) {
-        int64_t r = (i * NW + wave) * 8 + (lane >> 3);
-        if (m0 + r >= a.M) r = a.M - 1 - m0;
-        xo[i] = static_cast<uint32_t>(r) * K + c * 16;
+    for (int i = 0; i < PIECES; ++i) {
+        const int slot = (i * 4 + quarter) * 8 + (lane >> 3);
+        int64_t r = slot;
+        if (!second) r = (slot & ~31) + ((slot >> 2) & 3) * 8 + ((slot >> 4) & 1) * 4 + (slot & 3);
+        const int64_t most = (second ? a.M - m0 : a.N - n0) - 1;
+        if (r > most) r = most;
+        off[i] = static_cast<uint32_t>(r) * K + c * 16;
     }
+    const Row src = second ? row_of(a.a, m0 * K, 0x7fffffffu) : row_of(a.w, n0 * K, 0x7fffffffu);
+    auto piece = [&](uint8_t* to, int i, int t) { load_lds(src, off[i], t * kBlockK, to + (i * 4 + quarter) * 1024); };
+    // all of a step that is not whole, or none
+    auto rest = [&](uint8_t* to, int t) {
+        const int left = K - t * kBlockK - c * 16;             // codes of this lane's sixteen that exist: a multiple of 8
 #pragma unroll
-    for (int i = 0; i < WI; ++i) {
-        const int slot = (i * NW + wave) * 8 + (lane >> 3);
-        int64_t r = (slot & ~31) + ((slot >> 2) & 3) * 8 + ((slot >> 4) & 1) * 4 + (slot & 3);
-        if (n0 + r >= a.N) r = a.N - 1 - n0;
-        wo[i] = static_cast<uint32_t>(r) * K + c * 16;
-    }
-    const Row xrow = row_of(a.a, m0 * K, 0x7fffffffu), wrow = row_of(a.w, n0 * K, 0x7fffffffu);
-
-    auto fetch = [&](int t) {
-        if (t >= steps) return;
-        const int k0 = t * kBlockK;
-        uint8_t *dx = sx[t & 1] + wave * 1024, *dw = sw[t & 1] + wave * 1024;
-        if (k0 + kBlockK <= K) {
+        for (int i = 0; i < PIECES; ++i)
+            *reinterpret_cast<u32x4*>(to + (i * 4 + quarter) * 1024 + lane * 16) = load_codes16(src, off[i], t * kBlockK, left);
+    };
+    auto bring = [&](uint8_t* to, int t) {
+        if (t < whole) {
 #pragma unroll
-            for (int i = 0; i < XI; ++i) load_lds(xrow, xo[i], k0, dx + i * NW * 1024);
-#pragma unroll
-            for (int i = 0; i < WI; ++i) load_lds(wrow, wo[i], k0, dw + i * NW * 1024);
-            return;
-        }
-        const int left = K - k0 - c * 16;                      // codes of this lane's sixteen that exist: a multiple of 8
-#pragma unroll
-        for (int i = 0; i < XI + WI; ++i)
-            *reinterpret_cast<u32x4*>((i < XI ? dx : dw) + (i % XI) * NW * 1024 + lane * 16) =
-                load_codes16(i < XI ? xrow : wrow, i < XI ? xo[i % XI] : wo[i % WI], k0, left);
+            for (int i = 0; i < PIECES; ++i) piece(to, i, t);
+        } else if (t < steps) rest(to, t);
     };
 
     typename mac::Sum acc[TM][TN];
@@ -300,36 +303,44 @@ __global__ __launch_bounds__(8 * kWave, 2) void product_large_kernel(const Produ
         return mac::frag(*reinterpret_cast<const i32x4*>(p + fo), *reinterpret_cast<const i32x4*>(p + (fo ^ 64)));
     };
 
-    fetch(0);
+    bring(second ? sx : sw, 0);
+    if (!second) bring(sw + kPart, 1);
     wait_loads();
     __builtin_amdgcn_s_barrier();
     if (second) {
-        fetch(1);
+        bring(sx + kPart, 1);
         __builtin_amdgcn_s_barrier();
     }
+    int at = 0;                                                // t modulo 3
 #pragma unroll 1
     for (int t = 0; t < steps; ++t) {
-        if (!second) fetch(t + 1);
         typename mac::Frag xf[TM], wf[TN];
-        const uint8_t *px = sx[t & 1] + wm * TM * 16 * kBlockK, *pw = sw[t & 1] + wn * TN * 16 * kBlockK;
+        const uint8_t *px = sx + (t & 1) * kPart + wm * TM * 16 * kBlockK, *pw = sw + at * kPart + wn * TN * 16 * kBlockK;
 #pragma unroll
         for (int j = 0; j < TN; ++j) wf[j] = frag(pw + j * 16 * kBlockK);
 #pragma unroll
         for (int i = 0; i < TM; ++i) xf[i] = frag(px + i * 16 * kBlockK);
-        if (second) wait_loads();
-        else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        wait_loads();
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
-        if (second) fetch(t + 2);
+        // a piece between every four products: eight at once would have this wave wait for room in the loads' queue
+        uint8_t* to = second ? sx + (t & 1) * kPart : sw + (at == 0 ? 2 : at - 1) * kPart;
+        const bool ahead = t + 2 < whole;
+        if (!ahead && t + 2 < steps) rest(to, t + 2);
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int i = 0; i < TM; ++i)
+        for (int i = 0; i < TM; ++i) {
+            if (ahead) piece(to, i, t + 2);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = mac::add(wf[j], xf[i], acc[i][j]);
+            for (int h = 0; h < mac::kParts; ++h)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] = mac::add(wf[j], xf[i], acc[i][j], h);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         __builtin_amdgcn_s_setprio(0);
-        __builtin_amdgcn_sched_barrier(0);
-        if (!second) wait_loads();
         __builtin_amdgcn_s_barrier();
+        at = at == 2 ? 0 : at + 1;
     }
     if (!second) __builtin_amdgcn_s_barrier();
 
