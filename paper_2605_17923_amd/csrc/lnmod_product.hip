@@ -12,8 +12,8 @@ void go(ProductArgs a, hipStream_t st) {
         if (a.M >= 256 && a.N >= 256 && a.M * a.N >= int64_t{64} * 65536) {
             a.tiles_m = static_cast<int32_t>((a.M + 255) / 256);
             a.tiles = static_cast<int64_t>(a.tiles_m) * ((a.N + 255) / 256);
-            const int64_t x = a.tiles < kRowOfBlocks ? a.tiles : kRowOfBlocks;
-            hipLaunchKernelGGL((product_large_kernel<C, Tag>), dim3(static_cast<unsigned>(x), static_cast<unsigned>((a.tiles + x - 1) / x)), dim3(512), 0, st, a);
+            const int64_t blocks = a.tiles < kNumCU ? a.tiles : kNumCU;
+            hipLaunchKernelGGL((product_large_kernel<C, Tag>), dim3(static_cast<unsigned>(blocks)), dim3(512), 0, st, a);
             return;
         }
     }

@@ -72,6 +72,8 @@ template <> struct Mac<e4m3_code, f32_io> {
 
 typedef uint8_t __attribute__((address_space(3))) lds_byte;
 
+__device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+
 // Sixteen codes of a row of which `left` exist (a multiple of 8, or fewer than 1), the others 0.
 __device__ inline u32x4 load_codes16(Row src, uint32_t offset, int uniform, int left) {
     u32x4 v = {0u, 0u, 0u, 0u};
@@ -90,10 +92,8 @@ __device__ inline u32x4 load_codes16(Row src, uint32_t offset, int uniform, int 
 struct Tile {
     int64_t m, n;
 };
-__device__ inline Tile tile_of(const ProductArgs& a) {
+__device__ inline Tile tile_of(const ProductArgs& a, int64_t id) {
     constexpr int64_t kXcds = 8, kRows = 8;
-    const int64_t id = static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x;
-    if (id >= a.tiles) return Tile{-1, 0};
     const int64_t each = a.tiles / kXcds, more = a.tiles % kXcds, x = id % kXcds;
     const int64_t seq = x * each + (x < more ? x : more) + id / kXcds;
     const int64_t tiles_n = a.tiles / a.tiles_m, band = seq / (kRows * tiles_n), at = seq - band * kRows * tiles_n;
@@ -109,29 +109,37 @@ __device__ inline void store_products(const ProductArgs& a, const typename Mac<C
     constexpr bool kHalf = std::is_same<Tag, bf16_io>::value;
     const int lane = threadIdx.x & (kWave - 1);
     const bool whole = a.N % 8 == 0;
+    float sa[TM], sw[TN / 2][8], b[TN / 2][8];
 #pragma unroll
-    for (int j = 0; j < TN; j += 2) {
-        const int64_t n = n0 + j * 16 + (lane >> 4) * 8;
-        float sw[8], b[8];
+    for (int i = 0; i < TM; ++i) {
+        const int64_t m = m0 + i * 16 + (lane & 15);
+        sa[i] = a.sa[m < a.M ? m : a.M - 1];
+    }
+#pragma unroll
+    for (int j = 0; j < TN / 2; ++j) {
+        const int64_t n = n0 + j * 32 + (lane >> 4) * 8;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int64_t at = n + e < a.N ? n + e : a.N - 1;
-            sw[e] = a.sw[at];
-            b[e] = !a.bias ? 0.0f : kHalf ? static_cast<float>(static_cast<const __bf16*>(a.bias)[at]) : static_cast<const float*>(a.bias)[at];
+            sw[j][e] = a.sw[at];
+            b[j][e] = !a.bias ? 0.0f : kHalf ? static_cast<float>(static_cast<const __bf16*>(a.bias)[at]) : static_cast<const float*>(a.bias)[at];
         }
+    }
+    wait_loads();                            // also what the wave has sent for into LDS: its next wait would wait for these stores
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            const int64_t m = m0 + i * 16 + (lane & 15);
-            if (m >= a.M) continue;
-            const float sa = a.sa[m];
+    for (int i = 0; i < TM; ++i) {
+        const int64_t m = m0 + i * 16 + (lane & 15);
+#pragma unroll
+        for (int j = 0; j < TN / 2; ++j) {
+            const int64_t n = n0 + j * 32 + (lane >> 4) * 8;
             float v[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                v[e] = static_cast<float>(acc[i][j + e / 4][e % 4]) * sa * sw[e];
-                if (a.bias) v[e] += b[e];
+                v[e] = static_cast<float>(acc[i][2 * j + e / 4][e % 4]) * sa[i] * sw[j][e];
+                if (a.bias) v[e] += b[j][e];
             }
+            if (m >= a.M || n >= a.N) continue;
             if (whole) {
-                if (n >= a.N) continue;
                 char* y = static_cast<char*>(a.y) + (m * a.N + n) * IO<Tag>::kBytes;
                 if constexpr (kHalf) *reinterpret_cast<u32x4*>(y) = IO<Tag>::pack(v);
                 else {
@@ -161,8 +169,9 @@ __global__ __launch_bounds__(WM* WN* kWave, 1) void product_tile_kernel(const Pr
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WM, wn = wave / WM;
-    const Tile tile = tile_of(a);
-    if (tile.m < 0) return;
+    const int64_t id = static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x;
+    if (id >= a.tiles) return;
+    const Tile tile = tile_of(a, id);
     const int64_t m0 = tile.m * BM, n0 = tile.n * BN;
     const int K = a.K, steps = (K + kBlockK - 1) / kBlockK;
 
@@ -238,113 +247,129 @@ __device__ inline void load_lds(Row src, uint32_t offset, int uniform, const uin
     const uint32_t at = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_byte*)dst)));
     asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(offset), "s"(src), "s"(uniform), "s"(at) : "m0");
 }
-__device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 
 // 256 x 256 outputs by eight waves of 128 x 64, two on each SIMD that take turns: while one reads the fragments of its next 128
-// features from LDS, the other multiplies.  Waves 0 to 3 bring w, two steps ahead into three buffers, waves 4 to 7 a, one step
-// ahead into two; each while it multiplies, so that a quarter of a CU's loads is in its queue at a time.
+// features from LDS and sends for the features after them, the other multiplies.  Waves 0 to 3 bring a, one step ahead into
+// two buffers, waves 4 to 7 w, two steps ahead into three.
 //
 //   phase      2t                                  2t + 1                               2t + 2
-//   waves 0-3  read a(t), w(t)                     multiply t, bring w(t+2)             read a(t+1), w(t+1)
-//   waves 4-7  multiply t-1, bring a(t+1)          read a(t), w(t)                      multiply t, bring a(t+2)
+//   waves 0-3  read a(t), w(t); send for a(t+1)    multiply t; wait                     read a(t+1), w(t+1); ...
+//   waves 4-7  multiply t-1; wait                  read a(t), w(t); send for w(t+2)     multiply t; wait
 //
-// A wave waits for what it has brought at the end of the phase after, when it has read.
+// A block takes tiles until there are none: the first steps of the next tile are on their way while the outputs of the last
+// one are stored, and the stores reach memory while the next tile is computed.
 template <typename C, typename Tag>
 __global__ __launch_bounds__(8 * kWave, 2) void product_large_kernel(const ProductArgs a) {
     using mac = Mac<C, Tag>;
-    constexpr int BM = 256, BN = 256, TM = 8, TN = 4, PIECES = 8, kPart = 256 * kBlockK;
+    constexpr int BM = 256, BN = 256, TM = 8, TN = 4, kPieces = 8, kPart = 256 * kBlockK;
     __shared__ __attribute__((aligned(1024))) uint8_t sx[2 * kPart], sw[3 * kPart];
-    const Tile tile = tile_of(a);
-    if (tile.m < 0) return;
-    const int64_t m0 = tile.m * BM, n0 = tile.n * BN;
-
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave & 1, wn = wave >> 1;
     const bool second = wave >= 4;                             // waves w and w + 4 share a SIMD
     const int K = a.K, whole = K / kBlockK, steps = (K + kBlockK - 1) / kBlockK;
 
-    // what a lane brings: eight pieces of eight rows, sixteen features of a row; the sixteens of a row are exchanged by the row,
-    // so that the eight rows that a fragment's lanes read at a time lie in different banks
-    const int c = (lane & 7) ^ (lane >> 3), quarter = wave & 3;
-    uint32_t off[PIECES];
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-        const int slot = (i * 4 + quarter) * 8 + (lane >> 3);
-        int64_t r = slot;
-        if (!second) r = (slot & ~31) + ((slot >> 2) & 3) * 8 + ((slot >> 4) & 1) * 4 + (slot & 3);
-        const int64_t most = (second ? a.M - m0 : a.N - n0) - 1;
-        if (r > most) r = most;
-        off[i] = static_cast<uint32_t>(r) * K + c * 16;
-    }
-    const Row src = second ? row_of(a.a, m0 * K, 0x7fffffffu) : row_of(a.w, n0 * K, 0x7fffffffu);
-    auto piece = [&](uint8_t* to, int i, int t) { load_lds(src, off[i], t * kBlockK, to + (i * 4 + quarter) * 1024); };
-    // all of a step that is not whole, or none
-    auto rest = [&](uint8_t* to, int t) {
-        const int left = K - t * kBlockK - c * 16;             // codes of this lane's sixteen that exist: a multiple of 8
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i)
-            *reinterpret_cast<u32x4*>(to + (i * 4 + quarter) * 1024 + lane * 16) = load_codes16(src, off[i], t * kBlockK, left);
+    // what a lane brings: sixteen features of a row of each of eight pieces of eight rows; the sixteens of a row are exchanged
+    // by the row, so that the eight rows that a fragment's lanes read at a time lie in different banks.  Rows beyond the last
+    // one are the last one.
+    const int c = (lane & 7) ^ (lane >> 3), quarter = wave & 3, slot = quarter * 8 + (lane >> 3);
+    const uint32_t xfirst = static_cast<uint32_t>(slot) * K + c * 16;
+    const uint32_t wfirst = static_cast<uint32_t>(((slot >> 2) & 3) * 8 + ((slot >> 4) & 1) * 4 + (slot & 3)) * K + c * 16;
+    int64_t m0 = 0, n0 = 0;
+    uint32_t xlast = 0, wlast = 0;
+    auto aim = [&](const Tile& t) __attribute__((always_inline)) {
+        m0 = t.m * BM;
+        n0 = t.n * BN;
+        const int64_t m = a.M - 1 - m0, n = a.N - 1 - n0;
+        xlast = static_cast<uint32_t>(m < BM ? m : BM - 1) * K + c * 16;
+        wlast = static_cast<uint32_t>(n < BN ? n : BN - 1) * K + c * 16;
     };
-    auto bring = [&](uint8_t* to, int t) {
+    auto bring = [&](bool x, uint8_t* to, int t) __attribute__((always_inline)) {
+        const Row src = row_of(x ? a.a : a.w, (x ? m0 : n0) * K, 0x7fffffffu);
+        const uint32_t last = x ? xlast : wlast;
+        uint32_t first = x ? xfirst : wfirst;
+        asm volatile("" : "+v"(first));                        // the addresses are formed here, not kept in registers across the loop
         if (t < whole) {
 #pragma unroll
-            for (int i = 0; i < PIECES; ++i) piece(to, i, t);
-        } else if (t < steps) rest(to, t);
+            for (int i = 0; i < kPieces; ++i) {
+                const uint32_t off = first + i * 32 * K;
+                load_lds(src, off < last ? off : last, t * kBlockK, to + (i * 4 + quarter) * 1024);
+            }
+        } else if (t < steps) {
+            const int left = K - t * kBlockK - c * 16;         // codes of this lane's sixteen that exist: a multiple of 8
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const uint32_t off = first + i * 32 * K;
+                *reinterpret_cast<u32x4*>(to + (i * 4 + quarter) * 1024 + lane * 16) = load_codes16(src, off < last ? off : last, t * kBlockK, left);
+            }
+        }
+    };
+    auto first_steps = [&]() __attribute__((always_inline)) {
+        if (second) bring(false, sw + kPart, 1);
+        else {
+            bring(true, sx, 0);
+            bring(false, sw, 0);
+        }
     };
 
-    typename mac::Sum acc[TM][TN];
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = mac::zero();
     const int fo = (lane & 15) * kBlockK + (((lane >> 4) ^ (lane & 7)) << 4);
-    auto frag = [&](const uint8_t* p) {
+    auto frag = [&](const uint8_t* p) __attribute__((always_inline)) {
         return mac::frag(*reinterpret_cast<const i32x4*>(p + fo), *reinterpret_cast<const i32x4*>(p + (fo ^ 64)));
     };
 
-    bring(second ? sx : sw, 0);
-    if (!second) bring(sw + kPart, 1);
+    int64_t id = blockIdx.x;
+    aim(tile_of(a, id));
+    first_steps();
     wait_loads();
     __builtin_amdgcn_s_barrier();
-    if (second) {
-        bring(sx + kPart, 1);
-        __builtin_amdgcn_s_barrier();
-    }
-    int at = 0;                                                // t modulo 3
 #pragma unroll 1
-    for (int t = 0; t < steps; ++t) {
-        typename mac::Frag xf[TM], wf[TN];
-        const uint8_t *px = sx + (t & 1) * kPart + wm * TM * 16 * kBlockK, *pw = sw + at * kPart + wn * TN * 16 * kBlockK;
+    while (true) {
+        typename mac::Sum acc[TM][TN];
 #pragma unroll
-        for (int j = 0; j < TN; ++j) wf[j] = frag(pw + j * 16 * kBlockK);
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int i = 0; i < TM; ++i) xf[i] = frag(px + i * 16 * kBlockK);
-        wait_loads();
-        __builtin_amdgcn_s_barrier();
-        __builtin_amdgcn_sched_barrier(0);
-        // a piece between every four products: eight at once would have this wave wait for room in the loads' queue
-        uint8_t* to = second ? sx + (t & 1) * kPart : sw + (at == 0 ? 2 : at - 1) * kPart;
-        const bool ahead = t + 2 < whole;
-        if (!ahead && t + 2 < steps) rest(to, t + 2);
-        __builtin_amdgcn_s_setprio(1);
+            for (int j = 0; j < TN; ++j) acc[i][j] = mac::zero();
+        if (second) __builtin_amdgcn_s_barrier();
+        int at = 0;                                            // t modulo 3
+#pragma unroll 1
+        for (int t = 0; t < steps; ++t) {
+            typename mac::Frag xf[TM], wf[TN];
+            const uint8_t *px = sx + (t & 1) * kPart + wm * TM * 16 * kBlockK, *pw = sw + at * kPart + wn * TN * 16 * kBlockK;
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            if (ahead) piece(to, i, t + 2);
+            for (int j = 0; j < TN; ++j) wf[j] = frag(pw + j * 16 * kBlockK);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) xf[i] = frag(px + i * 16 * kBlockK);
             __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int h = 0; h < mac::kParts; ++h)
-#pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = mac::add(wf[j], xf[i], acc[i][j], h);
+            if (second) bring(false, sw + (at == 0 ? 2 : at - 1) * kPart, t + 2);
+            else bring(true, sx + (~t & 1) * kPart, t + 1);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int h = 0; h < mac::kParts; ++h)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) acc[i][j] = mac::add(wf[j], xf[i], acc[i][j], h);
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+            wait_loads();
+            __builtin_amdgcn_s_barrier();
+            at = at == 2 ? 0 : at + 1;
         }
-        __builtin_amdgcn_s_setprio(0);
-        __builtin_amdgcn_s_barrier();
-        at = at == 2 ? 0 : at + 1;
-    }
-    if (!second) __builtin_amdgcn_s_barrier();
 
-    store_products<C, Tag, TM, TN>(a, acc, m0 + wm * TM * 16, n0 + wn * TN * 16);
+        const int64_t m = m0 + wm * TM * 16, n = n0 + wn * TN * 16;
+        id += gridDim.x;
+        const bool more = id < a.tiles;
+        if (more) {
+            aim(tile_of(a, id));
+            first_steps();
+        }
+        store_products<C, Tag, TM, TN>(a, acc, m, n);
+        if (!second) __builtin_amdgcn_s_barrier();
+        if (!more) break;
+    }
 }
 
 }  // namespace lnmod
