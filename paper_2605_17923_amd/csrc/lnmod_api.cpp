@@ -579,7 +579,7 @@ int lnmod_code_product(const void* a, const float* a_scales, const void* w, cons
     if (M == 0 || N == 0) return LNMOD_OK;
     if (!a || !a_scales || !w || !w_scales || !y) return LNMOD_EINVAL;
     if (!aligned16(a) || !aligned16(w) || !aligned16(y)) return LNMOD_EALIGN;
-    lnmod::ProductArgs p{a, a_scales, w, w_scales, bias, y, M, N, static_cast<int32_t>(K), 0, 0};
+    lnmod::ProductArgs p{a, a_scales, w, w_scales, bias, y, M, N, static_cast<int32_t>(K)};
     const hipError_t e = lnmod::launch_product(dtype, code, p, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? LNMOD_OK : LNMOD_ELAUNCH;
 }

@@ -919,9 +919,23 @@ struct ProductArgs {
     void* y;                   // [M, N]
     int64_t M, N;
     int32_t K;
-    int32_t tiles_m;           // set by the launcher
-    int64_t tiles;
+    int32_t keep;              // whether y stays in the caches
+    // set by deal_tiles: how the tiles are dealt to the blocks
+    int32_t tiles_m, tiles_n;
+    uint32_t tiles, each, more;
+    Divider band_of, row_of;
 };
+constexpr int kXcds = 8;               // an XCD has an L2 of its own; consecutive blocks go to them in turn
+constexpr int kBandRows = 8;           // rows of tiles that are walked side by side
+inline void deal_tiles(ProductArgs& a, int bm, int bn) {
+    a.tiles_m = static_cast<int32_t>((a.M + bm - 1) / bm);
+    a.tiles_n = static_cast<int32_t>((a.N + bn - 1) / bn);
+    a.tiles = static_cast<uint32_t>(a.tiles_m) * static_cast<uint32_t>(a.tiles_n);
+    a.each = a.tiles / kXcds;
+    a.more = a.tiles % kXcds;
+    a.band_of = Divider(static_cast<uint32_t>(kBandRows) * a.tiles_n);
+    a.row_of = Divider(a.tiles_m % kBandRows ? a.tiles_m % kBandRows : kBandRows);
+}
 hipError_t launch_product(int dtype, int code, const ProductArgs& a, hipStream_t st);
 
 }  // namespace lnmod

@@ -4,25 +4,21 @@
 namespace lnmod {
 namespace {
 
-constexpr int64_t kRowOfBlocks = int64_t{1} << 22;   // a dimension of a grid has fewer than 2^32 threads
+constexpr uint32_t kRowOfBlocks = uint32_t{1} << 22;   // a dimension of a grid has fewer than 2^32 threads
 
 template <typename C, typename Tag>
 void go(ProductArgs a, hipStream_t st) {
+    a.keep = 0;
     if constexpr (!(std::is_same<C, e4m3_code>::value && std::is_same<Tag, f32_io>::value)) {
-        if (a.M >= 256 && a.N >= 256 && a.M * a.N >= int64_t{64} * 65536) {
-            a.tiles_m = static_cast<int32_t>((a.M + 255) / 256);
-            a.tiles = static_cast<int64_t>(a.tiles_m) * ((a.N + 255) / 256);
-            const int64_t blocks = a.tiles < kNumCU ? a.tiles : kNumCU;
-            hipLaunchKernelGGL((product_large_kernel<C, Tag>), dim3(static_cast<unsigned>(blocks)), dim3(512), 0, st, a);
+        if (a.K > kBlockK && a.M >= 256 && a.N >= 256 && a.M * a.N >= int64_t{64} * 65536) {
+            deal_tiles(a, 256, 256);
+            hipLaunchKernelGGL((product_large_kernel<C, Tag>), dim3(a.tiles < kNumCU ? a.tiles : kNumCU), dim3(8 * kWave), 0, st, a);
             return;
         }
     }
-    constexpr int BM = 128, BN = 128;
-    a.tiles_m = static_cast<int32_t>((a.M + BM - 1) / BM);
-    a.tiles = static_cast<int64_t>(a.tiles_m) * ((a.N + BN - 1) / BN);
-    const int64_t x = a.tiles < kRowOfBlocks ? a.tiles : kRowOfBlocks;
-    const dim3 grid(static_cast<unsigned>(x), static_cast<unsigned>((a.tiles + x - 1) / x));
-    hipLaunchKernelGGL((product_tile_kernel<C, Tag, BM, BN, 2, 2>), grid, dim3(256), 0, st, a);
+    deal_tiles(a, 128, 128);
+    const uint32_t x = a.tiles < kRowOfBlocks ? a.tiles : kRowOfBlocks;
+    hipLaunchKernelGGL((product_tile_kernel<C, Tag, 128, 128, 2, 2>), dim3(x, (a.tiles + x - 1) / x), dim3(4 * kWave), 0, st, a);
 }
 
 }  // namespace

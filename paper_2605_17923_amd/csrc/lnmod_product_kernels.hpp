@@ -90,42 +90,77 @@ __device__ inline u32x4 load_codes16(Row src, uint32_t offset, int uniform, int 
 // of tiles, and inside it eight rows of tiles are walked side by side, so that the tiles that its CUs have in hand at a time
 // share their rows of a and of w.
 struct Tile {
-    int64_t m, n;
+    uint32_t m, n;
 };
-__device__ inline Tile tile_of(const ProductArgs& a, int64_t id) {
-    constexpr int64_t kXcds = 8, kRows = 8;
-    const int64_t each = a.tiles / kXcds, more = a.tiles % kXcds, x = id % kXcds;
-    const int64_t seq = x * each + (x < more ? x : more) + id / kXcds;
-    const int64_t tiles_n = a.tiles / a.tiles_m, band = seq / (kRows * tiles_n), at = seq - band * kRows * tiles_n;
-    const int64_t rows = a.tiles_m - band * kRows < kRows ? a.tiles_m - band * kRows : kRows;
-    return Tile{band * kRows + at % rows, at / rows};
+__device__ inline Tile tile_of(const ProductArgs& a, uint32_t id) {
+    const uint32_t x = id % kXcds, seq = x * a.each + (x < a.more ? x : a.more) + id / kXcds;
+    const uint32_t band = a.band_of(seq), at = seq - band * kBandRows * a.tiles_n;
+    const uint32_t left = a.tiles_m - band * kBandRows, rows = left < kBandRows ? left : kBandRows;
+    const uint32_t n = left < kBandRows ? a.row_of(at) : at / kBandRows;
+    return Tile{band * kBandRows + at - n * rows, n};
 }
 
-// The outputs of a wave's TM x TN fragments, the first of them at (m0, n0).  A lane holds eight consecutive outputs of a row for
-// each pair of fragments of w, four lanes 32: where every row of y starts at a multiple of eight outputs they are stored
-// as they lie.
-template <typename C, typename Tag, int TM, int TN>
-__device__ inline void store_products(const ProductArgs& a, const typename Mac<C, Tag>::Sum (&acc)[TM][TN], int64_t m0, int64_t n0) {
-    constexpr bool kHalf = std::is_same<Tag, bf16_io>::value;
-    const int lane = threadIdx.x & (kWave - 1);
-    const bool whole = a.N % 8 == 0;
-    float sa[TM], sw[TN / 2][8], b[TN / 2][8];
+// What the outputs of a wave's TM x TN fragments, the first of them at (m0, n0), are scaled with.  A lane holds eight
+// consecutive outputs of a row for each pair of fragments of w, four lanes 32.
+template <typename Tag, int TM, int TN>
+struct Scales {
+    static constexpr bool kHalf = std::is_same<Tag, bf16_io>::value;
+    float a[TM], w[TN / 2][8];
+    u32x4 b[TN / 2][Unit<Tag>::NV];
+    // m0 and n0 are uniform; rows and features beyond the last one have the last one's
+    __device__ inline void load(const ProductArgs& p, int64_t m0, int64_t n0) {
+        constexpr int kBytes = IO<Tag>::kBytes;
+        const int lane = threadIdx.x & (kWave - 1);
+        const int rows = static_cast<int>(p.M - 1 - m0 < TM * 16 ? p.M - 1 - m0 : TM * 16);
+        const int most = static_cast<int>(p.N - 1 - n0 < TN * 16 ? p.N - 1 - n0 : TN * 16);
+        const Row ra = row_of(p.sa, m0 * 4, 0x7fffffffu), rw = row_of(p.sw, n0 * 4, 0x7fffffffu);
+        const Row rb = row_of(p.bias, n0 * kBytes, 0x7fffffffu);
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int64_t m = m0 + i * 16 + (lane & 15);
-        sa[i] = a.sa[m < a.M ? m : a.M - 1];
-    }
+        for (int i = 0; i < TM; ++i) {
+            const int m = i * 16 + (lane & 15);
+            a[i] = load_float(ra, (m < rows ? m : rows) * 4);
+        }
+        if (p.N % 8 == 0) {                  // eight at a time, whatever they are aligned to
 #pragma unroll
-    for (int j = 0; j < TN / 2; ++j) {
-        const int64_t n = n0 + j * 32 + (lane >> 4) * 8;
+            for (int j = 0; j < TN / 2; ++j) {
+                int n = j * 32 + (lane >> 4) * 8;
+                if (n > most) n = most - 7;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int64_t at = n + e < a.N ? n + e : a.N - 1;
-            sw[j][e] = a.sw[at];
-            b[j][e] = !a.bias ? 0.0f : kHalf ? static_cast<float>(static_cast<const __bf16*>(a.bias)[at]) : static_cast<const float*>(a.bias)[at];
+                for (int h = 0; h < 2; ++h) {
+                    const f32x4 t = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, n * 4 + 16 * h, 0, 0));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[j][4 * h + e] = t[e];
+                }
+                if (!p.bias) continue;
+#pragma unroll
+                for (int h = 0; h < Unit<Tag>::NV; ++h) b[j][h] = __builtin_amdgcn_raw_buffer_load_b128(rb, n * kBytes + 16 * h, 0, 0);
+            }
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < TN / 2; ++j) {
+            float v[8] = {};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                int n = j * 32 + (lane >> 4) * 8 + e;
+                if (n > most) n = most;
+                w[j][e] = load_float(rw, n * 4);
+                if (!p.bias) continue;
+                if constexpr (kHalf) v[e] = __builtin_bit_cast(float, static_cast<uint32_t>(__builtin_amdgcn_raw_buffer_load_b16(rb, n * 2, 0, 0)) << 16);
+                else v[e] = load_float(rb, n * 4);
+            }
+            Unit<Tag>::pack(v, b[j]);
         }
     }
-    wait_loads();                            // also what the wave has sent for into LDS: its next wait would wait for these stores
+};
+
+// Where every row of y starts at a multiple of eight outputs they are stored as they lie in the lanes.
+template <typename C, typename Tag, int TM, int TN>
+__device__ inline void store_products(const ProductArgs& p, const typename Mac<C, Tag>::Sum (&acc)[TM][TN], const Scales<Tag, TM, TN>& s,
+                                      int64_t m0, int64_t n0) {
+    constexpr bool kHalf = std::is_same<Tag, bf16_io>::value;
+    const int lane = threadIdx.x & (kWave - 1);
+    const bool whole = p.N % 8 == 0;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         const int64_t m = m0 + i * 16 + (lane & 15);
@@ -134,25 +169,32 @@ __device__ inline void store_products(const ProductArgs& a, const typename Mac<C
             const int64_t n = n0 + j * 32 + (lane >> 4) * 8;
             float v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                v[e] = static_cast<float>(acc[i][2 * j + e / 4][e % 4]) * sa[i] * sw[j][e];
-                if (a.bias) v[e] += b[j][e];
+            for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(acc[i][2 * j + e / 4][e % 4]) * s.a[i] * s.w[j][e];
+            if (p.bias) {
+                float b[8];
+                Unit<Tag>::unpack(s.b[j], b);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += b[e];
             }
-            if (m >= a.M || n >= a.N) continue;
+            if (m >= p.M || n >= p.N) continue;
             if (whole) {
-                char* y = static_cast<char*>(a.y) + (m * a.N + n) * IO<Tag>::kBytes;
-                if constexpr (kHalf) *reinterpret_cast<u32x4*>(y) = IO<Tag>::pack(v);
-                else {
-                    *reinterpret_cast<f32x4*>(y) = f32x4{v[0], v[1], v[2], v[3]};
-                    *reinterpret_cast<f32x4*>(y + 16) = f32x4{v[4], v[5], v[6], v[7]};
+                char* y = static_cast<char*>(p.y) + (m * p.N + n) * IO<Tag>::kBytes;
+                u32x4 q[kHalf ? 1 : 2];
+                if constexpr (kHalf) q[0] = IO<Tag>::pack(v);
+                else Unit<f32_io>::pack(v, q);
+#pragma unroll
+                for (int h = 0; h < (kHalf ? 1 : 2); ++h) {
+                    u32x4* to = reinterpret_cast<u32x4*>(y) + h;
+                    if (p.keep) *to = q[h];
+                    else __builtin_nontemporal_store(q[h], to);
                 }
                 continue;
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if (n + e >= a.N) continue;
-                if constexpr (kHalf) static_cast<__bf16*>(a.y)[m * a.N + n + e] = static_cast<__bf16>(v[e]);
-                else static_cast<float*>(a.y)[m * a.N + n + e] = v[e];
+                if (n + e >= p.N) continue;
+                if constexpr (kHalf) static_cast<__bf16*>(p.y)[m * p.N + n + e] = static_cast<__bf16>(v[e]);
+                else static_cast<float*>(p.y)[m * p.N + n + e] = v[e];
             }
         }
     }
@@ -169,10 +211,10 @@ __global__ __launch_bounds__(WM* WN* kWave, 1) void product_tile_kernel(const Pr
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WM, wn = wave / WM;
-    const int64_t id = static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x;
+    const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x;
     if (id >= a.tiles) return;
     const Tile tile = tile_of(a, id);
-    const int64_t m0 = tile.m * BM, n0 = tile.n * BN;
+    const int64_t m0 = static_cast<int64_t>(tile.m) * BM, n0 = static_cast<int64_t>(tile.n) * BN;
     const int K = a.K, steps = (K + kBlockK - 1) / kBlockK;
 
     // what a lane fetches: row slot (i*NW + wave)*8 + lane/8, sixteen features; the slot of eight sixteens is permuted by
@@ -236,7 +278,9 @@ __global__ __launch_bounds__(WM* WN* kWave, 1) void product_tile_kernel(const Pr
         __syncthreads();
     }
 
-    store_products<C, Tag, TM, TN>(a, acc, m0 + wm * TM * 16, n0 + wn * TN * 16);
+    Scales<Tag, TM, TN> scales;
+    scales.load(a, m0 + wm * TM * 16, n0 + wn * TN * 16);
+    store_products<C, Tag, TM, TN>(a, acc, scales, m0 + wm * TM * 16, n0 + wn * TN * 16);
 }
 
 // ---- large products ------------------------------------------------------------------------------------------------
@@ -256,8 +300,9 @@ __device__ inline void load_lds(Row src, uint32_t offset, int uniform, const uin
 //   waves 0-3  read a(t), w(t); send for a(t+1)    multiply t; wait                     read a(t+1), w(t+1); ...
 //   waves 4-7  multiply t-1; wait                  read a(t), w(t); send for w(t+2)     multiply t; wait
 //
-// A block takes tiles until there are none: the first steps of the next tile are on their way while the outputs of the last
-// one are stored, and the stores reach memory while the next tile is computed.
+// A block takes tiles until there are none, and the steps of all of them are one sequence: the next tile's first steps are sent
+// for in the last steps of this one, whose outputs are stored in front of the next reading phase.  There are two steps to a
+// tile at least.
 template <typename C, typename Tag>
 __global__ __launch_bounds__(8 * kWave, 2) void product_large_kernel(const ProductArgs a) {
     using mac = Mac<C, Tag>;
@@ -273,42 +318,34 @@ __global__ __launch_bounds__(8 * kWave, 2) void product_large_kernel(const Produ
     // by the row, so that the eight rows that a fragment's lanes read at a time lie in different banks.  Rows beyond the last
     // one are the last one.
     const int c = (lane & 7) ^ (lane >> 3), quarter = wave & 3, slot = quarter * 8 + (lane >> 3);
-    const uint32_t xfirst = static_cast<uint32_t>(slot) * K + c * 16;
-    const uint32_t wfirst = static_cast<uint32_t>(((slot >> 2) & 3) * 8 + ((slot >> 4) & 1) * 4 + (slot & 3)) * K + c * 16;
-    int64_t m0 = 0, n0 = 0;
-    uint32_t xlast = 0, wlast = 0;
-    auto aim = [&](const Tile& t) __attribute__((always_inline)) {
-        m0 = t.m * BM;
-        n0 = t.n * BN;
-        const int64_t m = a.M - 1 - m0, n = a.N - 1 - n0;
-        xlast = static_cast<uint32_t>(m < BM ? m : BM - 1) * K + c * 16;
-        wlast = static_cast<uint32_t>(n < BN ? n : BN - 1) * K + c * 16;
+    const int row = second ? ((slot >> 2) & 3) * 8 + ((slot >> 4) & 1) * 4 + (slot & 3) : slot;
+    const uint32_t first = static_cast<uint32_t>(row) * K + c * 16;
+    struct Source {
+        int64_t at;                                            // of the tile's first row
+        uint32_t last;                                         // a lane's offset in the last row that it may read
     };
-    auto bring = [&](bool x, uint8_t* to, int t) __attribute__((always_inline)) {
-        const Row src = row_of(x ? a.a : a.w, (x ? m0 : n0) * K, 0x7fffffffu);
-        const uint32_t last = x ? xlast : wlast;
-        uint32_t first = x ? xfirst : wfirst;
-        asm volatile("" : "+v"(first));                        // the addresses are formed here, not kept in registers across the loop
+    auto source = [&](const Tile& t) __attribute__((always_inline)) {
+        const int64_t r0 = static_cast<int64_t>(second ? t.n : t.m) * 256, left = (second ? a.N : a.M) - 1 - r0;
+        return Source{r0 * K, static_cast<uint32_t>(left < 255 ? left : 255) * K + c * 16};
+    };
+    const void* matrix = second ? a.w : a.a;
+    auto bring = [&](const Source& s, uint8_t* to, int t) __attribute__((always_inline)) {
+        const Row src = row_of(matrix, s.at, 0x7fffffffu);
+        uint32_t off0 = first;
+        asm volatile("" : "+v"(off0));                         // the addresses are formed here, not kept in registers across the loop
         if (t < whole) {
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
-                const uint32_t off = first + i * 32 * K;
-                load_lds(src, off < last ? off : last, t * kBlockK, to + (i * 4 + quarter) * 1024);
+                const uint32_t off = off0 + i * 32 * K;
+                load_lds(src, off < s.last ? off : s.last, t * kBlockK, to + (i * 4 + quarter) * 1024);
             }
-        } else if (t < steps) {
+        } else {
             const int left = K - t * kBlockK - c * 16;         // codes of this lane's sixteen that exist: a multiple of 8
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
-                const uint32_t off = first + i * 32 * K;
-                *reinterpret_cast<u32x4*>(to + (i * 4 + quarter) * 1024 + lane * 16) = load_codes16(src, off < last ? off : last, t * kBlockK, left);
+                const uint32_t off = off0 + i * 32 * K;
+                *reinterpret_cast<u32x4*>(to + (i * 4 + quarter) * 1024 + lane * 16) = load_codes16(src, off < s.last ? off : s.last, t * kBlockK, left);
             }
-        }
-    };
-    auto first_steps = [&]() __attribute__((always_inline)) {
-        if (second) bring(false, sw + kPart, 1);
-        else {
-            bring(true, sx, 0);
-            bring(false, sw, 0);
         }
     };
 
@@ -317,59 +354,70 @@ __global__ __launch_bounds__(8 * kWave, 2) void product_large_kernel(const Produ
         return mac::frag(*reinterpret_cast<const i32x4*>(p + fo), *reinterpret_cast<const i32x4*>(p + (fo ^ 64)));
     };
 
-    int64_t id = blockIdx.x;
-    aim(tile_of(a, id));
-    first_steps();
+    uint32_t id = blockIdx.x;
+    Tile tile = tile_of(a, id), next = tile;
+    Source here = source(tile), there = here;
+    const int ahead = second ? 2 : 1;
+    bring(here, second ? sw : sx, 0);
+    if (second) bring(here, sw + kPart, 1);
     wait_loads();
     __builtin_amdgcn_s_barrier();
+    if (second) __builtin_amdgcn_s_barrier();
+    int odd = 0, at = 0;                                       // the step's buffers, its number modulo 2 and 3
 #pragma unroll 1
     while (true) {
+        id += gridDim.x;
+        const bool more = id < a.tiles;
+        if (more) {
+            next = tile_of(a, id);
+            there = source(next);
+        }
         typename mac::Sum acc[TM][TN];
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j) acc[i][j] = mac::zero();
-        if (second) __builtin_amdgcn_s_barrier();
-        int at = 0;                                            // t modulo 3
-#pragma unroll 1
-        for (int t = 0; t < steps; ++t) {
+        Scales<Tag, TM, TN> scales;
+        const int64_t m = static_cast<int64_t>(tile.m) * BM + wm * TM * 16, n = static_cast<int64_t>(tile.n) * BN + wn * TN * 16;
+
+        auto step = [&](int t) __attribute__((always_inline)) {
             typename mac::Frag xf[TM], wf[TN];
-            const uint8_t *px = sx + (t & 1) * kPart + wm * TM * 16 * kBlockK, *pw = sw + at * kPart + wn * TN * 16 * kBlockK;
+            const uint8_t *px = sx + odd * kPart + wm * TM * 16 * kBlockK, *pw = sw + at * kPart + wn * TN * 16 * kBlockK;
 #pragma unroll
             for (int j = 0; j < TN; ++j) wf[j] = frag(pw + j * 16 * kBlockK);
 #pragma unroll
             for (int i = 0; i < TM; ++i) xf[i] = frag(px + i * 16 * kBlockK);
             __builtin_amdgcn_sched_barrier(0);
-            if (second) bring(false, sw + (at == 0 ? 2 : at - 1) * kPart, t + 2);
-            else bring(true, sx + (~t & 1) * kPart, t + 1);
+            uint8_t* to = second ? sw + (at == 0 ? 2 : at - 1) * kPart : sx + (odd ^ 1) * kPart;
+            if (t + ahead < steps) bring(here, to, t + ahead);
+            else if (more) bring(there, to, t + ahead - steps);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+            for (int i = 0; i < TM; ++i) {
 #pragma unroll
                 for (int h = 0; h < mac::kParts; ++h)
 #pragma unroll
                     for (int j = 0; j < TN; ++j) acc[i][j] = mac::add(wf[j], xf[i], acc[i][j], h);
+            }
             __builtin_amdgcn_s_setprio(0);
             __builtin_amdgcn_sched_barrier(0);
             wait_loads();
             __builtin_amdgcn_s_barrier();
             at = at == 2 ? 0 : at + 1;
-        }
-
-        const int64_t m = m0 + wm * TM * 16, n = n0 + wn * TN * 16;
-        id += gridDim.x;
-        const bool more = id < a.tiles;
-        if (more) {
-            aim(tile_of(a, id));
-            first_steps();
-        }
-        store_products<C, Tag, TM, TN>(a, acc, m, n);
-        if (!second) __builtin_amdgcn_s_barrier();
+            odd ^= 1;
+        };
+#pragma unroll 1
+        for (int t = 0; t < steps; ++t) step(t);
+        scales.load(a, m, n);
+        store_products<C, Tag, TM, TN>(a, acc, scales, m, n);
         if (!more) break;
+        tile = next;
+        here = there;
     }
+    if (!second) __builtin_amdgcn_s_barrier();
 }
 
 }  // namespace lnmod
