@@ -920,6 +920,7 @@ struct ProductArgs {
     int64_t M, N;
     int32_t K;
     int32_t keep;              // whether y stays in the caches
+    int32_t wide;              // whether eight scales and biases may be read at once
     // set by deal_tiles: how the tiles are dealt to the blocks
     int32_t tiles_m, tiles_n;
     uint32_t tiles, each, more;
@@ -936,6 +937,6 @@ inline void deal_tiles(ProductArgs& a, int bm, int bn) {
     a.band_of = Divider(static_cast<uint32_t>(kBandRows) * a.tiles_n);
     a.row_of = Divider(a.tiles_m % kBandRows ? a.tiles_m % kBandRows : kBandRows);
 }
-hipError_t launch_product(int dtype, int code, const ProductArgs& a, hipStream_t st);
+hipError_t launch_product(int dtype, int code, ProductArgs a, hipStream_t st);
 
 }  // namespace lnmod

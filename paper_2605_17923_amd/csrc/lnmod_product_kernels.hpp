@@ -72,6 +72,12 @@ template <> struct Mac<e4m3_code, f32_io> {
 
 typedef uint8_t __attribute__((address_space(3))) lds_byte;
 
+// A barrier that no access to memory is moved across.
+__device__ inline void meet() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
 __device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 
 // Sixteen codes of a row of which `left` exist (a multiple of 8, or fewer than 1), the others 0.
@@ -108,23 +114,26 @@ struct Scales {
     float a[TM], w[TN / 2][8];
     u32x4 b[TN / 2][Unit<Tag>::NV];
     // m0 and n0 are uniform; rows and features beyond the last one have the last one's
-    __device__ inline void load(const ProductArgs& p, int64_t m0, int64_t n0) {
-        constexpr int kBytes = IO<Tag>::kBytes;
+    __device__ inline void load_rows(const ProductArgs& p, int64_t m0) {
         const int lane = threadIdx.x & (kWave - 1);
         const int rows = static_cast<int>(p.M - 1 - m0 < TM * 16 ? p.M - 1 - m0 : TM * 16);
-        const int most = static_cast<int>(p.N - 1 - n0 < TN * 16 ? p.N - 1 - n0 : TN * 16);
-        const Row ra = row_of(p.sa, m0 * 4, 0x7fffffffu), rw = row_of(p.sw, n0 * 4, 0x7fffffffu);
-        const Row rb = row_of(p.bias, n0 * kBytes, 0x7fffffffu);
+        const Row ra = row_of(p.sa, m0 * 4, 0x7fffffffu);
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             const int m = i * 16 + (lane & 15);
             a[i] = load_float(ra, (m < rows ? m : rows) * 4);
         }
-        if (p.N % 8 == 0) {                  // eight at a time, whatever they are aligned to
+    }
+    // of the pairs of fragments from `from` to `to` - 1
+    __device__ inline void load_features(const ProductArgs& p, int64_t n0, int from, int to) {
+        constexpr int kBytes = IO<Tag>::kBytes;
+        const int lane = threadIdx.x & (kWave - 1);
+        const int most = static_cast<int>(p.N - 1 - n0 < TN * 16 ? p.N - 1 - n0 : TN * 16);
+        const Row rw = row_of(p.sw, n0 * 4, 0x7fffffffu), rb = row_of(p.bias, n0 * kBytes, 0x7fffffffu);
 #pragma unroll
-            for (int j = 0; j < TN / 2; ++j) {
-                int n = j * 32 + (lane >> 4) * 8;
-                if (n > most) n = most - 7;
+        for (int j = from; j < to; ++j) {
+            const int n = j * 32 + (lane >> 4) * 8;
+            if (p.wide && n + 7 <= most) {   // eight at a time, whatever they are aligned to
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const f32x4 t = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, n * 4 + 16 * h, 0, 0));
@@ -134,39 +143,37 @@ struct Scales {
                 if (!p.bias) continue;
 #pragma unroll
                 for (int h = 0; h < Unit<Tag>::NV; ++h) b[j][h] = __builtin_amdgcn_raw_buffer_load_b128(rb, n * kBytes + 16 * h, 0, 0);
+                continue;
             }
-            return;
-        }
-#pragma unroll
-        for (int j = 0; j < TN / 2; ++j) {
             float v[8] = {};
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                int n = j * 32 + (lane >> 4) * 8 + e;
-                if (n > most) n = most;
-                w[j][e] = load_float(rw, n * 4);
+                const int at = n + e < most ? n + e : most;
+                w[j][e] = load_float(rw, at * 4);
                 if (!p.bias) continue;
-                if constexpr (kHalf) v[e] = __builtin_bit_cast(float, static_cast<uint32_t>(__builtin_amdgcn_raw_buffer_load_b16(rb, n * 2, 0, 0)) << 16);
-                else v[e] = load_float(rb, n * 4);
+                if constexpr (kHalf) v[e] = __builtin_bit_cast(float, static_cast<uint32_t>(__builtin_amdgcn_raw_buffer_load_b16(rb, at * 2, 0, 0)) << 16);
+                else v[e] = load_float(rb, at * 4);
             }
             Unit<Tag>::pack(v, b[j]);
         }
     }
 };
 
-// Where every row of y starts at a multiple of eight outputs they are stored as they lie in the lanes.
+// Eight outputs of a lane are stored at once, at any element's address; those of the last features one by one.
 template <typename C, typename Tag, int TM, int TN>
-__device__ inline void store_products(const ProductArgs& p, const typename Mac<C, Tag>::Sum (&acc)[TM][TN], const Scales<Tag, TM, TN>& s,
-                                      int64_t m0, int64_t n0) {
+__device__ inline void store_products(const ProductArgs& p, const typename Mac<C, Tag>::Sum (&acc)[TM][TN], int64_t m0, int64_t n0) {
     constexpr bool kHalf = std::is_same<Tag, bf16_io>::value;
     const int lane = threadIdx.x & (kWave - 1);
-    const bool whole = p.N % 8 == 0;
+    Scales<Tag, TM, TN> s;
+    s.load_rows(p, m0);
+    if (kHalf) s.load_features(p, n0, 0, TN / 2);
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int64_t m = m0 + i * 16 + (lane & 15);
+    for (int j = 0; j < TN / 2; ++j) {
+        if (!kHalf) s.load_features(p, n0, j, j + 1);                // float32 biases of all pairs at once would not fit beside the sums
+        const int64_t n = n0 + j * 32 + (lane >> 4) * 8;
 #pragma unroll
-        for (int j = 0; j < TN / 2; ++j) {
-            const int64_t n = n0 + j * 32 + (lane >> 4) * 8;
+        for (int i = 0; i < TM; ++i) {
+            const int64_t m = m0 + i * 16 + (lane & 15);
             float v[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(acc[i][2 * j + e / 4][e % 4]) * s.a[i] * s.w[j][e];
@@ -177,16 +184,15 @@ __device__ inline void store_products(const ProductArgs& p, const typename Mac<C
                 for (int e = 0; e < 8; ++e) v[e] += b[e];
             }
             if (m >= p.M || n >= p.N) continue;
-            if (whole) {
-                char* y = static_cast<char*>(p.y) + (m * p.N + n) * IO<Tag>::kBytes;
-                u32x4 q[kHalf ? 1 : 2];
-                if constexpr (kHalf) q[0] = IO<Tag>::pack(v);
-                else Unit<f32_io>::pack(v, q);
+            if (n + 8 <= p.N) {
+                typedef u32x4 loose __attribute__((aligned(2)));
+                loose* y = reinterpret_cast<loose*>(static_cast<char*>(p.y) + (m * p.N + n) * IO<Tag>::kBytes);
+                u32x4 q[Unit<Tag>::NV];
+                Unit<Tag>::pack(v, q);
 #pragma unroll
-                for (int h = 0; h < (kHalf ? 1 : 2); ++h) {
-                    u32x4* to = reinterpret_cast<u32x4*>(y) + h;
-                    if (p.keep) *to = q[h];
-                    else __builtin_nontemporal_store(q[h], to);
+                for (int h = 0; h < Unit<Tag>::NV; ++h) {
+                    if (p.keep) y[h] = q[h];
+                    else __builtin_nontemporal_store(q[h], y + h);
                 }
                 continue;
             }
@@ -200,90 +206,6 @@ __device__ inline void store_products(const ProductArgs& p, const typename Mac<C
     }
 }
 
-// BM x BN outputs per block of WM x WN waves.
-template <typename C, typename Tag, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM* WN* kWave, 1) void product_tile_kernel(const ProductArgs a) {
-    constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
-    constexpr int XI = BM / 8 / NW, WI = BN / 8 / NW;          // loads of a wave for each operand and step
-    static_assert(TN % 2 == 0 && XI * 8 * NW == BM && WI * 8 * NW == BN, "tile");
-    __shared__ __attribute__((aligned(1024))) uint8_t sx[2][BM * kBlockK], sw[2][BN * kBlockK];
-
-    const int lane = threadIdx.x & (kWave - 1);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave % WM, wn = wave / WM;
-    const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x;
-    if (id >= a.tiles) return;
-    const Tile tile = tile_of(a, id);
-    const int64_t m0 = static_cast<int64_t>(tile.m) * BM, n0 = static_cast<int64_t>(tile.n) * BN;
-    const int K = a.K, steps = (K + kBlockK - 1) / kBlockK;
-
-    // what a lane fetches: row slot (i*NW + wave)*8 + lane/8, sixteen features; the slot of eight sixteens is permuted by
-    // the row, so that eight consecutive rows of a fragment lie in different banks
-    const int c = (lane & 7) ^ (lane >> 3);
-    uint32_t xo[XI], wo[WI];
-#pragma unroll
-    for (int i = 0; i < XI; ++i) {
-        int64_t r = (i * NW + wave) * 8 + (lane >> 3);
-        if (m0 + r >= a.M) r = a.M - 1 - m0;
-        xo[i] = static_cast<uint32_t>(r) * K + c * 16;
-    }
-#pragma unroll
-    for (int i = 0; i < WI; ++i) {
-        const int slot = (i * NW + wave) * 8 + (lane >> 3);
-        int64_t r = (slot & ~31) + ((slot >> 2) & 3) * 8 + ((slot >> 4) & 1) * 4 + (slot & 3);
-        if (n0 + r >= a.N) r = a.N - 1 - n0;
-        wo[i] = static_cast<uint32_t>(r) * K + c * 16;
-    }
-    const Row xrow = row_of(a.a, m0 * K, 0x7fffffffu), wrow = row_of(a.w, n0 * K, 0x7fffffffu);
-
-    auto fetch = [&](Row src, const uint32_t* off, int count, uint8_t* dst, int t) {
-        const int k0 = t * kBlockK;
-        if (k0 + kBlockK <= K) {
-            for (int i = 0; i < count; ++i)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_byte*)(dst + (i * NW + wave) * 1024), 16, off[i], k0, 0, 0);
-        } else {
-            const int left = K - k0 - c * 16;                  // codes of this lane's sixteen that exist: a multiple of 8
-            for (int i = 0; i < count; ++i)
-                *reinterpret_cast<u32x4*>(dst + (i * NW + wave) * 1024 + lane * 16) = load_codes16(src, off[i], k0, left);
-        }
-    };
-
-    using mac = Mac<C, Tag>;
-    typename mac::Sum acc[TM][TN];
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = mac::zero();
-
-    const int fo = (lane & 15) * kBlockK + (((lane >> 4) ^ (lane & 7)) << 4);
-    for (int t = 0; t < steps; ++t) {
-        fetch(xrow, xo, XI, sx[0], t);
-        fetch(wrow, wo, WI, sw[0], t);
-        __syncthreads();
-        typename mac::Frag xf[TM];
-#pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            const uint8_t* p = sx[0] + (wm * TM + i) * 16 * kBlockK;
-            xf[i] = mac::frag(*reinterpret_cast<const i32x4*>(p + fo), *reinterpret_cast<const i32x4*>(p + (fo ^ 64)));
-        }
-#pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            const uint8_t* p = sw[0] + (wn * TN + j) * 16 * kBlockK;
-            const typename mac::Frag wf = mac::frag(*reinterpret_cast<const i32x4*>(p + fo), *reinterpret_cast<const i32x4*>(p + (fo ^ 64)));
-#pragma unroll
-            for (int h = 0; h < mac::kParts; ++h)
-#pragma unroll
-                for (int i = 0; i < TM; ++i) acc[i][j] = mac::add(wf, xf[i], acc[i][j], h);
-        }
-        __syncthreads();
-    }
-
-    Scales<Tag, TM, TN> scales;
-    scales.load(a, m0 + wm * TM * 16, n0 + wn * TN * 16);
-    store_products<C, Tag, TM, TN>(a, acc, scales, m0 + wm * TM * 16, n0 + wn * TN * 16);
-}
-
-// ---- large products ------------------------------------------------------------------------------------------------
 // 1024 bytes from global memory into LDS, sixteen from each lane's address, at dst + 16 lane.  In assembly because the compiler
 // makes every later read of LDS wait for such a load, whatever part of LDS it fills: no register is written here, and whoever
 // reads dst has waited for this wave's vmcnt and met the others at a barrier first.
@@ -292,6 +214,223 @@ __device__ inline void load_lds(Row src, uint32_t offset, int uniform, const uin
     asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(offset), "s"(src), "s"(uniform), "s"(at) : "m0");
 }
 
+// ---- ordinary products ---------------------------------------------------------------------------------------------
+// BM x BN outputs per block: GROUPS teams of WM x WN waves, each of which takes every GROUPS-th step, has STAGES of them in LDS, of
+// which one is multiplied while the others are on their way, and adds its sums to the first team's at the end.
+template <typename C, typename Tag, int BM, int BN, int WM, int WN, int STAGES, int GROUPS>
+__global__ __launch_bounds__(GROUPS* WM* WN* kWave) void product_tile_kernel(const ProductArgs a) {
+    using mac = Mac<C, Tag>;
+    constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
+    constexpr int kPieces = (BM + BN) / 8 / NW, kStage = (BM + BN) * kBlockK;
+    static_assert(TN % 2 == 0 && kPieces * 8 * NW == BM + BN && BM % 8 == 0 && STAGES >= 2, "tile");
+    __shared__ __attribute__((aligned(1024))) uint8_t shared[GROUPS * STAGES * kStage];
+    const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x;
+    if (id >= a.tiles) return;
+    const Tile tile = tile_of(a, id);
+    const int64_t m0 = static_cast<int64_t>(tile.m) * BM, n0 = static_cast<int64_t>(tile.n) * BN;
+
+    const int lane = threadIdx.x & (kWave - 1);
+    const int group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / NW, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % NW;
+    const int wm = wave % WM, wn = wave / WM;
+    uint8_t* stage = shared + group * STAGES * kStage;         // rows of w, then rows of a
+    const int K = a.K, whole = K / kBlockK, steps = (K + kBlockK - 1) / kBlockK;
+
+    // what a lane brings: piece i*NW + wave has eight rows, of which a lane has sixteen features of one; the sixteens of a row
+    // are exchanged by the row, so that the eight rows that a fragment's lanes read at a time lie in different banks.  Rows
+    // beyond the last one are the last one.
+    const int c = (lane & 7) ^ (lane >> 3);
+    uint32_t off[kPieces];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+        const int slot = (i * NW + wave) * 8 + (lane >> 3);
+        int64_t r = slot - BN, most = a.M - 1 - m0;
+        if (slot < BN) {
+            r = (slot & ~31) + ((slot >> 2) & 3) * 8 + ((slot >> 4) & 1) * 4 + (slot & 3);
+            most = a.N - 1 - n0;
+        }
+        off[i] = static_cast<uint32_t>(r < most ? r : most) * K + c * 16;
+    }
+    const Row xrow = row_of(a.a, m0 * K, 0x7fffffffu), wrow = row_of(a.w, n0 * K, 0x7fffffffu);
+    auto bring = [&](uint8_t* to, int t) __attribute__((always_inline)) {
+        if (t < whole) {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+                load_lds((i * NW + wave) * 8 < BN ? wrow : xrow, off[i], t * kBlockK, to + (i * NW + wave) * 1024);
+        } else if (t < steps) {
+            const int left = K - t * kBlockK - c * 16;         // codes of this lane's sixteen that exist: a multiple of 8
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+                *reinterpret_cast<u32x4*>(to + (i * NW + wave) * 1024 + lane * 16) =
+                    load_codes16((i * NW + wave) * 8 < BN ? wrow : xrow, off[i], t * kBlockK, left);
+        }
+    };
+
+    typename mac::Sum acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = mac::zero();
+    const int fo = (lane & 15) * kBlockK + (((lane >> 4) ^ (lane & 7)) << 4);
+    auto frag = [&](const uint8_t* p) __attribute__((always_inline)) {
+        return mac::frag(*reinterpret_cast<const i32x4*>(p + fo), *reinterpret_cast<const i32x4*>(p + (fo ^ 64)));
+    };
+
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) bring(stage + i * kStage, i * GROUPS + group);
+    int at = 0, to = STAGES - 1;                               // the buffers of this step and of the one that is sent for
+#pragma unroll 1
+    for (int t0 = 0; t0 < steps; t0 += GROUPS) {
+        const int t = t0 + group;
+        // loads come back in their order: with the whole steps behind t still on their way, t is here
+        if (t + (STAGES - 2) * GROUPS < whole) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kPieces * (STAGES - 2)) : "memory");
+        else wait_loads();
+        meet();                          // and every wave is done with the buffer that is filled now
+        bring(stage + to * kStage, t + (STAGES - 1) * GROUPS);
+        const uint8_t *pw = stage + at * kStage + wn * TN * 16 * kBlockK, *px = stage + at * kStage + (BN + wm * TM * 16) * kBlockK;
+        if (GROUPS == 1 || t < steps) {
+            typename mac::Frag xf[TM];
+#pragma unroll
+            for (int i = 0; i < TM; ++i) xf[i] = frag(px + i * 16 * kBlockK);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const typename mac::Frag wf = frag(pw + j * 16 * kBlockK);
+#pragma unroll
+                for (int h = 0; h < mac::kParts; ++h)
+#pragma unroll
+                    for (int i = 0; i < TM; ++i) acc[i][j] = mac::add(wf, xf[i], acc[i][j], h);
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // its reads are done when it meets the others
+        at = at == STAGES - 1 ? 0 : at + 1;
+        to = to == STAGES - 1 ? 0 : to + 1;
+    }
+    if constexpr (GROUPS > 1) {
+        typedef typename mac::Sum Sum;
+        static_assert((GROUPS - 1) * BM * BN * 4 <= GROUPS * STAGES * kStage, "sums");
+        Sum* sums = reinterpret_cast<Sum*>(shared) + wave * kWave + lane;
+        constexpr int kEach = NW * kWave;                      // of a fragment, all waves of a team
+        meet();
+        if (group > 0) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) sums[((group - 1) * TM * TN + i * TN + j) * kEach] = acc[i][j];
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        meet();
+        if (group > 0) return;
+#pragma unroll
+        for (int g = 0; g < GROUPS - 1; ++g)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] += sums[(g * TM * TN + i * TN + j) * kEach];
+    }
+    store_products<C, Tag, TM, TN>(a, acc, m0 + wm * TM * 16, n0 + wn * TN * 16);
+}
+
+// ---- few rows --------------------------------------------------------------------------------------------------------
+// Up to 16 TM rows of a: w is read once, straight into registers, and that takes all the time there is.  A block has 16 TN
+// features of y; its waves share out the steps and add their sums in LDS, wave by wave.
+template <typename C, typename Tag, int TM, int TN, int DEPTH, int kFewWaves>
+__global__ __launch_bounds__(kFewWaves* kWave) void product_few_kernel(const ProductArgs a) {
+    using mac = Mac<C, Tag>;
+    typedef typename mac::Sum Sum;
+    constexpr int kRows = 16 * TM, kFeatures = 16 * TN;
+    __shared__ Sum part[kFewWaves][TM * TN][kWave];
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int K = a.K, whole = K / kBlockK;
+    const int64_t n0 = (static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * kFeatures;
+    if (n0 >= a.N) return;
+    const Row xrow = row_of(a.a, 0, 0x7fffffffu), wrow = row_of(a.w, n0 * K, 0x7fffffffu);
+    uint32_t xo[TM], wo[TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int r = i * 16 + (lane & 15), most = static_cast<int>(a.M) - 1;
+        xo[i] = static_cast<uint32_t>(r < most ? r : most) * K + (lane >> 4) * 16;
+    }
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        const int64_t r = j * 16 + (lane & 15), most = a.N - 1 - n0;
+        wo[j] = static_cast<uint32_t>(r < most ? r : most) * K + (lane >> 4) * 16;
+    }
+
+    Sum acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = mac::zero();
+    auto multiply = [&](const i32x4 (&x)[TM][2], const i32x4 (&w)[TN][2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const typename mac::Frag xf = mac::frag(x[i][0], x[i][1]);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const typename mac::Frag wf = mac::frag(w[j][0], w[j][1]);
+#pragma unroll
+                for (int h = 0; h < mac::kParts; ++h) acc[i][j] = mac::add(wf, xf, acc[i][j], h);
+            }
+        }
+    };
+    // DEPTH steps are requested before the first of them is multiplied; steps beyond the whole ones are read again and not used
+    for (int t = wave; t < whole; t += DEPTH * kFewWaves) {
+        i32x4 x[DEPTH][TM][2], w[DEPTH][TN][2];
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            const int k0 = (t + d * kFewWaves < whole ? t + d * kFewWaves : t) * kBlockK;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int j = 0; j < TN; ++j) w[d][j][h] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(wrow, wo[j] + 64 * h, k0, 0));
+#pragma unroll
+                for (int i = 0; i < TM; ++i) x[d][i][h] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(xrow, xo[i] + 64 * h, k0, 0));
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d)
+            if (t + d * kFewWaves < whole) multiply(x[d], w[d]);
+    }
+    if (K % kBlockK != 0 && wave == whole % kFewWaves) {
+        i32x4 x[TM][2], w[TN][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int left = K - whole * kBlockK - (lane >> 4) * 16 - 64 * h;
+#pragma unroll
+            for (int j = 0; j < TN; ++j) w[j][h] = __builtin_bit_cast(i32x4, load_codes16(wrow, wo[j] + 64 * h, whole * kBlockK, left));
+#pragma unroll
+            for (int i = 0; i < TM; ++i) x[i][h] = __builtin_bit_cast(i32x4, load_codes16(xrow, xo[i] + 64 * h, whole * kBlockK, left));
+        }
+        multiply(x, w);
+    }
+
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) part[wave][i * TN + j][lane] = acc[i][j];
+    __syncthreads();
+    // fragment f of lane l: rows of a 16 (f / TN) + l % 16, features 16 (f % TN) + 4 (l / 16) .. + 3
+    for (int o = threadIdx.x; o < kRows * kFeatures; o += kFewWaves * kWave) {
+        const int m = o / kFeatures, f = o % kFeatures;
+        const int64_t n = n0 + f;
+        if (m >= a.M || n >= a.N) continue;
+        const int frag = (m / 16) * TN + f / 16, l = (f % 16) / 4 * 16 + m % 16, e = f % 4;
+        auto sum = part[0][frag][l][e];
+#pragma unroll
+        for (int w = 1; w < kFewWaves; ++w) sum += part[w][frag][l][e];
+        float v = static_cast<float>(sum) * a.sa[m] * a.sw[n];
+        if constexpr (std::is_same<Tag, bf16_io>::value) {
+            if (a.bias) v += static_cast<float>(static_cast<const __bf16*>(a.bias)[n]);
+            static_cast<__bf16*>(a.y)[m * a.N + n] = static_cast<__bf16>(v);
+        } else {
+            if (a.bias) v += static_cast<const float*>(a.bias)[n];
+            static_cast<float*>(a.y)[m * a.N + n] = v;
+        }
+    }
+}
+
+// ---- large products ------------------------------------------------------------------------------------------------
 // 256 x 256 outputs by eight waves of 128 x 64, two on each SIMD that take turns: while one reads the fragments of its next 128
 // features from LDS and sends for the features after them, the other multiplies.  Waves 0 to 3 bring a, one step ahead into
 // two buffers, waves 4 to 7 w, two steps ahead into three.
@@ -361,8 +500,8 @@ __global__ __launch_bounds__(8 * kWave, 2) void product_large_kernel(const Produ
     bring(here, second ? sw : sx, 0);
     if (second) bring(here, sw + kPart, 1);
     wait_loads();
-    __builtin_amdgcn_s_barrier();
-    if (second) __builtin_amdgcn_s_barrier();
+    meet();
+    if (second) meet();
     int odd = 0, at = 0;                                       // the step's buffers, its number modulo 2 and 3
 #pragma unroll 1
     while (true) {
@@ -377,7 +516,6 @@ __global__ __launch_bounds__(8 * kWave, 2) void product_large_kernel(const Produ
         for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j) acc[i][j] = mac::zero();
-        Scales<Tag, TM, TN> scales;
         const int64_t m = static_cast<int64_t>(tile.m) * BM + wm * TM * 16, n = static_cast<int64_t>(tile.n) * BN + wn * TN * 16;
 
         auto step = [&](int t) __attribute__((always_inline)) {
@@ -392,7 +530,7 @@ __global__ __launch_bounds__(8 * kWave, 2) void product_large_kernel(const Produ
             if (t + ahead < steps) bring(here, to, t + ahead);
             else if (more) bring(there, to, t + ahead - steps);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
+            meet();
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -405,19 +543,18 @@ __global__ __launch_bounds__(8 * kWave, 2) void product_large_kernel(const Produ
             __builtin_amdgcn_s_setprio(0);
             __builtin_amdgcn_sched_barrier(0);
             wait_loads();
-            __builtin_amdgcn_s_barrier();
+            meet();
             at = at == 2 ? 0 : at + 1;
             odd ^= 1;
         };
 #pragma unroll 1
         for (int t = 0; t < steps; ++t) step(t);
-        scales.load(a, m, n);
-        store_products<C, Tag, TM, TN>(a, acc, scales, m, n);
+        store_products<C, Tag, TM, TN>(a, acc, m, n);
         if (!more) break;
         tile = next;
         here = there;
     }
-    if (!second) __builtin_amdgcn_s_barrier();
+    if (!second) meet();
 }
 
 }  // namespace lnmod

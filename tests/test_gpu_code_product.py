@@ -67,7 +67,7 @@ def test_product(size, code, dtype):
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("code", ["int8", "e4m3"])
 @pytest.mark.parametrize("size", [(2049, 2056, 128), (4097, 1030, 24), (2305, 1900, 256), (300, 16001, 136), (8200, 520, 384),
-                                  (2048, 2048, 520), (8200, 2330, 264), (70001, 300, 72)], ids=str)
+                                  (2048, 2048, 520), (8200, 2330, 264), (70001, 300, 72), (33000, 520, 520), (4100, 4104, 1416)], ids=str)
 def test_large_product(size, code, dtype):
     product(code, dtype, *size, bias=size[0] % 2 == 1, whole=True)
     if (code == "int8" or dtype == torch.float32) and size[0] < 8000:
