@@ -210,6 +210,7 @@ int rotary_args(lnmod::RotaryArgs& a, int64_t B, int64_t S, int64_t q_heads, int
     a.rot.half = static_cast<int32_t>(width / 2);
     a.rot.axes = r.axes;
     a.rot.per_token = r.position_rows != S;
+    a.rot.part = width < head_dim;
     for (int i = 0, first = 0; i < LNMOD_MAX_AXES; ++i) {
         a.rot.first[i] = i < r.axes ? first : INT32_MAX;
         if (i < r.axes) first += r.features[i] / 2;

@@ -12,8 +12,9 @@ constexpr uint32_t kRowOfBlocks = uint32_t{1} << 21;   // a dimension of a grid 
 // for each of the steps that a block's teams take in turn, `more` for each further block that shares a CU's round.  The
 // numbers are least squares to 173 random products of int8 codes and 87 of e4m3 codes to float32 (M 1 to 12 000, N 16 to
 // 16 384, K 136 to 14 400, half of the N no multiples of 8) with every one of these kernels.  The kernel that this picks takes
-// 1.026 of the fastest one's time in the mean and 1.05 in nine of ten (float32 from e4m3 1.003, 1.00).  Picking one kernel
-// for all would cost, in the mean: 128 x 128 1.9 times the fastest, 32 x 32 2.5 times.
+// 1.026 of the fastest one's time in the mean and 1.05 in nine of ten (float32 from e4m3 1.003, 1.00).  One kernel
+// for all int8 problems would take in the mean 1.5 (32 x 64), 1.7 (64 x 64), 2.1 (32 x 32), 2.6 (128 x 128) or 4.5 (256 x 256)
+// times the fastest one's time, each of them 3 to 14 times at its worst.
 struct Cost {
     float step, more, tile, start;
 };

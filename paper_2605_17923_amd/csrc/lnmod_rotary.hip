@@ -1,4 +1,6 @@
 // lnmod_rotary.hip -- plan, instantiation and launch of the rotation and of the query and key norm with it.
+#include <algorithm>
+
 #include "lnmod_rotary_kernels.hpp"
 
 namespace lnmod {
@@ -22,24 +24,25 @@ struct Bwd {
     }
 };
 
-template <template <typename, int, bool, int> class Go, typename Tag, int NORM, bool HALVES>
-bool by_vpl(const RotaryArgs& a, const RotaryShape& sh, hipStream_t st) {
-    const unsigned blocks = static_cast<unsigned>(a.side[0].blocks + a.side[1].blocks);
-    const unsigned threads = static_cast<unsigned>(sh.block_waves * kWave);
-    switch (sh.vpl) {
-        case 1: Go<Tag, NORM, HALVES, 1>::go(a, blocks, threads, st); return true;
-        case 2: Go<Tag, NORM, HALVES, 2>::go(a, blocks, threads, st); return true;
-        case 3: Go<Tag, NORM, HALVES, 3>::go(a, blocks, threads, st); return true;
-        case 4: Go<Tag, NORM, HALVES, 4>::go(a, blocks, threads, st); return true;
-        default: break;
-    }
-    if constexpr (std::is_same<Tag, f32_io>::value && NORM == kRowNorm) {
-        if (sh.vpl == 8) {
-            Go<Tag, NORM, HALVES, 8>::go(a, blocks, threads, st);
-            return true;
-        }
+// Units of a lane that are compiled: a row of 8192 features by eight waves needs four, eight in fp32.
+constexpr bool has_vpl(bool f32, int norm, int vpl) { return vpl <= 4 || (f32 && norm == kRowNorm && vpl == 8); }
+
+template <template <typename, int, bool, int> class Go, typename Tag, int NORM, bool HALVES, int VPL>
+bool one_vpl(const RotaryArgs& a, const RotaryShape& sh, hipStream_t st) {
+    if constexpr (has_vpl(std::is_same<Tag, f32_io>::value, NORM, VPL)) {
+        if (sh.vpl != VPL) return false;
+        const unsigned blocks = static_cast<unsigned>(a.side[0].blocks + a.side[1].blocks);
+        Go<Tag, NORM, HALVES, VPL>::go(a, blocks, static_cast<unsigned>(sh.block_waves * kWave), st);
+        return true;
     }
     return false;
+}
+
+template <template <typename, int, bool, int> class Go, typename Tag, int NORM, bool HALVES>
+bool by_vpl(const RotaryArgs& a, const RotaryShape& sh, hipStream_t st) {
+    return one_vpl<Go, Tag, NORM, HALVES, 1>(a, sh, st) || one_vpl<Go, Tag, NORM, HALVES, 2>(a, sh, st) ||
+           one_vpl<Go, Tag, NORM, HALVES, 3>(a, sh, st) || one_vpl<Go, Tag, NORM, HALVES, 4>(a, sh, st) ||
+           one_vpl<Go, Tag, NORM, HALVES, 8>(a, sh, st);
 }
 
 template <template <typename, int, bool, int> class Go, int NORM>
@@ -53,33 +56,49 @@ void lay_out(RotaryArgs& a, int dtype) {
     a.g_log2 = ceil_log2(a.units);
 }
 
-RotaryShape shape_for(const RotaryArgs& a, int dtype, int norm, bool backward) {
-    const int32_t heads[2] = {a.side[0].heads, a.side[1].heads};
-    return rotary_shape(dtype, heads, a.g_log2, norm, backward);
+// Launch shapes, from sweeps of 1 to 4 units a lane, 1 to 8 waves a block and 1 to 128 blocks a CU over 40 problems (both types,
+// 4 to 64 heads of 64 to 256 features, 1560 to 75 600 tokens).
+//
+// Three units a lane where nothing is against it: more loads in flight than with fewer, and registers for four waves a SIMD.
+// Forwards four, where a round of heads is less idle so.  Backwards, where a CU holds eight waves, two or three, whichever
+// leaves it fewer empty (backward of 28 heads of 128: 389 us with three units in three waves, 235 with two in four).  Blocks are
+// what a CU holds at once where a block stays for long: with a norm over rows, whose weights it has loaded (forward of 64 heads
+// of 128: 203 us with four blocks a CU where three fit, 188 with three), and backwards, whose partial sums it keeps; three times
+// that if the queries' blocks and the keys' have rows of different lengths to do (28 and 4 heads: 235 -> 204 us).  Else, and
+// where blocks of three waves would have to be packed four to a CU, which they are after an idle moment (32 760 x 40 x 128:
+// 238 us) but not while another kernel drains (316, with 32 blocks a CU 244), more of them even out the CUs (75 600 x 40 x 128
+// without a norm: 586 us with blocks of four waves, 550 with two tokens side by side in eight).
+RotaryShape shape_for(const RotaryArgs& a, int norm, bool backward) {
+    int rounds = 1;
+    for (const RotarySide& s : a.side) {
+        if (s.heads == 0) continue;
+        const int r = head_split(s.heads, a.g_log2).rounds;
+        if (r > rounds) rounds = r;
+    }
+    const auto waves_of = [&](int vpl) { return (rounds + vpl - 1) / vpl; };
+    int vpl = 3;
+    if (backward) {
+        const auto held = [&](int vpl) { return 8 / waves_of(vpl) * waves_of(vpl); };
+        if (held(2) > held(3) || (held(2) == held(3) && waves_of(2) * 2 < waves_of(3) * 3)) vpl = 2;
+    } else if (waves_of(4) * 4 < waves_of(3) * 3 || (norm == kRowNorm && rounds > 6)) {
+        vpl = 4;
+    }
+    if (vpl > rounds) vpl = rounds;
+    if (norm == kRowNorm) {                                          // eight waves hold a row
+        while (waves_of(vpl) > 8) vpl = vpl < 4 ? vpl + 1 : 8;
+    }
+    int waves = waves_of(vpl);
+    if (waves > 8) waves = 8;
+    if (waves < 4) waves = waves * (4 / waves);
+    else if (waves == 4 && norm == kNoNorm) waves = 8;
+    const int resident = backward ? 8 : vpl <= 3 ? 16 : vpl == 4 ? 12 : 8;             // waves of a CU, see LNMOD_OCCUPANCY
+    const bool stays = backward || (norm == kRowNorm && waves != 3);
+    int per_cu = stays ? std::max(1, resident / waves) : 32;
+    if (backward && a.side[0].heads != a.side[1].heads) per_cu *= 3;
+    return {vpl, waves, per_cu};
 }
 
 }  // namespace
-
-RotaryShape rotary_shape(int dtype, const int32_t (&heads)[2], int g_log2, int norm, bool backward) {
-    int rounds = 1;
-    for (const int32_t h : heads) {
-        if (h == 0) continue;
-        const int r = head_split(h, g_log2).rounds;
-        if (r > rounds) rounds = r;
-    }
-    (void)backward;
-    int vpl = rounds <= 8 ? (rounds + 3) / 4 : rounds <= 16 ? 2 : rounds <= 24 ? 3 : 4;
-    if (dtype == 1 && norm == kRowNorm && rounds > 32) vpl = 8;
-    int waves = (rounds + vpl - 1) / vpl;
-    if (waves > 8) waves = 8;
-    if (waves < 4) waves = waves * (4 / waves);
-    return {vpl, waves};
-}
-
-int64_t rotary_blocks_per_cu(int norm, bool backward) {
-    (void)norm;
-    return backward ? 2 : 16;
-}
 
 void rotary_bwd_slots(int dtype, int64_t N, const int32_t (&heads)[2], int head_dim, int norm, int64_t (&slots)[2]) {
     RotaryArgs a{};
@@ -87,14 +106,14 @@ void rotary_bwd_slots(int dtype, int64_t N, const int32_t (&heads)[2], int head_
     a.head_dim = head_dim;
     for (int t = 0; t < 2; ++t) a.side[t].heads = heads[t];
     lay_out(a, dtype);
-    plan_rotary(a, shape_for(a, dtype, norm, true), norm != kRowNorm, rotary_blocks_per_cu(norm, true));
+    plan_rotary(a, shape_for(a, norm, true), norm != kRowNorm);
     for (int t = 0; t < 2; ++t) slots[t] = a.side[t].blocks;
 }
 
 hipError_t launch_rotary_fwd(int dtype, int norm, bool halves, RotaryArgs a, hipStream_t st) {
     lay_out(a, dtype);
-    const RotaryShape sh = shape_for(a, dtype, norm, false);
-    plan_rotary(a, sh, norm != kRowNorm, rotary_blocks_per_cu(norm, false));
+    const RotaryShape sh = shape_for(a, norm, false);
+    plan_rotary(a, sh, norm != kRowNorm);
     a.sample_of = Divider(static_cast<uint32_t>(a.S));
     const bool ok = norm == kNoNorm    ? by_type<Fwd, kNoNorm>(dtype, halves, a, sh, st)
                     : norm == kRowNorm ? by_type<Fwd, kRowNorm>(dtype, halves, a, sh, st)
@@ -105,8 +124,8 @@ hipError_t launch_rotary_fwd(int dtype, int norm, bool halves, RotaryArgs a, hip
 hipError_t launch_rotary_bwd(int dtype, int norm, bool halves, RotaryArgs a, void* const (&dw)[2], bool io_grads, float* ws,
                              hipStream_t st) {
     lay_out(a, dtype);
-    const RotaryShape sh = shape_for(a, dtype, norm, true);
-    plan_rotary(a, sh, norm != kRowNorm, rotary_blocks_per_cu(norm, true));
+    const RotaryShape sh = shape_for(a, norm, true);
+    plan_rotary(a, sh, norm != kRowNorm);
     a.sample_of = Divider(static_cast<uint32_t>(a.S));
     RotaryDwArgs r{};
     int widest = 0;
@@ -124,7 +143,7 @@ hipError_t launch_rotary_bwd(int dtype, int norm, bool halves, RotaryArgs a, voi
     if (!ok) return hipErrorInvalidConfiguration;
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const dim3 grid(static_cast<unsigned>((widest + kWave - 1) / kWave), 2);
+    const dim3 grid(static_cast<unsigned>((widest + kDwFeatures - 1) / kDwFeatures), 2);
     if (io_grads && dtype == 0) hipLaunchKernelGGL((rotary_dw_kernel<bf16_io>), grid, dim3(16 * kWave), 0, st, r);
     else hipLaunchKernelGGL((rotary_dw_kernel<f32_io>), grid, dim3(16 * kWave), 0, st, r);
     return hipGetLastError();

@@ -20,6 +20,7 @@ struct RotaryPlan {
     int32_t axes;
     int32_t per_token;
     int32_t first[kMaxAxes];         // first pair of each axis
+    int32_t part;                    // a head has features that are not turned
 };
 
 // One of the two tensors, and how its tokens and heads are shared out.
@@ -56,7 +57,7 @@ struct RotaryDwArgs {
 enum RotaryNorm { kNoNorm = 0, kRowNorm = 1, kHeadNorm = 2 };
 
 struct RotaryShape {
-    int vpl, block_waves;
+    int vpl, block_waves, per_cu;    // units of a lane, waves of a block, blocks of a CU (both tensors together)
 };
 
 inline int ceil_log2(int64_t v) {
@@ -75,8 +76,8 @@ inline HeadSplit head_split(int heads, int g_log2) {
     return {hs, (heads + (1 << hs) - 1) >> hs};
 }
 
-// Fills the shares of both tensors; `per_cu`: blocks of both tensors together.
-inline void plan_rotary(RotaryArgs& a, const RotaryShape& sh, bool chunked, int64_t per_cu) {
+// Fills the shares of both tensors.
+inline void plan_rotary(RotaryArgs& a, const RotaryShape& sh, bool chunked) {
     int64_t weight[2] = {0, 0};
     for (int t = 0; t < 2; ++t) {
         RotarySide& s = a.side[t];
@@ -103,16 +104,14 @@ inline void plan_rotary(RotaryArgs& a, const RotaryShape& sh, bool chunked, int6
         if (s.heads == 0) continue;
         const int64_t tokens = static_cast<int64_t>(s.teams) << (6 - a.g_log2 - s.hs_log2);
         const int64_t need = (a.N + tokens - 1) / tokens;
-        int64_t most = kNumCU * per_cu * weight[t] / ((weight[0] + weight[1]) * s.chunks);
+        int64_t most = static_cast<int64_t>(kNumCU) * sh.per_cu * weight[t] / ((weight[0] + weight[1]) * s.chunks);
         if (most < 1) most = 1;
         s.members = static_cast<int32_t>(need < most ? need : most);
         s.blocks = s.members * s.chunks;
     }
 }
 
-RotaryShape rotary_shape(int dtype, const int32_t (&heads)[2], int g_log2, int norm, bool backward);
-int64_t rotary_blocks_per_cu(int norm, bool backward);
-// slots of partial weight gradients of q and of k (the same for every element type's plan or more)
+// slots of partial weight gradients of q and of k
 void rotary_bwd_slots(int dtype, int64_t N, const int32_t (&heads)[2], int head_dim, int norm, int64_t (&slots)[2]);
 
 hipError_t launch_rotary_fwd(int dtype, int norm, bool halves, RotaryArgs a, hipStream_t st);

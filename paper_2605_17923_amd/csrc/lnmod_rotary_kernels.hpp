@@ -54,11 +54,11 @@ struct UnitPlace {
         return static_cast<int>((e < P ? lo : hi) / IO<Tag>::kBytes) + (e < P ? e : e - P);
     }
 
+    // Runs of eight bytes share their lines with another access of the wave, which finds them in the cache (24 x 96 bf16, a norm
+    // for each head, 130 us past the caches, 120 so).
     __device__ inline u32x4 load(const char* head) const {
         if (!HALVES) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(head + lo));
-        const u32x2 a = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(head + lo));
-        const u32x2 b = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(head + hi));
-        return u32x4{a[0], a[1], b[0], b[1]};
+        return load_cached(head);
     }
     __device__ inline u32x4 load_cached(const char* head) const {
         if (!HALVES) return *reinterpret_cast<const u32x4*>(head + lo);
@@ -70,8 +70,8 @@ struct UnitPlace {
             __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(head + lo));
             return;
         }
-        __builtin_nontemporal_store(u32x2{v[0], v[1]}, reinterpret_cast<u32x2*>(head + lo));
-        __builtin_nontemporal_store(u32x2{v[2], v[3]}, reinterpret_cast<u32x2*>(head + hi));
+        *reinterpret_cast<u32x2*>(head + lo) = u32x2{v[0], v[1]};
+        *reinterpret_cast<u32x2*>(head + hi) = u32x2{v[2], v[3]};
     }
 };
 
@@ -97,14 +97,15 @@ __device__ inline void angles_of(const RotaryPlan& r, const UnitPlace<Tag, HALVE
 
 // Features beyond the turned ones pass as they are, whatever stands in them.
 template <typename Tag, bool HALVES>
-__device__ inline void turn(const UnitPlace<Tag, HALVES>& at, const Angles<IO<Tag>::E / 2>& t, float sign, float (&v)[IO<Tag>::E]) {
+__device__ inline void turn(const RotaryPlan& r, const UnitPlace<Tag, HALVES>& at, const Angles<IO<Tag>::E / 2>& t, float sign,
+                            float (&v)[IO<Tag>::E]) {
 #pragma unroll
     for (int i = 0; i < IO<Tag>::E / 2; ++i) {
         const int a = at.first_of(i), b = at.second_of(i);
         const float u = v[a], w = v[b], s = t.s[i] * sign;
         const float x = __builtin_fmaf(u, t.c[i], -(w * s)), y = __builtin_fmaf(u, s, w * t.c[i]);
-        v[a] = at.turned[i] ? x : u;
-        v[b] = at.turned[i] ? y : w;
+        v[a] = !r.part || at.turned[i] ? x : u;
+        v[b] = !r.part || at.turned[i] ? y : w;
     }
 }
 
@@ -144,9 +145,14 @@ struct Lanes {
     }
 };
 
+__device__ inline void zero_unless(bool keep, u32x4& q) {
+    const uint32_t m = keep ? ~0u : 0u;
+    q &= u32x4{m, m, m, m};
+}
+
 // NORM: 0 none, 1 over a token's row, 2 over each head
 template <typename Tag, int NORM, bool HALVES, int VPL>
-__global__ __launch_bounds__(8 * kWave) void rotary_fwd_kernel(const RotaryArgs a) {
+__global__ __launch_bounds__(8 * kWave) LNMOD_OCCUPANCY(VPL <= 3 ? 4 : VPL == 4 ? 3 : 2) void rotary_fwd_kernel(const RotaryArgs a) {
     using io = IO<Tag>;
     constexpr int E = io::E;
     __shared__ float sums[2][8];
@@ -202,10 +208,11 @@ __global__ __launch_bounds__(8 * kWave) void rotary_fwd_kernel(const RotaryArgs 
             float q = 0.0f;
 #pragma unroll
             for (int i = 0; i < VPL; ++i) {
+                zero_unless(ok[i], raw[i]);
                 float v[E];
                 io::unpack(raw[i], v);
 #pragma unroll
-                for (int e = 0; e < E; ++e) q += ok[i] ? v[e] * v[e] : 0.0f;
+                for (int e = 0; e < E; ++e) q = __builtin_fmaf(v[e], v[e], q);
             }
             q = lanes_sum(q, a.g_log2 + side.hs_log2);
             if (side.waves > 1) {
@@ -221,13 +228,14 @@ __global__ __launch_bounds__(8 * kWave) void rotary_fwd_kernel(const RotaryArgs 
         char* y = static_cast<char*>(side.y) + n * (static_cast<int64_t>(side.heads) * head_bytes);
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
+            if (NORM == 2) zero_unless(me.unit, raw[i]);
             float v[E];
             io::unpack(raw[i], v);
             if (NORM == 2) {
                 float q = 0.0f;
 #pragma unroll
-                for (int e = 0; e < E; ++e) q += v[e] * v[e];
-                q = lanes_sum(me.unit ? q : 0.0f, a.g_log2);
+                for (int e = 0; e < E; ++e) q = __builtin_fmaf(v[e], v[e], q);
+                q = lanes_sum(q, a.g_log2);
                 rs = 1.0f / sqrtf(q * side.inv_width + a.eps);
                 if (here && ok[i] && (me.lane & ((1 << a.g_log2) - 1)) == 0)
                     side.rstd[n * side.heads + head0 + ((i * side.waves + me.part) << side.hs_log2) + me.slot] = rs;
@@ -236,7 +244,7 @@ __global__ __launch_bounds__(8 * kWave) void rotary_fwd_kernel(const RotaryArgs 
 #pragma unroll
                 for (int e = 0; e < E; ++e) v[e] = (v[e] * rs) * W[NORM == 1 ? i : 0][e];
             }
-            turn(at, ang, a.sign, v);
+            turn(a.rot, at, ang, a.sign, v);
             if (here && ok[i]) at.store(y + out[i], io::pack(v));
         }
 #pragma unroll
@@ -317,6 +325,9 @@ __global__ __launch_bounds__(8 * kWave) void rotary_bwd_kernel(const RotaryArgs 
         fetch(base + stride, nxt, ngrad, nrs, nang);
         const int64_t n = base + (static_cast<int64_t>(me.team) << tokens_log2) + me.sub;
         const bool here = n < a.N;
+        // gradients that do not count are zeros: x beside them is a row's own, so that no product is NaN but the row's own
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) zero_unless(here && ok[i], grad[i]);
         float c = 0.0f;
         if (NORM == 1) {
 #pragma unroll
@@ -324,13 +335,12 @@ __global__ __launch_bounds__(8 * kWave) void rotary_bwd_kernel(const RotaryArgs 
                 float x[E], g[E];
                 io::unpack(raw[i], x);
                 io::unpack(grad[i], g);
-                turn(at, ang, -1.0f, g);
-                const bool count = here && ok[i];
+                turn(a.rot, at, ang, -1.0f, g);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    const float h = x[e] * rs[0], p = g[e] * h;
-                    c += count ? p * W[i][e] : 0.0f;
-                    acc[i][e] += count ? p : 0.0f;
+                    const float p = g[e] * (x[e] * rs[0]);
+                    c = __builtin_fmaf(p, W[i][e], c);
+                    acc[i][e] += p;
                 }
             }
             c = lanes_sum(c, a.g_log2 + side.hs_log2);
@@ -348,18 +358,17 @@ __global__ __launch_bounds__(8 * kWave) void rotary_bwd_kernel(const RotaryArgs 
             float x[E], g[E];
             io::unpack(raw[i], x);
             io::unpack(grad[i], g);
-            turn(at, ang, -1.0f, g);
+            turn(a.rot, at, ang, -1.0f, g);
             const float r = rs[NORM == 1 ? 0 : i];
             if (NORM == 2) {
                 c = 0.0f;
-                const bool count = here && ok[i];
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    const float h = x[e] * r, p = g[e] * h;
-                    c += p * W[0][e];
-                    acc[0][e] += count ? p : 0.0f;
+                    const float p = g[e] * (x[e] * r);
+                    c = __builtin_fmaf(p, W[0][e], c);
+                    acc[0][e] += p;
                 }
-                c = lanes_sum(me.unit ? c : 0.0f, a.g_log2);
+                c = lanes_sum(c, a.g_log2);
             }
             const float k = c * side.inv_width;
 #pragma unroll
@@ -408,22 +417,47 @@ __global__ __launch_bounds__(8 * kWave) void rotary_bwd_kernel(const RotaryArgs 
     }
 }
 
-// Second pass: the slots of both tensors, added in their order by sixteen waves that each take every sixteenth.
+// Second pass: the slots of both tensors, in an order that only their number sets.  Few bytes that a chain of loads would
+// wait for, so a block takes 16 features by 64 slots at a time, eight of those loads under way: 512 slots of 5120 features 6.4 us
+// with 64 features by 16 slots, 5.6 us so; 1536 slots of 96 features 4.7 us so.
+constexpr int kDwFeatures = 16, kDwRows = 16 * kWave / kDwFeatures;
+
 template <typename Tag>
 __global__ __launch_bounds__(16 * kWave) void rotary_dw_kernel(const RotaryDwArgs a) {
-    __shared__ float part[16][kWave];
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
+    __shared__ float part[kDwRows][kDwFeatures + 1];
+    const int at = threadIdx.x % kDwFeatures, row = threadIdx.x / kDwFeatures;
     const int t = blockIdx.y;
-    const int f = blockIdx.x * kWave + lane;
+    const int f = blockIdx.x * kDwFeatures + at;
     const int width = a.width[t];
     float s = 0.0f;
-    if (f < width)
-        for (int i = wave; i < a.slots[t]; i += 16) s += a.ws[t][static_cast<int64_t>(i) * width + f];
-    part[wave][lane] = s;
-    __syncthreads();
-    if (wave || f >= width) return;
+    if (f < width) {
+        const float* from = a.ws[t] + f;
+        int i = row;
+        for (; i + 7 * kDwRows < a.slots[t]; i += 8 * kDwRows) {
+            float v[8];
 #pragma unroll
-    for (int w = 1; w < 16; ++w) s += part[w][lane];
+            for (int j = 0; j < 8; ++j) v[j] = from[static_cast<int64_t>(i + j * kDwRows) * width];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s += v[j];
+        }
+        float v[7];                                                  // fewer than eight are left
+#pragma unroll
+        for (int j = 0; j < 7; ++j) {
+            const int slot = i + j * kDwRows;
+            v[j] = slot < a.slots[t] ? from[static_cast<int64_t>(slot) * width] : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 7; ++j) s += v[j];
+    }
+    part[row][at] = s;
+    __syncthreads();
+    if (row >= 4 || f >= width) return;                              // one wave; its four rows add sixteen each
+    s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kDwRows / 4; ++j) s += part[row * (kDwRows / 4) + j][at];
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    if (row) return;
     if constexpr (std::is_same<Tag, bf16_io>::value) static_cast<__bf16*>(a.dw[t])[f] = static_cast<__bf16>(s);
     else static_cast<float*>(a.dw[t])[f] = s;
 }
