@@ -12,7 +12,9 @@ constexpr uint32_t kRowOfBlocks = uint32_t{1} << 21;   // a dimension of a grid 
 // for each of the steps that a block's teams take in turn, `more` for each further block that shares a CU's round.  The
 // numbers are least squares to 173 random products of int8 codes and 87 of e4m3 codes to float32 (M 1 to 12 000, N 16 to
 // 16 384, K 136 to 14 400, half of the N no multiples of 8) with every one of these kernels.  The kernel that this picks takes
-// 1.026 of the fastest one's time in the mean and 1.05 in nine of ten (float32 from e4m3 1.003, 1.00).  One kernel
+// 1.026 of the fastest one's time in the mean and 1.05 in nine of ten (float32 from e4m3 1.003, 1.00).  The kernel for few rows
+// was measured by itself, on 400 problems of up to 16 rows against the first three of the others: 1.04 and 1.13 (with blocks of
+// sixteen waves 1.08, 1.23; of four waves with four steps under way 1.07, 1.21).  One kernel
 // for all int8 problems would take in the mean 1.5 (32 x 64), 1.7 (64 x 64), 2.1 (32 x 32), 2.6 (128 x 128) or 4.5 (256 x 256)
 // times the fastest one's time, each of them 3 to 14 times at its worst.
 struct Cost {
@@ -23,7 +25,7 @@ struct Variant {
     Cost cost[2];                      // one instruction for a product's eight bits, or four through half precision
 };
 constexpr Variant kVariants[] = {
-    {16, 16, 16, 2, {{1.19f, 0.59f, 0.94f, 0.82f}, {1.09f, 1.68f, 0.22f, 1.51f}}},       // few rows
+    {16, 16, 8, 2, {{0.470f, 0.939f, 0.0f, 2.14f}, {0.499f, 0.853f, 0.0f, 2.14f}}},      // few rows
     {32, 32, 4, 1, {{0.452f, 0.0f, 1.77f, 1.43f}, {0.614f, 0.0f, 1.76f, 1.31f}}},
     {32, 64, 2, 2, {{0.328f, 0.338f, 1.51f, 2.05f}, {0.488f, 0.324f, 1.73f, 1.94f}}},
     {64, 64, 2, 1, {{0.473f, 0.0f, 2.32f, 1.47f}, {0.647f, 0.0f, 3.03f, 1.09f}}},
@@ -72,7 +74,7 @@ hipError_t go(ProductArgs a, hipStream_t st) {
     switch (pick(a.M, a.N, a.K, kHalves)) {
         case kFew: {
             const uint32_t blocks = static_cast<uint32_t>((a.N + 15) / 16), x = blocks < kRowOfBlocks ? blocks : kRowOfBlocks;
-            hipLaunchKernelGGL((product_few_kernel<C, Tag, 1, 1, 2, 16>), dim3(x, (blocks + x - 1) / x), dim3(16 * kWave), 0, st, a);
+            hipLaunchKernelGGL((product_few_kernel<C, Tag, 1, 1, 2, 8>), dim3(x, (blocks + x - 1) / x), dim3(8 * kWave), 0, st, a);
             break;
         }
         case 1: tiles<C, Tag, 32, 32, 2, 1, 4, 4>(a, st); break;
