@@ -589,11 +589,11 @@ int lnmod_rotary(const lnmod_heads* q, const lnmod_heads* k, int64_t B, int64_t 
                  int64_t head_dim, const lnmod_rotation* rotation, int inverse, void* stream, void* q_out, void* k_out,
                  int dtype) {
     const bool both = k_heads != 0;
-    if (!q || !rotation || (k != nullptr) != both || (k_out != nullptr) != both) return LNMOD_EINVAL;
+    if (!q || !rotation || (k != nullptr) != both) return LNMOD_EINVAL;
     lnmod::RotaryArgs a{};
     const int st = rotary_args(a, B, S, q_heads, k_heads, head_dim, *rotation, dtype);
-    if (st != LNMOD_OK || a.N == 0) return st;
-    if (!q_out) return LNMOD_EINVAL;
+    if (st != LNMOD_OK || a.N == 0) return st;                // without tokens the results have no address either
+    if (!q_out || (k_out != nullptr) != both) return LNMOD_EINVAL;
     const lnmod_heads* x[2] = {q, k};
     void* y[2] = {q_out, k_out};
     for (int t = 0; t < (both ? 2 : 1); ++t) {

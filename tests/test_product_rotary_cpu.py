@@ -97,6 +97,15 @@ def test_rotary_rejections():
     assert rotary(S=0) == OK and rotary(B=0, r=rot(pos=None)) == OK
 
 
+def test_no_tokens_need_no_addresses():
+    for B, S in ((1, 0), (0, 5), (2, 0)):
+        none = dict(B=B, S=S, q=heads(None), k=heads(None), r=rot(pos=None, rows=0), qo=None, ko=None)
+        assert rotary(**none) == OK and rotary(**none, dtype=1) == OK
+        assert fwd(**none, wq=None, wk=None, rq=None, rk=None) == OK
+        assert rotary(**{**none, "r": rot(axes=(8, 4, 6))}) == EUNS
+    assert rotary(ko=None) == EINVAL and rotary(k=None, hk=0) == EINVAL
+
+
 def test_norm_with_rotation_rejections():
     for call, names in ((fwd, ("wq", "wk", "qo", "ko", "rq", "rk")), (bwd, ("wq", "wk", "dq", "dk", "rq", "rk", "dwq", "dwk"))):
         for name in names:
