@@ -223,6 +223,48 @@ def test_beyond_four_gigabytes(interleaved):
     assert torch.equal(got, lnmod.rotary(q[-9:, :2].clone(), None, pos[-9:].clone(), table, axes, interleaved)[0])
 
 
+# Heads that take 1 to 57 rounds of a wave's lanes, with idle lanes and without: one to eight units a lane, one to eight waves a
+# token, two tokens a block, tokens side by side in a wave, heads in pieces for different blocks.
+MANY = [(128, (4, 3)), (128, (8, 5)), (128, (12, 12)), (128, (17, 16)), (128, (28, 4)), (128, (36, 20)), (128, (52, 8)), (128, (64, 41)),
+        (72, (113, 60)), (72, (29, 97)), (40, (200, 3)), (256, (32, 7)), (8, (1000, 33)), (24, (65, 341)), (136, (60, 1))]
+
+
+@BOTH
+@pytest.mark.parametrize("shape", MANY, ids=str)
+def test_every_launch_shape(shape, dtype):
+    hd, heads = shape
+    R = hd // 16 * 16 or 8
+    for interleaved, tokens in ((True, 53), (False, 700)):
+        for per_head in (False, True):
+            c = Case(dtype, lead=(tokens,), heads=heads, hd=hd, axes=(R // 2, R // 2), interleaved=interleaved, per_head=per_head)
+            yq, yk, rq, rk = lnmod.qknorm_rotary_forward(c.q, c.k, c.wq, c.wk, c.pos, c.table, c.axes, interleaved, EPS)
+            c.check_forward(yq, c.q, c.wq, "q")
+            c.check_forward(yk, c.k, c.wk, "k")
+            dq, dk, dwq, dwk = lnmod.qknorm_rotary_backward(c.dq, c.dk, c.q, c.k, c.wq, c.wk, rq, rk, c.pos, c.table, c.axes, interleaved)
+            c.check_backward(dq, dwq, c.q, c.wq, c.dq, "q")
+            c.check_backward(dk, dwk, c.k, c.wk, c.dk, "k")
+        for y, x in zip(lnmod.rotary(c.q, c.k, c.pos, c.table, c.axes, interleaved), (c.q, c.k)):
+            x = x.double().cpu()
+            near(y.cpu(), c.turn(x), 4 * U * c.turn(x, magnitude=True), "rotation")
+
+
+@BOTH
+def test_more_heads_than_a_norm_takes(dtype):
+    """Rotation, and the norm over heads, of rows beyond 8192 features, in pieces."""
+    c = Case(dtype, lead=(31,), heads=(1000, 77), hd=128, axes=(44, 42, 42), per_head=True)
+    for y, x in zip(lnmod.rotary(c.q, c.k, c.pos, c.table, c.axes), (c.q, c.k)):
+        x = x.double().cpu()
+        near(y.cpu(), c.turn(x), 4 * U * c.turn(x, magnitude=True), "rotation")
+    yq, yk, rq, rk = lnmod.qknorm_rotary_forward(c.q, c.k, c.wq, c.wk, c.pos, c.table, c.axes, True, EPS)
+    c.check_forward(yq, c.q, c.wq, "q")
+    dq, dk, dwq, dwk = lnmod.qknorm_rotary_backward(c.dq, c.dk, c.q, c.k, c.wq, c.wk, rq, rk, c.pos, c.table, c.axes)
+    c.check_backward(dq, dwq, c.q, c.wq, c.dq, "q")
+    c.check_backward(dk, dwk, c.k, c.wk, c.dk, "k")
+    w = torch.ones(128 * 1000, dtype=dtype, device="cuda")
+    with pytest.raises(lnmod.LnmodError, match="unsupported"):
+        lnmod.qknorm_rotary_forward(c.q, c.k, w, w[:77 * 128], c.pos, c.table, c.axes)
+
+
 # ---- gradients against differences ----------------------------------------------------------------------------------------
 @pytest.mark.parametrize("per_head", [False, True], ids=["row", "head"])
 @PAIRS
