@@ -369,9 +369,11 @@ int lnmod_quantize_rows(const void* x, int64_t N, int64_t D, void* stream, void*
  *
  * a: [M, K], w: [N, K] (a linear layer's weight as it is stored), both of type `code`; a_scales: float32 [M]; w_scales: float32
  * [N]; bias: [N] in the I/O dtype or NULL; y: [M, N] in the I/O dtype, rounded once.  The sum is exact for LNMOD_INT8 (32-bit
- * integers) and float32 for LNMOD_E4M3, where a code that is NaN makes its row or column NaN.  A row with a scale of NaN is
- * NaN.  K is a multiple of 8, 8 <= K < 2^17 (LNMOD_EUNSUPPORTED); M, N < 2^31; M == 0 or N == 0 does nothing.
- * a, w and y are 16-byte aligned, the scales and bias at any of their elements' addresses.
+ * integers).  For LNMOD_E4M3 it is float32's where y is; where y is bf16 the matrix unit adds the products of eight neighbouring
+ * features with 13 bits below the largest of them, which is less than a hundredth of bf16's own rounding on ordinary values.  A
+ * code that is NaN makes its row or column NaN, as does a scale that is.  K is a multiple of 8, 8 <= K < 2^17
+ * (LNMOD_EUNSUPPORTED); M, N < 2^31; M == 0 or N == 0 does nothing.  a, w and y are 16-byte aligned, the scales and bias at any
+ * of their elements' addresses.
  */
 int lnmod_code_product(const void* a, const float* a_scales, const void* w, const float* w_scales, const void* bias,
                        int64_t M, int64_t N, int64_t K, void* stream, void* y, int dtype, int code);

@@ -1,6 +1,14 @@
 // lnmod_product_kernels.hpp -- gfx950 device code of the product of 8-bit codes that have one scale for each row.
 //
 //   y[m,n] = (sum_k a[m,k] w[n,k]) sa[m] sw[n] + bias[n]
+//
+// Three kernels, by what bounds a product (lnmod_product.hip picks).  A few rows read w once: HBM, and the 2 to 3 us that a launch
+// and a chain of loads take.  Products of some hundred rows or features have few tiles, and each step of a tile waits for the
+// caches: small tiles, several steps on their way, teams of waves that share out the sum.  Large ones are bound by the matrix
+// instructions and by what LDS gives them, 256 x 256 outputs a block.
+//
+// A step is 128 features of rows of a and of w, one cache line of each, brought straight to LDS.  The sixteen rows of w that a
+// fragment takes are chosen so that a lane ends up with eight neighbouring outputs: one store of 16 bytes in bf16.
 #pragma once
 #include "lnmod_code.hpp"
 
@@ -217,6 +225,11 @@ __device__ inline void load_lds(Row src, uint32_t offset, int uniform, const uin
 // ---- ordinary products ---------------------------------------------------------------------------------------------
 // BM x BN outputs per block: GROUPS teams of WM x WN waves, each of which takes every GROUPS-th step, has STAGES of them in LDS, of
 // which one is multiplied while the others are on their way, and adds its sums to the first team's at the end.
+//
+// What bounds it is the way from the caches: a CU has one block or two, and a step lasts as long as its lines need, however
+// small the tile (0.33 to 0.86 us, lnmod_product.hip).  So the lines of several steps are on their way at a time, teams take
+// steps side by side, and the tile is the smallest that still fills the CUs: 1025 x 2600 by 1433 to float32 13.5 us (45 in
+// tiles of the first kernel, 128 x 128), 96 x 4096 by 12 288 e4m3 12.1 us, 4.4 TB/s (50).
 template <typename C, typename Tag, int BM, int BN, int WM, int WN, int STAGES, int GROUPS>
 __global__ __launch_bounds__(GROUPS* WM* WN* kWave) void product_tile_kernel(const ProductArgs a) {
     using mac = Mac<C, Tag>;
@@ -331,7 +344,8 @@ __global__ __launch_bounds__(GROUPS* WM* WN* kWave) void product_tile_kernel(con
 
 // ---- few rows --------------------------------------------------------------------------------------------------------
 // Up to 16 TM rows of a: w is read once, straight into registers, and that takes all the time there is.  A block has 16 TN
-// features of y; its waves share out the steps and add their sums in LDS, wave by wave.
+// features of y; its waves share out the steps and add their sums in LDS, wave by wave.  1 x 1536 by 1536 int8 3.0 us, where a
+// launch that does nothing takes 2.5; 1 x 4096 by 4096 7 us.
 template <typename C, typename Tag, int TM, int TN, int DEPTH, int kFewWaves>
 __global__ __launch_bounds__(kFewWaves* kWave) void product_few_kernel(const ProductArgs a) {
     using mac = Mac<C, Tag>;
@@ -442,6 +456,11 @@ __global__ __launch_bounds__(kFewWaves* kWave) void product_few_kernel(const Pro
 // A block takes tiles until there are none, and the steps of all of them are one sequence: the next tile's first steps are sent
 // for in the last steps of this one, whose outputs are stored in front of the next reading phase.  There are two steps to a
 // tile at least.
+//
+// 32 760 x 5120 by 15 360, int8 to bf16: 128 x 128 tiles by four waves 4589 us, 256 x 256 2520, each operand brought while its waves
+// multiply and w two steps ahead 2300, tiles in turn 2187, one sequence of steps and outputs past the caches 1980 to 2040: 2.55
+// to 2.60e15 operations a second.  8190 x 5120 by 13 824 e4m3 436 us, 2.66e15.  The matrix units are busy 64 and 71 % of the
+// time; a loop of such instructions alone reaches 81 % of their peak rate.
 template <typename C, typename Tag>
 __global__ __launch_bounds__(8 * kWave, 2) void product_large_kernel(const ProductArgs a) {
     using mac = Mac<C, Tag>;

@@ -2,6 +2,9 @@
 //
 // A row stays in registers between its maximum and its codes, so it is read once: 2^lanes_log2 lanes hold a short row, K waves
 // a long one.  Rows beyond what sixteen waves hold are read twice, the second time from the caches.
+//
+// HBM bounds it: 32 760 x 5120 bf16 to e4m3 88 us, 5.7 TB/s; 1025 x 13 824 9.3 us, 4.5 TB/s, with 7 us in the bytes.  Rows of 65 to 192
+// units have two of them a lane, longer ones four (lnmod_rowcodes.hip).
 #pragma once
 #include "lnmod_code.hpp"
 
