@@ -472,14 +472,15 @@ class _on_stream:
     """Work (allocations included) goes to `stream`: None is torch's current stream; a
     torch.cuda.Stream or a raw hipStream_t handle becomes the current stream for the duration,
     so that outputs and the temporary workspace come from that stream's memory pool and are not
-    handed to another allocation while the kernels are still queued."""
+    handed to another allocation while the kernels are still queued.  Handle 0 is the default stream
+    (an ExternalStream of 0 would be a new stream of torch's pool, ordered with nothing)."""
 
     def __init__(self, stream):
         import torch
         if stream is None:
             self._ctx = None
         elif isinstance(stream, int):
-            self._ctx = torch.cuda.stream(torch.cuda.ExternalStream(stream))
+            self._ctx = torch.cuda.stream(torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream())
         else:
             self._ctx = torch.cuda.stream(stream)
 

@@ -418,6 +418,18 @@ def test_native_and_python_bindings_agree():
             assert torch.equal(y, z)
 
 
+def test_a_handle_of_zero_is_the_default_stream():
+    side = torch.cuda.Stream()
+    for around in (torch.cuda.default_stream(), side):
+        with torch.cuda.stream(around):
+            with lnmod._on_stream(0) as handle:
+                assert handle == 0 and torch.cuda.current_stream() == torch.cuda.default_stream()
+            with lnmod._on_stream(side.cuda_stream) as handle:
+                assert handle == side.cuda_stream
+            with lnmod._on_stream(None) as handle:
+                assert handle == around.cuda_stream
+
+
 # ---- used together ----------------------------------------------------------------------------------------------------------
 HEADS, KV, HD, AXES = 6, 2, 64, (16, 24, 24)
 
