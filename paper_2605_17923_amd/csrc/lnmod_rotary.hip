@@ -24,12 +24,16 @@ struct Bwd {
     }
 };
 
-// Units of a lane that are compiled: a row of 8192 features by eight waves needs four, eight in fp32.
-constexpr bool has_vpl(bool f32, int norm, int vpl) { return vpl <= 4 || (f32 && norm == kRowNorm && vpl == 8); }
+// Units of a lane that are compiled: a row of 8192 features by eight waves needs four, eight in fp32; where a lane keeps no
+// weights' sums a row, backwards have three at most.
+constexpr bool has_vpl(bool f32, int norm, int vpl, bool backward) {
+    return vpl <= 3 || (vpl == 4 && (norm == kRowNorm || !backward)) || (f32 && norm == kRowNorm && vpl == 8);
+}
 
 template <template <typename, int, bool, int> class Go, typename Tag, int NORM, bool HALVES, int VPL>
 bool one_vpl(const RotaryArgs& a, const RotaryShape& sh, hipStream_t st) {
-    if constexpr (has_vpl(std::is_same<Tag, f32_io>::value, NORM, VPL)) {
+    constexpr bool kBackward = std::is_same<Go<Tag, NORM, HALVES, VPL>, Bwd<Tag, NORM, HALVES, VPL>>::value;
+    if constexpr (has_vpl(std::is_same<Tag, f32_io>::value, NORM, VPL, kBackward)) {
         if (sh.vpl != VPL) return false;
         const unsigned blocks = static_cast<unsigned>(a.side[0].blocks + a.side[1].blocks);
         Go<Tag, NORM, HALVES, VPL>::go(a, blocks, static_cast<unsigned>(sh.block_waves * kWave), st);

@@ -265,6 +265,43 @@ def test_more_heads_than_a_norm_takes(dtype):
         lnmod.qknorm_rotary_forward(c.q, c.k, w, w[:77 * 128], c.pos, c.table, c.axes)
 
 
+@BOTH
+def test_one_tensor_and_one_pair(dtype):
+    """k None with its gradient; two features turned by a table of one row; a position of its own for every token."""
+    c = Case(dtype, lead=(3, 21), heads=(5, 2), hd=40, axes=(2,), rows=1, shared=False)
+    q = c.q.detach().requires_grad_()
+    y = F.rotary(q, None, c.pos, c.table, c.axes)
+    d, = torch.autograd.grad(y, q, c.dq)
+    z = F._Rotary.apply(q, None, c.pos, c.table, c.axes, True)
+    e, = torch.autograd.grad(z, q, c.dq)
+    assert torch.equal(y, z) and torch.equal(d, e)
+    assert torch.equal(y, c.q) and torch.equal(d, c.dq)                         # position 0 turns nothing
+    c = Case(dtype, lead=(3, 21), heads=(5, 2), hd=40, axes=(2,), shared=False)
+    for y, x in zip(lnmod.rotary(c.q, c.k, c.pos, c.table, c.axes, inverse=True), (c.q, c.k)):
+        x = x.double().cpu()
+        near(y.cpu(), c.turn(x, back=True), 4 * U * c.turn(x, magnitude=True), "one pair")
+
+
+@BOTH
+def test_repeated_samples_and_heads(dtype):
+    """Expanded inputs: a stride of 0.  Their gradients are sums over the copies: of three in float32 and one rounding, or three
+    roundings in bf16 (torch adds them)."""
+    c = Case(dtype, lead=(3, 17), heads=(4, 4), hd=64)
+    one = c.q[:1].detach().requires_grad_()
+    head = c.k[:, :, :1].detach().requires_grad_()
+    q, k = one.expand(3, -1, -1, -1), head.expand(-1, -1, 4, -1)
+    got = F.qk_norm_rotary(q, k, c.wq, c.wk, c.pos, c.table, c.axes)
+    want = F.qk_norm_rotary(q.detach().clone(), k.detach().clone(), c.wq, c.wk, c.pos, c.table, c.axes)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    grads = torch.autograd.grad(got, (one, head), (c.dq, c.dk))
+    lq, lk = (t.detach().clone().requires_grad_() for t in (q, k))
+    whole = torch.autograd.grad(F.qk_norm_rotary(lq, lk, c.wq, c.wk, c.pos, c.table, c.axes), (lq, lk), (c.dq, c.dk))
+    for g, w, dim in ((grads[0], whole[0], 0), (grads[1], whole[1], 2)):
+        w = w.double()
+        tol = 4 * torch.finfo(dtype).eps / 2 * w.abs().sum(dim, keepdim=True)
+        assert bool(((g.double() - w.sum(dim, keepdim=True)).abs() <= tol).all())
+
+
 # ---- gradients against differences ----------------------------------------------------------------------------------------
 @pytest.mark.parametrize("per_head", [False, True], ids=["row", "head"])
 @PAIRS
