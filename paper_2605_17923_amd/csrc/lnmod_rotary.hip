@@ -65,13 +65,19 @@ void lay_out(RotaryArgs& a, int dtype) {
 //
 // Three units a lane where nothing is against it: more loads in flight than with fewer, and registers for four waves a SIMD.
 // Forwards four, where a round of heads is less idle so.  Backwards, where a CU holds eight waves, two or three, whichever
-// leaves it fewer empty (backward of 28 heads of 128: 389 us with three units in three waves, 235 with two in four).  Blocks are
-// what a CU holds at once where a block stays for long: with a norm over rows, whose weights it has loaded (forward of 64 heads
-// of 128: 203 us with four blocks a CU where three fit, 188 with three), and backwards, whose partial sums it keeps; three times
-// that if the queries' blocks and the keys' have rows of different lengths to do (28 and 4 heads: 235 -> 204 us).  Else, and
-// where blocks of three waves would have to be packed four to a CU, which they are after an idle moment (32 760 x 40 x 128:
-// 238 us) but not while another kernel drains (316, with 32 blocks a CU 244), more of them even out the CUs (75 600 x 40 x 128
-// without a norm: 586 us with blocks of four waves, 550 with two tokens side by side in eight).
+// leaves it fewer empty (of 28 heads of 128: 389 us with three units in three waves, 204 with two in four), and four where two
+// waves have a row then (32 x 72: 243 us, 255 with fewer).
+//
+// Blocks forwards are what a CU holds at once where a norm over rows has its weights loaded (64 heads of 128: 203 us with four
+// blocks a CU where three fit, 188 with three).  Else, and where blocks of three waves would have to be packed four to a CU,
+// which they are after an idle moment (32 760 x 40 x 128: 238 us) but not while another kernel drains (316, with 32 blocks a CU
+// 244), more of them even out the CUs (75 600 x 40 x 128 without a norm: 586 us with blocks of four waves, 550 with two tokens
+// side by side in eight).
+//
+// Backwards a block keeps its partial sums, and one for a CU is best: of eight waves where a row takes two or more (32 760 x 40 x 128
+// 360 us in two blocks of four waves, 335 in one of eight), else of four (24 heads of 128, a norm for each: 258 us in two blocks
+// of four waves, 245 in one), twice that where a lane has two units only.  Rows of different lengths, of queries and of
+// keys, take three times as many blocks (28 and 4 heads: 235 -> 204 us).
 RotaryShape shape_for(const RotaryArgs& a, int norm, bool backward) {
     int rounds = 1;
     for (const RotarySide& s : a.side) {
@@ -84,6 +90,7 @@ RotaryShape shape_for(const RotaryArgs& a, int norm, bool backward) {
     if (backward) {
         const auto held = [&](int vpl) { return 8 / waves_of(vpl) * waves_of(vpl); };
         if (held(2) > held(3) || (held(2) == held(3) && waves_of(2) * 2 < waves_of(3) * 3)) vpl = 2;
+        if (norm == kRowNorm && rounds == 8) vpl = 4;
     } else if (waves_of(4) * 4 < waves_of(3) * 3 || (norm == kRowNorm && rounds > 6)) {
         vpl = 4;
     }
@@ -91,14 +98,18 @@ RotaryShape shape_for(const RotaryArgs& a, int norm, bool backward) {
     if (norm == kRowNorm) {                                          // eight waves hold a row
         while (waves_of(vpl) > 8) vpl = vpl < 4 ? vpl + 1 : 8;
     }
-    int waves = waves_of(vpl);
+    int waves = waves_of(vpl), per_cu = 32;
     if (waves > 8) waves = 8;
-    if (waves < 4) waves = waves * (4 / waves);
+    const bool even = a.side[0].heads == a.side[1].heads;
+    if (backward && even && norm == kRowNorm && waves > 1) waves = 8 / waves * waves;
+    else if (waves < 4) waves = waves * (4 / waves);
     else if (waves == 4 && norm == kNoNorm) waves = 8;
-    const int resident = backward ? 8 : vpl <= 3 ? 16 : vpl == 4 ? 12 : 8;             // waves of a CU, see LNMOD_OCCUPANCY
-    const bool stays = backward || (norm == kRowNorm && waves != 3);
-    int per_cu = stays ? std::max(1, resident / waves) : 32;
-    if (backward && a.side[0].heads != a.side[1].heads) per_cu *= 3;
+    if (backward) {
+        per_cu = waves > 4 || (even && vpl >= 3) ? 1 : 2;
+        if (!even) per_cu *= 3;
+    } else if (norm == kRowNorm && waves != 3) {
+        per_cu = std::max(1, (vpl <= 3 ? 16 : vpl == 4 ? 12 : 8) / waves);             // see LNMOD_OCCUPANCY
+    }
     return {vpl, waves, per_cu};
 }
 

@@ -85,14 +85,21 @@ template <int P> struct Angles {
     float c[P], s[P];
 };
 
-// Cosines and sines of a token for a lane's pairs.  A position outside the table has none: NaN.
+// A token's positions on the axes of a lane's pairs.
 template <typename Tag, bool HALVES>
-__device__ inline void angles_of(const RotaryPlan& r, const UnitPlace<Tag, HALVES>& at, int64_t row, Angles<IO<Tag>::E / 2>& out) {
-    constexpr int P = IO<Tag>::E / 2;
+__device__ inline void positions_of(const RotaryPlan& r, const UnitPlace<Tag, HALVES>& at, int64_t row, int32_t (&p)[IO<Tag>::E / 2]) {
     const int32_t* pos = r.positions + row * r.axes;
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-        const uint32_t p = static_cast<uint32_t>(pos[at.axis[i]]);
+    for (int i = 0; i < IO<Tag>::E / 2; ++i) p[i] = pos[at.axis[i]];
+}
+
+// The cosines and sines of the pairs there.  A position outside the table has none: NaN.
+template <typename Tag, bool HALVES>
+__device__ inline void angles_of(const RotaryPlan& r, const UnitPlace<Tag, HALVES>& at, const int32_t (&pos)[IO<Tag>::E / 2],
+                                 Angles<IO<Tag>::E / 2>& out) {
+#pragma unroll
+    for (int i = 0; i < IO<Tag>::E / 2; ++i) {
+        const uint32_t p = static_cast<uint32_t>(pos[i]);
         const bool known = p < r.table_rows;
         const int64_t e = static_cast<int64_t>(known ? p : 0u) * r.half + (at.turned[i] ? at.pair + i : 0);
         const f32x2 t = *reinterpret_cast<const f32x2*>(r.table + 2 * e);
@@ -196,7 +203,9 @@ __global__ __launch_bounds__(8 * kWave) LNMOD_OCCUPANCY(VPL <= 3 ? 4 : VPL == 4 
         const char* x = side.x.p + b * side.x.batch + s * side.x.token;
 #pragma unroll
         for (int i = 0; i < VPL; ++i) raw[i] = at.load(x + in[i]);
-        angles_of(a.rot, at, a.rot.per_token ? n : static_cast<int64_t>(s), ang);
+        int32_t pos[E / 2];
+        positions_of(a.rot, at, a.rot.per_token ? n : static_cast<int64_t>(s), pos);
+        angles_of(a.rot, at, pos, ang);
     };
 
     u32x4 raw[VPL];
@@ -297,9 +306,22 @@ __global__ __launch_bounds__(8 * kWave) void rotary_bwd_kernel(const RotaryArgs 
 
     const int64_t stride = (static_cast<int64_t>(side.members) * side.teams) << tokens_log2;
     const int64_t first = ((member * side.teams) << tokens_log2);
+    // Positions are loaded two steps ahead, so that a step's angles, which they choose, come with its units.  32 760 x 40 x 128,
+    // a norm over rows, in the best shape of each: 365 us with the positions loaded beside the units, 334 so (gradients with the
+    // heads in front 394 and 341).  Forwards, where blocks are many and short, the longer start costs what this saves (75 600 x
+    // 40 x 128 without a norm 536 and 530 us, 32 760 x 12 x 128 69 and 72).
+    auto token = [&](int64_t base) {
+        const int64_t n = base + (static_cast<int64_t>(me.team) << tokens_log2) + me.sub;
+        return n < a.N ? n : a.N - 1;
+    };
+    int32_t pos[E / 2];
+    auto positions = [&](int64_t base) {
+        const int64_t n = token(base);
+        const uint32_t b = a.rot.per_token ? 0u : a.sample_of(static_cast<uint32_t>(n));
+        positions_of(a.rot, at, n - static_cast<int64_t>(b) * a.S, pos);
+    };
     auto fetch = [&](int64_t base, u32x4 (&raw)[VPL], u32x4 (&grad)[VPL], float (&rs)[NORM == 1 ? 1 : VPL], Angles<E / 2>& ang) {
-        int64_t n = base + (static_cast<int64_t>(me.team) << tokens_log2) + me.sub;
-        if (n >= a.N) n = a.N - 1;
+        const int64_t n = token(base);
         const uint32_t b = a.sample_of(static_cast<uint32_t>(n)), s = static_cast<uint32_t>(n) - b * a.S;
         const char* x = side.x.p + b * side.x.batch + s * side.x.token;
         const char* g = side.dy.p + b * side.dy.batch + s * side.dy.token;
@@ -316,19 +338,22 @@ __global__ __launch_bounds__(8 * kWave) void rotary_bwd_kernel(const RotaryArgs 
                 rs[i] = side.rstd[n * side.heads + (h < side.heads ? h : side.heads - 1)];
             }
         }
-        angles_of(a.rot, at, a.rot.per_token ? n : static_cast<int64_t>(s), ang);
+        angles_of(a.rot, at, pos, ang);
     };
 
     u32x4 raw[VPL], grad[VPL];
     float rs[NORM == 1 ? 1 : VPL];
     Angles<E / 2> ang;
+    positions(first);
     fetch(first, raw, grad, rs, ang);
+    positions(first + stride);
     int buf = 0;
     for (int64_t base = first; base < a.N; base += stride) {
         u32x4 nxt[VPL], ngrad[VPL];
         float nrs[NORM == 1 ? 1 : VPL];
         Angles<E / 2> nang;
         fetch(base + stride, nxt, ngrad, nrs, nang);
+        positions(base + 2 * stride);
         const int64_t n = base + (static_cast<int64_t>(me.team) << tokens_log2) + me.sub;
         const bool here = n < a.N;
         // gradients that do not count are zeros: x beside them is a row's own, so that no product is NaN but the row's own

@@ -1,6 +1,6 @@
 """hipcc's resource report for the kernels of the row codes, their product and the rotations: none has scratch, but for a few
-registers around the loop of row norms in bf16 (measured with them: a wave more on a SIMD is worth more), and for fp32 rows of
-more than 32 rounds of heads, which eight waves hold with eight units a lane.  Needs only hipcc."""
+registers of row norms in bf16 (measured with them: a wave more on a SIMD, or four units a lane, are worth more), and for fp32 rows
+of more than 32 rounds of heads, which eight waves hold with eight units a lane.  Needs only hipcc."""
 import os
 import re
 import shutil
@@ -11,8 +11,8 @@ import pytest
 
 from paper_2605_17923_amd import build
 
-ALLOWED = {r"rotary_fwd_kernel<lnmod::bf16_io, 1, (true|false), 3>": 12, r"rotary_bwd_kernel<lnmod::bf16_io, 1, false, 4>": 12,
-           r"rotary_bwd_kernel<lnmod::f32_io, 1, (true|false), 8>": 204}
+ALLOWED = {r"rotary_fwd_kernel<lnmod::bf16_io, 1, (true|false), 3>": 12, r"rotary_bwd_kernel<lnmod::bf16_io, 1, (true|false), 4>": 32,
+           r"rotary_bwd_kernel<lnmod::f32_io, 1, (true|false), 8>": 236}
 
 
 def test_no_scratch(tmp_path):
