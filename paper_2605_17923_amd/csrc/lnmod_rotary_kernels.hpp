@@ -13,10 +13,10 @@
 // token are loaded once for all of them.  Lanes without a unit of their own read a neighbour's and write nothing.
 //
 // HBM bounds the large ones: 75 600 x 40 x 128 bf16, queries and keys, 552 us, 5.6 TB/s; with the norm over rows 32 760 x 40 x 128
-// from dense tensors 240 us forwards (5.6 TB/s), 380 backwards with gradients that have the heads in front (5.3; 365 without).  The
+// from dense tensors 243 us forwards (5.5 TB/s), 335 backwards (6.0), 342 with gradients that have the heads in front.  The
 // next token's units are loaded while this one's are worked on.  Heads of 96 features leave a quarter of the lanes idle, and with
-// them a quarter of the loads that could be under way: 24 + 8 heads in halves, a norm for each, 28 837 tokens 97 and 125 us (3.7
-// and 4.3 TB/s), where 24 x 128 reach 5.7.
+// them a quarter of the loads that could be under way: 24 + 8 heads in halves, a norm for each, 28 837 tokens 96 and 122 us (3.7
+// and 4.4 TB/s), where 24 x 128 reach 5.6 and 6.0.
 #pragma once
 #include "lnmod_kernels.hpp"
 #include "lnmod_rotary.hpp"
