@@ -71,14 +71,18 @@ void lay_out(RotaryArgs& a, int dtype) {
 // Blocks forwards are what a CU holds at once where a norm over rows has its weights loaded (64 heads of 128: 203 us with four
 // blocks a CU where three fit, 188 with three).  Else, and where blocks of three waves would have to be packed four to a CU,
 // which they are after an idle moment (32 760 x 40 x 128: 238 us) but not while another kernel drains (316, with 32 blocks a CU
-// 244), more of them even out the CUs (75 600 x 40 x 128 without a norm: 586 us with blocks of four waves, 550 with two tokens
-// side by side in eight).
+// 244), more of them even out the CUs (a row of four waves without a norm: two tokens side by side in a block of eight, 75 600 x
+// 40 x 128 586 -> 550 us).
+//
+// Without a norm one block of six waves a CU is better still where the queries' rows are the keys' and three waves take a row, or
+// fewer and no round of heads is idle: 75 600 x 40 x 128 540 -> 529 us, 6000 tokens of it 57 -> 47, 32 760 x 36 x 128 215 -> 204,
+// 75 600 x 12 x 128 165 -> 160.  Not with idle rounds (20 heads: 146 and 150 us), nor with pairs of halves (24 x 128: 159 and 163).
 //
 // Backwards a block keeps its partial sums, and one for a CU is best: of eight waves where a row takes two or more (32 760 x 40 x 128
 // 360 us in two blocks of four waves, 335 in one of eight), else of four (24 heads of 128, a norm for each: 258 us in two blocks
 // of four waves, 245 in one), twice that where a lane has two units only.  Rows of different lengths, of queries and of
 // keys, take three times as many blocks (28 and 4 heads: 235 -> 204 us).
-RotaryShape shape_for(const RotaryArgs& a, int norm, bool backward) {
+RotaryShape shape_for(const RotaryArgs& a, bool halves, int norm, bool backward) {
     int rounds = 1;
     for (const RotarySide& s : a.side) {
         if (s.heads == 0) continue;
@@ -98,9 +102,13 @@ RotaryShape shape_for(const RotaryArgs& a, int norm, bool backward) {
     if (norm == kRowNorm) {                                          // eight waves hold a row
         while (waves_of(vpl) > 8) vpl = vpl < 4 ? vpl + 1 : 8;
     }
+    const bool even = a.side[0].heads == a.side[1].heads || a.side[1].heads == 0;
+    if (norm == kNoNorm && even && !halves) {
+        const int v = rounds > 9 && waves_of(4) == 3 ? 4 : vpl, k = waves_of(v);
+        if (v >= 3 && (k == 3 || (6 % k == 0 && k * v == rounds))) return {v, 6, 1};
+    }
     int waves = waves_of(vpl), per_cu = 32;
     if (waves > 8) waves = 8;
-    const bool even = a.side[0].heads == a.side[1].heads;
     if (backward && even && norm == kRowNorm && waves > 1) waves = 8 / waves * waves;
     else if (waves < 4) waves = waves * (4 / waves);
     else if (waves == 4 && norm == kNoNorm) waves = 8;
@@ -121,13 +129,13 @@ void rotary_bwd_slots(int dtype, int64_t N, const int32_t (&heads)[2], int head_
     a.head_dim = head_dim;
     for (int t = 0; t < 2; ++t) a.side[t].heads = heads[t];
     lay_out(a, dtype);
-    plan_rotary(a, shape_for(a, norm, true), norm != kRowNorm);
+    plan_rotary(a, shape_for(a, false, norm, true), norm != kRowNorm);
     for (int t = 0; t < 2; ++t) slots[t] = a.side[t].blocks;
 }
 
 hipError_t launch_rotary_fwd(int dtype, int norm, bool halves, RotaryArgs a, hipStream_t st) {
     lay_out(a, dtype);
-    const RotaryShape sh = shape_for(a, norm, false);
+    const RotaryShape sh = shape_for(a, halves, norm, false);
     plan_rotary(a, sh, norm != kRowNorm);
     a.sample_of = Divider(static_cast<uint32_t>(a.S));
     const bool ok = norm == kNoNorm    ? by_type<Fwd, kNoNorm>(dtype, halves, a, sh, st)
@@ -139,7 +147,7 @@ hipError_t launch_rotary_fwd(int dtype, int norm, bool halves, RotaryArgs a, hip
 hipError_t launch_rotary_bwd(int dtype, int norm, bool halves, RotaryArgs a, void* const (&dw)[2], bool io_grads, float* ws,
                              hipStream_t st) {
     lay_out(a, dtype);
-    const RotaryShape sh = shape_for(a, norm, true);
+    const RotaryShape sh = shape_for(a, false, norm, true);
     plan_rotary(a, sh, norm != kRowNorm);
     a.sample_of = Divider(static_cast<uint32_t>(a.S));
     RotaryDwArgs r{};

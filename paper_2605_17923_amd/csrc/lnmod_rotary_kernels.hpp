@@ -196,26 +196,42 @@ __global__ __launch_bounds__(8 * kWave) LNMOD_OCCUPANCY(VPL <= 3 ? 4 : VPL == 4 
 
     const int64_t stride = (static_cast<int64_t>(side.members) * side.teams) << tokens_log2;
     const int64_t first = ((member * side.teams) << tokens_log2);
+    // Positions are loaded two steps ahead where there is no norm, so that a step's angles, which they choose, come with its units
+    // and six waves keep a CU's share of HBM busy: 32 760 x 40 x 128 from tensors with the heads in front 248 -> 231 us.  A norm
+    // over rows, which waits between its loads and its stores in any case, had nothing of it and paid the longer start
+    // (32 760 x 12 x 128 77 -> 85 us).
+    constexpr bool kAhead = NORM == 0;
+    auto token = [&](int64_t base) {
+        const int64_t n = base + (static_cast<int64_t>(me.team) << tokens_log2) + me.sub;
+        return n < a.N ? n : a.N - 1;
+    };
+    int32_t pos[E / 2];
+    auto positions = [&](int64_t base) {
+        const int64_t n = token(base);
+        const uint32_t b = a.rot.per_token ? 0u : a.sample_of(static_cast<uint32_t>(n));
+        positions_of(a.rot, at, n - static_cast<int64_t>(b) * a.S, pos);
+    };
     auto fetch = [&](int64_t base, u32x4 (&raw)[VPL], Angles<E / 2>& ang) {
-        int64_t n = base + (static_cast<int64_t>(me.team) << tokens_log2) + me.sub;
-        if (n >= a.N) n = a.N - 1;
+        const int64_t n = token(base);
         const uint32_t b = a.sample_of(static_cast<uint32_t>(n)), s = static_cast<uint32_t>(n) - b * a.S;
         const char* x = side.x.p + b * side.x.batch + s * side.x.token;
 #pragma unroll
         for (int i = 0; i < VPL; ++i) raw[i] = at.load(x + in[i]);
-        int32_t pos[E / 2];
-        positions_of(a.rot, at, a.rot.per_token ? n : static_cast<int64_t>(s), pos);
+        if (!kAhead) positions_of(a.rot, at, a.rot.per_token ? n : static_cast<int64_t>(s), pos);
         angles_of(a.rot, at, pos, ang);
     };
 
     u32x4 raw[VPL];
     Angles<E / 2> ang;
+    if (kAhead) positions(first);
     fetch(first, raw, ang);
+    if (kAhead) positions(first + stride);
     int buf = 0;
     for (int64_t base = first; base < a.N; base += stride) {
         u32x4 nxt[VPL];
         Angles<E / 2> nang;
         fetch(base + stride, nxt, nang);
+        if (kAhead) positions(base + 2 * stride);
         const int64_t n = base + (static_cast<int64_t>(me.team) << tokens_log2) + me.sub;
         const bool here = n < a.N;
         float rs = 1.0f;
@@ -306,10 +322,8 @@ __global__ __launch_bounds__(8 * kWave) void rotary_bwd_kernel(const RotaryArgs 
 
     const int64_t stride = (static_cast<int64_t>(side.members) * side.teams) << tokens_log2;
     const int64_t first = ((member * side.teams) << tokens_log2);
-    // Positions are loaded two steps ahead, so that a step's angles, which they choose, come with its units.  32 760 x 40 x 128,
-    // a norm over rows, in the best shape of each: 365 us with the positions loaded beside the units, 334 so (gradients with the
-    // heads in front 394 and 341).  Forwards, where blocks are many and short, the longer start costs what this saves (75 600 x
-    // 40 x 128 without a norm 536 and 530 us, 32 760 x 12 x 128 69 and 72).
+    // Positions two steps ahead, as forwards without a norm.  32 760 x 40 x 128, a norm over rows, in the best shape of each: 365 us
+    // with the positions loaded beside the units, 334 so (gradients with the heads in front 394 and 341).
     auto token = [&](int64_t base) {
         const int64_t n = base + (static_cast<int64_t>(me.team) << tokens_log2) + me.sub;
         return n < a.N ? n : a.N - 1;
