@@ -60,7 +60,7 @@ void lay_out(RotaryArgs& a, int dtype) {
     a.g_log2 = ceil_log2(a.units);
 }
 
-// Launch shapes, from sweeps of 1 to 4 units a lane, 1 to 8 waves a block and 1 to 128 blocks a CU over 65 problems (both types,
+// Launch shapes, from sweeps of 1 to 4 units a lane, 1 to 8 waves a block and 1 to 128 blocks a CU over 73 problems (both types,
 // 4 to 64 heads of 64 to 256 features, 1560 to 75 600 tokens).
 //
 // Three units a lane where nothing is against it: more loads in flight than with fewer, and registers for four waves a SIMD.

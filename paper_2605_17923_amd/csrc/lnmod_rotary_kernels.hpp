@@ -12,7 +12,7 @@
 // its block and meets that place in several heads of a token, so the four (fp32: two) cosines and sines that it needs for a
 // token are loaded once for all of them.  Lanes without a unit of their own read a neighbour's and write nothing.
 //
-// HBM bounds the large ones: 75 600 x 40 x 128 bf16, queries and keys, 552 us, 5.6 TB/s; with the norm over rows 32 760 x 40 x 128
+// HBM bounds the large ones: 75 600 x 40 x 128 bf16, queries and keys, 533 us, 5.8 TB/s; with the norm over rows 32 760 x 40 x 128
 // from dense tensors 243 us forwards (5.5 TB/s), 335 backwards (6.0), 342 with gradients that have the heads in front.  The
 // next token's units are loaded while this one's are worked on.  Heads of 96 features leave a quarter of the lanes idle, and with
 // them a quarter of the loads that could be under way: 24 + 8 heads in halves, a norm for each, 28 837 tokens 96 and 122 us (3.7
