@@ -937,6 +937,14 @@ inline void deal_tiles(ProductArgs& a, int bm, int bn) {
     a.band_of = Divider(static_cast<uint32_t>(kBandRows) * a.tiles_n);
     a.row_of = Divider(a.tiles_m % kBandRows ? a.tiles_m % kBandRows : kBandRows);
 }
+// A wave's outputs begin at (m0, n0); without any it has no scale and no bias to read either.
+constexpr bool has_outputs(const ProductArgs& a, int64_t m0, int64_t n0) { return m0 < a.M && n0 < a.N; }
+// Of `count` rows (or features) from `first` on, the last one that there is in `total`, counted from `first`; whoever is beyond
+// it reads that one.
+constexpr int last_of(int64_t total, int64_t first, int count) {
+    return static_cast<int>(total - 1 - first < count - 1 ? total - 1 - first : count - 1);
+}
+constexpr int held(int at, int last) { return at < last ? at : last; }
 hipError_t launch_product(int dtype, int code, ProductArgs a, hipStream_t st);
 
 }  // namespace lnmod

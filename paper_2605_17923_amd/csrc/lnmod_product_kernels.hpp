@@ -121,27 +121,24 @@ struct Scales {
     static constexpr bool kHalf = std::is_same<Tag, bf16_io>::value;
     float a[TM], w[TN / 2][8];
     u32x4 b[TN / 2][Unit<Tag>::NV];
-    // m0 and n0 are uniform; rows and features beyond the last one have the last one's
+    // m0 and n0 are uniform, and there are outputs (has_outputs); rows and features beyond the last one have the last one's
     __device__ inline void load_rows(const ProductArgs& p, int64_t m0) {
         const int lane = threadIdx.x & (kWave - 1);
-        const int rows = static_cast<int>(p.M - 1 - m0 < TM * 16 ? p.M - 1 - m0 : TM * 16);
+        const int last = last_of(p.M, m0, TM * 16);
         const Row ra = row_of(p.sa, m0 * 4, 0x7fffffffu);
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            const int m = i * 16 + (lane & 15);
-            a[i] = load_float(ra, (m < rows ? m : rows) * 4);
-        }
+        for (int i = 0; i < TM; ++i) a[i] = load_float(ra, held(i * 16 + (lane & 15), last) * 4);
     }
     // of the pairs of fragments from `from` to `to` - 1
     __device__ inline void load_features(const ProductArgs& p, int64_t n0, int from, int to) {
         constexpr int kBytes = IO<Tag>::kBytes;
         const int lane = threadIdx.x & (kWave - 1);
-        const int most = static_cast<int>(p.N - 1 - n0 < TN * 16 ? p.N - 1 - n0 : TN * 16);
+        const int last = last_of(p.N, n0, TN * 16);
         const Row rw = row_of(p.sw, n0 * 4, 0x7fffffffu), rb = row_of(p.bias, n0 * kBytes, 0x7fffffffu);
 #pragma unroll
         for (int j = from; j < to; ++j) {
             const int n = j * 32 + (lane >> 4) * 8;
-            if (p.wide && n + 7 <= most) {   // eight at a time, whatever they are aligned to
+            if (p.wide && n + 7 <= last) {   // eight at a time, whatever they are aligned to
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const f32x4 t = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, n * 4 + 16 * h, 0, 0));
@@ -156,7 +153,7 @@ struct Scales {
             float v[8] = {};
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const int at = n + e < most ? n + e : most;
+                const int at = held(n + e, last);
                 w[j][e] = load_float(rw, at * 4);
                 if (!p.bias) continue;
                 if constexpr (kHalf) v[e] = __builtin_bit_cast(float, static_cast<uint32_t>(__builtin_amdgcn_raw_buffer_load_b16(rb, at * 2, 0, 0)) << 16);
@@ -172,6 +169,7 @@ template <typename C, typename Tag, int TM, int TN>
 __device__ inline void store_products(const ProductArgs& p, const typename Mac<C, Tag>::Sum (&acc)[TM][TN], int64_t m0, int64_t n0) {
     constexpr bool kHalf = std::is_same<Tag, bf16_io>::value;
     const int lane = threadIdx.x & (kWave - 1);
+    if (!has_outputs(p, m0, n0)) return;
     Scales<Tag, TM, TN> s;
     s.load_rows(p, m0);
     if (kHalf) s.load_features(p, n0, 0, TN / 2);
