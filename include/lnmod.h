@@ -368,8 +368,8 @@ int lnmod_quantize_rows(const void* x, int64_t N, int64_t D, void* stream, void*
  *     y[m,n] = (sum_k a[m,k]*w[n,k]) * a_scales[m] * w_scales[n] + bias[n]
  *
  * a: [M, K], w: [N, K] (a linear layer's weight as it is stored), both of type `code`; a_scales: float32 [M]; w_scales: float32
- * [N]; bias: [N] in the I/O dtype or NULL; y: [M, N] in the I/O dtype, rounded once.  The sum is exact for LNMOD_INT8 (32-bit
- * integers).  For LNMOD_E4M3 it is float32's where y is; where y is bf16 the matrix unit adds the products of eight neighbouring
+ * [N]; bias: [N] in the I/O dtype or NULL; y: [M, N] in the I/O dtype, rounded once.  The scaled sum is beyond float32 only where
+ * its value is, however far apart the two scales are.  The sum is exact for LNMOD_INT8 (32-bit integers).  For LNMOD_E4M3 it is float32's where y is; where y is bf16 the matrix unit adds the products of eight neighbouring
  * features with 13 bits below the largest of them, which is less than a hundredth of bf16's own rounding on ordinary values.  A
  * code that is NaN makes its row or column NaN, as does a scale that is.  K is a multiple of 8, 8 <= K < 2^17
  * (LNMOD_EUNSUPPORTED); M, N < 2^31; M == 0 or N == 0 does nothing.  a, w and y are 16-byte aligned, the scales and bias at any
