@@ -235,6 +235,7 @@ size_t lnmod_gated_backward_workspace_bytes(int64_t B_or_nseg, int64_t total_tok
  * for (x, w, y, rstd) = (q, wq, q_out, rstd_q) and (k, wk, k_out, rstd_k).  q, k, q_out, k_out:
  * [N, D] in the I/O dtype; wq, wk: [D] in the I/O dtype; rstd_q, rstd_k: float32 [N] (written).
  * N is the number of rows normalised (tokens, or tokens x heads when D is one head's width).
+ * All in float32: a row whose sum of squares is beyond it (values above 1.8e19) has rstd 0, so y and dx are 0.
  * Errors as for lnmod_forward.
  */
 int lnmod_qknorm_forward(const void* q, const void* k, const void* wq, const void* wk,
@@ -369,9 +370,11 @@ int lnmod_quantize_rows(const void* x, int64_t N, int64_t D, void* stream, void*
  *
  * a: [M, K], w: [N, K] (a linear layer's weight as it is stored), both of type `code`; a_scales: float32 [M]; w_scales: float32
  * [N]; bias: [N] in the I/O dtype or NULL; y: [M, N] in the I/O dtype, rounded once.  The scaled sum is beyond float32 only where
- * its value is, however far apart the two scales are.  The sum is exact for LNMOD_INT8 (32-bit integers).  For LNMOD_E4M3 it is float32's where y is; where y is bf16 the matrix unit adds the products of eight neighbouring
- * features with 13 bits below the largest of them, which is less than a hundredth of bf16's own rounding on ordinary values.  A
- * code that is NaN makes its row or column NaN, as does a scale that is.  K is a multiple of 8, 8 <= K < 2^17
+ * its value is, however far apart the two scales are.  The sum is exact for LNMOD_INT8 (32-bit integers).  For LNMOD_E4M3 it is
+ * float32's where y is.  Where y is bf16 the matrix unit adds the products of eight neighbouring features with 13 bits below the
+ * largest of them: the sum is off by less than 7 * 2^-13 of the sum, over the eights, of their largest product, which on ordinary
+ * values is about a hundredth of bf16's own rounding: two outputs in a hundred round to the other neighbour of their value.
+ * A code that is NaN makes its row or column NaN, as does a scale that is.  K is a multiple of 8, 8 <= K < 2^17
  * (LNMOD_EUNSUPPORTED); M, N < 2^31; M == 0 or N == 0 does nothing.  a, w and y are 16-byte aligned, the scales and bias at any
  * of their elements' addresses.
  */
@@ -425,6 +428,7 @@ int lnmod_rotary(const lnmod_heads* q, const lnmod_heads* k, int64_t B, int64_t 
  *
  *     rstd = 1/sqrt(mean x^2 + eps)      y = rotation of (x*rstd)*w
  *
+ * in float32 (a row whose sum of squares is beyond it has rstd 0, and y and dx are 0 there, as in lnmod_qknorm_forward),
  * over all heads of a token (per_head 0; w [heads*head_dim], rstd float32 [B*S], heads*head_dim <= 8192) or over each head
  * (w [head_dim], rstd float32 [B*S, heads]).  Both tensors are required.
  *
