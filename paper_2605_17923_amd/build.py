@@ -36,6 +36,7 @@ HEADERS = [os.path.join(CSRC, "lnmod_kernels.hpp"), os.path.join(CSRC, "lnmod_la
            os.path.join(CSRC, "lnmod_quant_kernels.hpp"),
            os.path.join(CSRC, "lnmod_ckpt_kernels.hpp"), os.path.join(CSRC, "lnmod_rmsq_kernels.hpp"),
            os.path.join(CSRC, "lnmod_rowcodes_kernels.hpp"), os.path.join(CSRC, "lnmod_product_kernels.hpp"),
+           os.path.join(CSRC, "lnmod_product_plan.hpp"),
            os.path.join(CSRC, "lnmod_rotary.hpp"), os.path.join(CSRC, "lnmod_rotary_kernels.hpp"),
            os.path.join(CSRC, "lnmod_api_impl.hpp"),
            os.path.join(INCLUDE, "lnmod.h"), os.path.join(INCLUDE, "lnmod_sched.h"),

@@ -2,7 +2,7 @@
 //
 //   y[m,n] = (sum_k a[m,k] w[n,k]) sa[m] sw[n] + bias[n]
 //
-// Three kernels, by what bounds a product (lnmod_product.hip picks).  A few rows read w once: HBM, and the 2 to 3 us that a launch
+// Three kernels, by what bounds a product (lnmod_product_plan.hpp picks).  A few rows read w once: HBM, and the 2 to 3 us that a launch
 // and a chain of loads take.  Products of some hundred rows or features have few tiles, and each step of a tile waits for the
 // caches: small tiles, several steps on their way, teams of waves that share out the sum.  Large ones are bound by the matrix
 // instructions and by what LDS gives them, 256 x 256 outputs a block.
@@ -11,13 +11,12 @@
 // fragment takes are chosen so that a lane ends up with eight neighbouring outputs: one store of 16 bytes in bf16.
 #pragma once
 #include "lnmod_code.hpp"
+#include "lnmod_product_plan.hpp"
 
 namespace lnmod {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-
-constexpr int kBlockK = 128;                 // features of a step: one cache line of a row
 
 // Sums and products of sixteen rows of each operand.  A lane holds 32 codes of one row: features 16 (lane / 16) .. + 15 of
 // the first and of the second half of a step.  Which feature goes where is no matter as long as both operands agree.
@@ -249,7 +248,7 @@ __device__ inline void load_lds(Row src, uint32_t offset, int uniform, const uin
 // which one is multiplied while the others are on their way, and adds its sums to the first team's at the end.
 //
 // What bounds it is the way from the caches: a CU has one block or two, and a step lasts as long as its lines need, however
-// small the tile (0.33 to 0.86 us, lnmod_product.hip).  So the lines of several steps are on their way at a time, teams take
+// small the tile (0.33 to 0.86 us, lnmod_product_plan.hpp).  So the lines of several steps are on their way at a time, teams take
 // steps side by side, and the tile is the smallest that still fills the CUs: 1025 x 2600 by 1433 to float32 13.5 us (45 in
 // tiles of the first kernel, 128 x 128), 96 x 4096 by 12 288 e4m3 12.1 us, 4.4 TB/s (50).
 template <typename C, typename Tag, int BM, int BN, int WM, int WN, int STAGES, int GROUPS>

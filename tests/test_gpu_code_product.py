@@ -62,8 +62,8 @@ def test_product(size, code, dtype):
     product(code, dtype, *size, bias=size[0] % 2 == 0, whole=True)
 
 
-# products that the tiles of 256 x 256 take: sizes that end inside a tile, one step, an odd and an even number of them, a tail,
-# several tiles for a block
+# products of 128 x 128 and 128 x 256 tiles: sizes that end inside a tile, one step, an odd and an even number of them, a tail, many
+# tiles (those of 256 x 256 are in test_gpu_product_large.py)
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("code", ["int8", "e4m3"])
 @pytest.mark.parametrize("size", [(2049, 2056, 128), (4097, 1030, 24), (2305, 1900, 256), (300, 16001, 136), (8200, 520, 384),
