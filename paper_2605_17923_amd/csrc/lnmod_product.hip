@@ -18,8 +18,8 @@ hipError_t go(ProductArgs a, hipStream_t st) {
     constexpr bool kHalves = std::is_same<C, e4m3_code>::value && std::is_same<Tag, f32_io>::value;
     switch (pick_product(a.M, a.N, a.K, kHalves)) {
         case kFew: {
-            const uint32_t blocks = static_cast<uint32_t>((a.N + 15) / 16), x = blocks < kRowOfBlocks ? blocks : kRowOfBlocks;
-            hipLaunchKernelGGL((product_few_kernel<C, Tag, 1, 1, 2, 8>), dim3(x, (blocks + x - 1) / x), dim3(8 * kWave), 0, st, a);
+            const uint32_t blocks = static_cast<uint32_t>((a.N + kFewOutputs - 1) / kFewOutputs), x = blocks < kRowOfBlocks ? blocks : kRowOfBlocks;
+            hipLaunchKernelGGL((product_few_kernel<C, Tag>), dim3(x, (blocks + x - 1) / x), dim3(kFewWaves * kWave), 0, st, a);
             break;
         }
         case 1: tiles<C, Tag, 32, 32, 2, 1, 4, 4>(a, st); break;

@@ -364,96 +364,71 @@ __global__ __launch_bounds__(GROUPS* WM* WN* kWave) void product_tile_kernel(con
 }
 
 // ---- few rows --------------------------------------------------------------------------------------------------------
-// Up to 16 TM rows of a: w is read once, straight into registers, and that takes all the time there is.  A block has 16 TN
-// features of y; its waves share out the steps and add their sums in LDS, wave by wave.  1 x 1536 by 1536 int8 3.0 us, where a
-// launch that does nothing takes 2.5; 1 x 4096 by 4096 7 us.
-template <typename C, typename Tag, int TM, int TN, int DEPTH, int kFewWaves>
+// Up to 16 rows of a: w is read once, straight into registers, and that takes all the time there is.  A block has 16 features of
+// y; its waves share out the steps and add their sums in LDS, wave by wave.  1 x 1536 by 1536 int8 3.0 us, where a launch that does
+// nothing takes 2.5; 1 x 4096 by 4096 7 us.
+constexpr int kFewWaves = 8, kFewDepth = 2, kFewOutputs = 16;
+
+template <typename C, typename Tag>
 __global__ __launch_bounds__(kFewWaves* kWave) void product_few_kernel(const ProductArgs a) {
     using mac = Mac<C, Tag>;
     typedef typename mac::Sum Sum;
-    constexpr int kRows = 16 * TM, kFeatures = 16 * TN;
-    __shared__ Sum part[kFewWaves][TM * TN][kWave];
+    __shared__ Sum part[kFewWaves][kWave];
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int K = a.K, whole = K / kBlockK;
-    const int64_t n0 = (static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * kFeatures;
+    const int64_t n0 = (static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * kFewOutputs;
     if (n0 >= a.N) return;
     const Row xrow = row_of(a.a, 0, 0x7fffffffu), wrow = row_of(a.w, n0 * K, 0x7fffffffu);
-    uint32_t xo[TM], wo[TN];
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int r = i * 16 + (lane & 15), most = static_cast<int>(a.M) - 1;
-        xo[i] = static_cast<uint32_t>(r < most ? r : most) * K + (lane >> 4) * 16;
-    }
-#pragma unroll
-    for (int j = 0; j < TN; ++j) {
-        const int64_t r = j * 16 + (lane & 15), most = a.N - 1 - n0;
-        wo[j] = static_cast<uint32_t>(r < most ? r : most) * K + (lane >> 4) * 16;
-    }
+    const int r = lane & 15;
+    const uint32_t xo = static_cast<uint32_t>(held(r, last_of(a.M, 0, kFewOutputs))) * K + (lane >> 4) * 16;
+    const uint32_t wo = static_cast<uint32_t>(held(r, last_of(a.N, n0, kFewOutputs))) * K + (lane >> 4) * 16;
 
-    Sum acc[TM][TN];
+    Sum acc = mac::zero();
+    auto multiply = [&](const i32x4 (&x)[2], const i32x4 (&w)[2]) __attribute__((always_inline)) {
+        const typename mac::Frag xf = mac::frag(x[0], x[1]), wf = mac::frag(w[0], w[1]);
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = mac::zero();
-    auto multiply = [&](const i32x4 (&x)[TM][2], const i32x4 (&w)[TN][2]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            const typename mac::Frag xf = mac::frag(x[i][0], x[i][1]);
-#pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                const typename mac::Frag wf = mac::frag(w[j][0], w[j][1]);
-#pragma unroll
-                for (int h = 0; h < mac::kParts; ++h) acc[i][j] = mac::add(wf, xf, acc[i][j], h);
-            }
-        }
+        for (int h = 0; h < mac::kParts; ++h) acc = mac::add(wf, xf, acc, h);
     };
-    // DEPTH steps are requested before the first of them is multiplied; steps beyond the whole ones are read again and not used
-    for (int t = wave; t < whole; t += DEPTH * kFewWaves) {
-        i32x4 x[DEPTH][TM][2], w[DEPTH][TN][2];
+    // kFewDepth steps are requested before the first of them is multiplied; steps beyond the whole ones are read again and not used
+    for (int t = wave; t < whole; t += kFewDepth * kFewWaves) {
+        i32x4 x[kFewDepth][2], w[kFewDepth][2];
 #pragma unroll
-        for (int d = 0; d < DEPTH; ++d) {
+        for (int d = 0; d < kFewDepth; ++d) {
             const int k0 = (t + d * kFewWaves < whole ? t + d * kFewWaves : t) * kBlockK;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                for (int j = 0; j < TN; ++j) w[d][j][h] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(wrow, wo[j] + 64 * h, k0, 0));
-#pragma unroll
-                for (int i = 0; i < TM; ++i) x[d][i][h] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(xrow, xo[i] + 64 * h, k0, 0));
+                w[d][h] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(wrow, wo + 64 * h, k0, 0));
+                x[d][h] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(xrow, xo + 64 * h, k0, 0));
             }
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int d = 0; d < DEPTH; ++d)
+        for (int d = 0; d < kFewDepth; ++d)
             if (t + d * kFewWaves < whole) multiply(x[d], w[d]);
     }
     if (K % kBlockK != 0 && wave == whole % kFewWaves) {
-        i32x4 x[TM][2], w[TN][2];
+        i32x4 x[2], w[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int left = K - whole * kBlockK - (lane >> 4) * 16 - 64 * h;
-#pragma unroll
-            for (int j = 0; j < TN; ++j) w[j][h] = __builtin_bit_cast(i32x4, load_codes16(wrow, wo[j] + 64 * h, whole * kBlockK, left));
-#pragma unroll
-            for (int i = 0; i < TM; ++i) x[i][h] = __builtin_bit_cast(i32x4, load_codes16(xrow, xo[i] + 64 * h, whole * kBlockK, left));
+            w[h] = __builtin_bit_cast(i32x4, load_codes16(wrow, wo + 64 * h, whole * kBlockK, left));
+            x[h] = __builtin_bit_cast(i32x4, load_codes16(xrow, xo + 64 * h, whole * kBlockK, left));
         }
         multiply(x, w);
     }
 
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) part[wave][i * TN + j][lane] = acc[i][j];
+    part[wave][lane] = acc;
     __syncthreads();
-    // fragment f of lane l: rows of a 16 (f / TN) + l % 16, features 16 (f % TN) + 4 (l / 16) .. + 3
-    for (int o = threadIdx.x; o < kRows * kFeatures; o += kFewWaves * kWave) {
-        const int m = o / kFeatures, f = o % kFeatures;
+    // lane l: row l % 16 of a, features 4 (l / 16) .. + 3
+    for (int o = threadIdx.x; o < kFewOutputs * kFewOutputs; o += kFewWaves * kWave) {
+        const int m = o / kFewOutputs, f = o % kFewOutputs;
         const int64_t n = n0 + f;
         if (m >= a.M || n >= a.N) continue;
-        const int frag = (m / 16) * TN + f / 16, l = (f % 16) / 4 * 16 + m % 16, e = f % 4;
-        auto sum = part[0][frag][l][e];
+        const int l = f / 4 * 16 + m, e = f % 4;
+        auto sum = part[0][l][e];
 #pragma unroll
-        for (int w = 1; w < kFewWaves; ++w) sum += part[w][frag][l][e];
+        for (int w = 1; w < kFewWaves; ++w) sum += part[w][l][e];
         const float sa = a.sa[m], sw = a.sw[n];
         float v = static_cast<float>(sum) * sa * sw;
         if (!plain_scale(sa)) v = far_scaled(static_cast<float>(sum), sa, sw);
