@@ -250,7 +250,8 @@ __device__ inline void load_lds(Row src, uint32_t offset, int uniform, const uin
 // What bounds it is the way from the caches: a CU has one block or two, and a step lasts as long as its lines need, however
 // small the tile (0.33 to 0.86 us, lnmod_product_plan.hpp).  So the lines of several steps are on their way at a time, teams take
 // steps side by side, and the tile is the smallest that still fills the CUs: 1025 x 2600 by 1433 to float32 13.5 us (45 in
-// tiles of the first kernel, 128 x 128), 96 x 4096 by 12 288 e4m3 12.1 us, 4.4 TB/s (50).
+// tiles of the first kernel, 128 x 128), 96 x 4096 by 12 288 e4m3 12.1 us (50).  Both are with w in the last-level cache; from HBM 16.2
+// and 17.3 us, the latter 3.1 TB/s.
 template <typename C, typename Tag, int BM, int BN, int WM, int WN, int STAGES, int GROUPS>
 __global__ __launch_bounds__(GROUPS* WM* WN* kWave) void product_tile_kernel(const ProductArgs a) {
     using mac = Mac<C, Tag>;
@@ -365,8 +366,8 @@ __global__ __launch_bounds__(GROUPS* WM* WN* kWave) void product_tile_kernel(con
 
 // ---- few rows --------------------------------------------------------------------------------------------------------
 // Up to 16 rows of a: w is read once, straight into registers, and that takes all the time there is.  A block has 16 features of
-// y; its waves share out the steps and add their sums in LDS, wave by wave.  1 x 1536 by 1536 int8 3.0 us, where a launch that does
-// nothing takes 2.5; 1 x 4096 by 4096 7 us.
+// y; its waves share out the steps and add their sums in LDS, wave by wave.  In a graph of such calls, int8, with w in the last-level
+// cache and from HBM: 1 x 1536 by 1536 2.8 and 3.7 us, 16 x 2048 by 4096 3.7 and 4.8, 1 x 4096 by 4096 4.7 and 6.1.
 constexpr int kFewWaves = 8, kFewDepth = 2, kFewOutputs = 16;
 
 template <typename C, typename Tag>

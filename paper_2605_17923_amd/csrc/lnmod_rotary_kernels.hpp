@@ -14,9 +14,12 @@
 //
 // HBM bounds the large ones: 75 600 x 40 x 128 bf16, queries and keys, 533 us, 5.8 TB/s; with the norm over rows 32 760 x 40 x 128
 // from dense tensors 243 us forwards (5.5 TB/s), 335 backwards (6.0), 342 with gradients that have the heads in front.  The
-// next token's units are loaded while this one's are worked on.  Heads of 96 features leave a quarter of the lanes idle, and with
-// them a quarter of the loads that could be under way: 24 + 8 heads in halves, a norm for each, 28 837 tokens 96 and 122 us (3.7
-// and 4.4 TB/s), where 24 x 128 reach 5.6 and 6.0.
+// next token's units are loaded while this one's are worked on.
+//
+// Two forms are further from it.  Pairs of halves are loaded and stored by runs of eight bytes, twice the accesses: the same row
+// backward 331 us in pairs, 401 in halves, the rotation alone 225 and 258.  Heads of 96 features leave a quarter of the lanes idle, of 72
+// seven of sixteen, as a head's lanes are a power of two: 24 + 8 x 96, a norm for each head, 28 837 tokens 84 us forwards and 105
+// backwards in pairs, 95 and 127 in halves, where the bytes ask for 59 and 89.
 #pragma once
 #include "lnmod_kernels.hpp"
 #include "lnmod_rotary.hpp"

@@ -217,7 +217,7 @@ class _Rotary(torch.autograd.Function):
 
 def rotary(q, k, positions, table, axes, interleaved=True):
     """Rotary positions with several axes of q and k, [B, S, heads, head_dim] or packed [T, heads, head_dim]; k may be None,
-    and one tensor is returned then.  See lnmod.rotary, lnmod.rotary_table and lnmod.rotary_grid."""
+    and one tensor is returned then; the table gets no gradient.  See lnmod.rotary, lnmod.rotary_table and lnmod.rotary_grid."""
     host = lnmod.native()
     r = None if host is None else host.rotary(q, k, positions, table, axes, interleaved)
     return _Rotary.apply(q, k, positions, table, axes, interleaved) if r is None else r
