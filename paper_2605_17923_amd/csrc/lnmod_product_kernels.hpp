@@ -182,7 +182,7 @@ __device__ inline void store_scaled(const ProductArgs& p, const typename Mac<C, 
     const int lane = threadIdx.x & (kWave - 1);
 #pragma unroll
     for (int j = 0; j < TN / 2; ++j) {
-        if (!kHalf) s.load_features(p, n0, j, j + 1);                // float32 biases of all pairs at once would not fit beside the sums
+        if (!kHalf && j > 0) s.load_features(p, n0, j, j + 1);       // float32 biases of all pairs at once would not fit beside the sums
         const int64_t n = n0 + j * 32 + (lane >> 4) * 8;
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
@@ -227,7 +227,7 @@ __device__ inline void store_products(const ProductArgs& p, const typename Mac<C
     if (!has_outputs(p, m0, n0)) return;
     Scales<Tag, TM, TN> s;
     s.load_rows(p, m0);
-    if (std::is_same<Tag, bf16_io>::value) s.load_features(p, n0, 0, TN / 2);
+    s.load_features(p, n0, 0, std::is_same<Tag, bf16_io>::value ? TN / 2 : 1);      // on their way while the rows' scales are looked at
     bool plain = true;
 #pragma unroll
     for (int i = 0; i < TM; ++i) plain = plain & plain_scale(s.a[i]);
