@@ -235,7 +235,7 @@ size_t lnmod_gated_backward_workspace_bytes(int64_t B_or_nseg, int64_t total_tok
  * for (x, w, y, rstd) = (q, wq, q_out, rstd_q) and (k, wk, k_out, rstd_k).  q, k, q_out, k_out:
  * [N, D] in the I/O dtype; wq, wk: [D] in the I/O dtype; rstd_q, rstd_k: float32 [N] (written).
  * N is the number of rows normalised (tokens, or tokens x heads when D is one head's width).
- * All in float32: a row whose sum of squares is beyond it (values above 1.8e19) has rstd 0, so y and dx are 0.
+ * All in float32: a row of finite values whose sum of squares is beyond it (values above 1.8e19) has rstd 0, so y and dx are 0.
  * Errors as for lnmod_forward.
  */
 int lnmod_qknorm_forward(const void* q, const void* k, const void* wq, const void* wk,
@@ -428,7 +428,7 @@ int lnmod_rotary(const lnmod_heads* q, const lnmod_heads* k, int64_t B, int64_t 
  *
  *     rstd = 1/sqrt(mean x^2 + eps)      y = rotation of (x*rstd)*w
  *
- * in float32 (a row whose sum of squares is beyond it has rstd 0, and y and dx are 0 there, as in lnmod_qknorm_forward),
+ * in float32 (a row of finite values whose sum of squares is beyond it has rstd 0, so y and dx are 0, as in lnmod_qknorm_forward),
  * over all heads of a token (per_head 0; w [heads*head_dim], rstd float32 [B*S], heads*head_dim <= 8192) or over each head
  * (w [head_dim], rstd float32 [B*S, heads]).  Both tensors are required.
  *
